@@ -423,6 +423,104 @@ cb_status cb_probe_scores(const float *r2, int32_t Lt, int32_t Ht, const int32_t
                           void *stream);
 cb_status cb_rank_layers(const float *scores, int32_t Lt, int32_t Ls, int32_t k, int32_t *layer_sets);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Paged target cache (the paper stops at a materialised target cache; a serving engine keeps that cache in pages and its
+ * model reads it by attention).  Four calls of one chain:
+ *     cb_page_tables      block tables, slots and positions of a batch from its request lengths, on the device
+ *     cb_rope_axes        rotary embedding with several position axes (queries, new keys)
+ *     cb_paged_store      rows of a mapped cache (cb_apply*'s output) or of a step's new keys and values into their pages
+ *     cb_paged_attention  attention of the new rows of every request over its pages
+ * All lengths are read from device memory, so a step can be captured into a CUDA graph once and replayed as requests grow.
+ * Every tensor of a call lives on the current device.
+ *
+ * cb_page_pool: K and V of all layers in pages of page_size rows.  Element (layer, page, slot, head, c) is at
+ *     (bf16*)k + layer*stride_layer + page*stride_page + slot*stride_slot + head*stride_head + c
+ * which covers [layer][page][slot][head][c] and [layer][page][head][slot][c].  Channels are contiguous, k and v 16-byte
+ * aligned, strides multiples of 8 and below 2^39 elements; a stride of 0 only on a dimension of size 1
+ * (CB_ERR_UNSUPPORTED otherwise).  head_dim 64 or 128; page_size 8, 16, 32, 64, 128 or 256; n_pages < 2^31.
+ */
+typedef struct cb_page_pool {
+    void *k;
+    void *v;
+    int32_t n_layers, n_heads, head_dim, page_size;
+    int64_t n_pages;
+    int64_t stride_layer, stride_page, stride_slot, stride_head;
+} cb_page_pool;
+
+/*
+ * Tables of one step.  Request b holds cached_len[b] rows in the cache and brings new_len[b] more (device int32, negative
+ * counts as 0; the sum of new_len and every cached_len + new_len below 2^31).  It keeps the ceil(cached/page_size) pages
+ * that its row of block_table (device int32 [n_requests][max_pages], row b at b*table_stride) lists, and takes the rest of
+ * ceil((cached + new)/page_size) from free_pages (device int32 [n_free]) in request order.  Written:
+ *   block_table   the entries of the new pages (all others are left as they are; an entry past max_pages is dropped);
+ *                 -1 where the free list has run out
+ *   cu_new        [n_requests + 1]  first row of every request in the batch; the last entry is the number of rows
+ *   total_len     [n_requests]      cached + new
+ *   positions     [n_rows]          position of every row; 0 behind the last request's rows
+ *   slot_map      [n_rows] int64    page*page_size + slot of every row; -1 behind the last request's rows and where a row
+ *                                   has no page
+ *   pages_used    [1] or NULL       pages taken from the free list; more than n_free if it was too short
+ * n_rows is the room in positions and slot_map (a captured step keeps it fixed); rows past it are dropped.  One launch,
+ * deterministic; calling again with the same inputs writes the same values.  free_pages and block_table may not overlap.
+ */
+cb_status cb_page_tables(const int32_t *cached_len, const int32_t *new_len, int32_t n_requests, int32_t page_size,
+                         const int32_t *free_pages, int64_t n_free, int32_t *block_table, int64_t table_stride, int32_t max_pages,
+                         int32_t *cu_new, int32_t *total_len, int32_t *positions, int64_t *slot_map, int64_t n_rows,
+                         int32_t *pages_used, void *stream);
+
+/*
+ * Stores row t of every layer and head to slot slot_map[t] (device int64 [n_rows]; negative or past the pool: the row is
+ * skipped).  src_k / src_v: device, element (layer, row, head, c) at layer*stride_layer + row*stride_token +
+ * head*stride_head + c elements of src_dtype (CB_DTYPE_BF16: copied; CB_DTYPE_F32: rounded to nearest even), 16-byte
+ * aligned, strides multiples of 8; the pool's layers, heads and head_dim.  Slots must differ (those of cb_page_tables do):
+ * of two rows with one slot either may end there, piece by piece.  n_rows == 0 is a no-op.
+ */
+cb_status cb_paged_store(const cb_page_pool *pool, const void *src_k, const void *src_v, int32_t src_dtype, int64_t n_rows,
+                         int64_t stride_layer, int64_t stride_token, int64_t stride_head, const int64_t *slot_map, void *stream);
+
+/*
+ * Rotary embedding with several position axes (time, height, width of images and video), out of place or in place:
+ * channel pair i (channels i and i + head_dim/2, the convention of cb_rope_rotate) turns by
+ *     positions[axis(i)][token] * rope_base^(-2 i / head_dim).
+ * positions: device int32, axis a at positions + a*axis_stride, any 32-bit value.  sections: HOST [n_axes] (<= 8), pairs
+ * per axis, summing to head_dim/2; axis(i) takes the sections one after the other, or with interleaved != 0 axis
+ * a = i mod n_axes while i < n_axes*sections[a], and axis 0 after that.  One axis is the ordinary embedding.  inverse != 0
+ * turns the other way (the adjoint, and the removal of the embedding).  x, out: bf16 [layer][token][head][channel] by
+ * strides (multiples of 8, 16-byte aligned; output strides of 0 only on dimensions of size 1); out may be x itself with
+ * the same strides, but not overlap it otherwise.  Angles are exact to 2^-22 turns at every 32-bit position.
+ */
+cb_status cb_rope_axes(const void *x, void *out, int32_t n_layers, int32_t n_heads, int32_t head_dim, int64_t n_tokens,
+                       int64_t x_stride_layer, int64_t x_stride_token, int64_t x_stride_head,
+                       int64_t o_stride_layer, int64_t o_stride_token, int64_t o_stride_head,
+                       const int32_t *positions, int64_t axis_stride, int32_t n_axes, const int32_t *sections,
+                       int32_t interleaved, double rope_base, int32_t inverse, void *stream);
+
+/*
+ * Attention of new rows over one layer of a paged cache.  Request b owns rows [cu_new[b], cu_new[b+1]) of q and out
+ * (bf16, row t of query head h at t*stride_token + h*stride_head, multiples of 8, 16-byte aligned); they are the LAST
+ * rows of its total_len[b] rows in the cache (their own keys and values are stored already), so row i of the request has
+ * position p = total_len - new + i, and
+ *     out = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale q . k_j)   over the keys j <= p with
+ *     window == 0  or  p - j < window  or  j < n_sink
+ * (a sliding window of the row's own and the window - 1 keys before it, and n_sink first keys that stay visible).  A row
+ * that sees no key (p < 0) gets zeros; rows of q behind cu_new[n_requests] are neither read nor written.  Query head h
+ * reads KV head h / (n_q_heads / n_heads).  Key j is at slot j mod page_size of page block_table[b][j / page_size]; only
+ * entries of pages that hold a visible key are read, and a page id outside the pool reads as zeros.  Rows of a page that
+ * no row of the request sees may hold anything; keys and values that some row of the request sees must be finite.
+ * max_new: the largest number of new rows of a request, or 0 if unknown.  It chooses between kernels and never changes
+ * which rows are computed.
+ * scale > 0.  workspace: device, 256-byte aligned, cb_paged_attention_workspace_bytes() bytes, ZERO-FILLED once by the
+ * caller before its first use (calls leave it ready for the next one); calls that share a workspace must be ordered on
+ * the device (one stream, or graphs that never run at the same time).  Results are bitwise reproducible.  A device-side
+ * time-out shows in cb_last_device_status.  n_rows * n_q_heads + n_requests < 2^31.
+ */
+cb_status cb_paged_attention_workspace_bytes(int32_t head_dim, size_t *bytes);
+cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void *q, int64_t q_stride_token, int64_t q_stride_head,
+                             void *out, int64_t o_stride_token, int64_t o_stride_head, int64_t n_rows, int32_t n_q_heads,
+                             const int32_t *block_table, int64_t table_stride, int32_t max_pages,
+                             const int32_t *cu_new, const int32_t *total_len, int32_t n_requests, int32_t max_new,
+                             float scale, int32_t window, int32_t n_sink, void *workspace, size_t workspace_bytes, void *stream);
+
 /*
  * Synchronises the stream and reads the context's device status word: CB_OK, or CB_ERR_TIMEOUT if a bounded
  * wait inside a kernel ran out (the statistics are then invalid; reset before reuse).
@@ -431,7 +529,7 @@ cb_status cb_device_status(cb_ctx *ctx, void *stream);
 
 /*
  * The same for the entry points that take no context (cb_apply, cb_apply_rope, cb_apply_multilayer,
- * cb_fullhead_stats_accumulate, cb_multilayer_stats_accumulate, cb_stats_build_static): their kernels record a
+ * cb_fullhead_stats_accumulate, cb_multilayer_stats_accumulate, cb_stats_build_static, cb_paged_attention): their kernels record a
  * time-out in a status word that belongs to the library (one per device).  Synchronises the stream, returns
  * CB_ERR_TIMEOUT if any such kernel on the current device gave up since the last call (the outputs of that call are
  * then incomplete) and clears the word; CB_OK otherwise.  The paper has no counterpart: error reporting only.

@@ -34,7 +34,8 @@ EXPORTS = ("cb_status_string", "cb_head_map_nearest", "cb_work_list", "cb_worksp
            "cb_means_accumulate_rope", "cb_stats_accumulate_centered_rope",
            "cb_means_energy", "cb_probe_r2", "cb_probe_scores", "cb_rank_layers",
            "cb_last_device_status", "cb_test_hooks", "cb_stats_state_bytes", "cb_stats_export", "cb_stats_import",
-           "cb_last_cuda_error", "cb_launch_count")
+           "cb_last_cuda_error", "cb_launch_count",
+           "cb_page_tables", "cb_paged_store", "cb_rope_axes", "cb_paged_attention_workspace_bytes", "cb_paged_attention")
 
 
 class CbError(RuntimeError):
@@ -634,6 +635,122 @@ def cb_apply_multilayer(prob: FullHeadProblem, src_head, Wb: torch.Tensor, src_k
                                      ctypes.c_int64(tgt_k.stride(0)), ctypes.c_int64(tgt_k.stride(1)), ctypes.c_int64(tgt_k.stride(2)),
                                      dt, ctypes.c_void_p(ws.data_ptr()), ctypes.c_size_t(ws.numel()), _stream_ptr(stream)),
            "cb_apply_multilayer")
+
+
+# ----------------------------------------------------------------------------- paged target cache
+class _PagePool(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("n_layers", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_pages", ctypes.c_int64),
+                ("stride_layer", ctypes.c_int64), ("stride_page", ctypes.c_int64), ("stride_slot", ctypes.c_int64),
+                ("stride_head", ctypes.c_int64)]
+
+
+class PagePool:
+    """K and V pages, bf16 tensors indexed [layer][page][slot][head][channel] (any strides, channels contiguous)."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        assert k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and k.dim() == 5
+        strides = k.stride()
+        assert k.shape == v.shape and strides == v.stride() and strides[4] == 1 and k.device == v.device
+        self.k, self.v = k, v
+        L, N, S, H, d = k.shape
+        self.c = _PagePool(k.data_ptr(), v.data_ptr(), L, H, d, S, N, strides[0], strides[1], strides[2], strides[3])
+
+
+def _on_one_device(stream, *tensors):
+    """All tensors on one CUDA device, and that the current one (a launch goes to the current device); the stream handle."""
+    dev = tensors[0].device
+    for t in tensors:
+        if not t.is_cuda or t.device != dev:
+            raise ValueError("all tensors of a call must be on one CUDA device")
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    if dev.index != torch.cuda.current_device() or stream.device != dev:
+        raise ValueError("the tensors' device must be the current device and the stream's")
+    return ctypes.c_void_p(stream.cuda_stream)
+
+
+def _ptr(t: torch.Tensor) -> ctypes.c_void_p:
+    return ctypes.c_void_p(t.data_ptr())
+
+
+_I64 = ctypes.c_int64
+
+
+def cb_page_tables(cached_len: torch.Tensor, new_len: torch.Tensor, page_size: int, free_pages: torch.Tensor,
+                   block_table: torch.Tensor, cu_new: torch.Tensor, total_len: torch.Tensor, positions: torch.Tensor,
+                   slot_map: torch.Tensor, pages_used: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Block tables, slots and positions of a batch from its request lengths: device int32 tensors (slot_map int64);
+    block_table [B][max_pages] is completed in place, cu_new [B + 1], total_len [B], positions and slot_map [rows]."""
+    B = cached_len.numel()
+    for t in (cached_len, new_len, free_pages, block_table, cu_new, total_len, positions):
+        assert t.dtype == torch.int32
+    for t in (cached_len, new_len, free_pages, cu_new, total_len, positions, slot_map):
+        assert t.is_contiguous()
+    assert slot_map.dtype == torch.int64 and new_len.numel() == B and total_len.numel() == B and cu_new.numel() == B + 1
+    assert block_table.dim() == 2 and block_table.shape[0] == B and (block_table.stride(1) == 1 or block_table.shape[1] <= 1)
+    assert slot_map.numel() == positions.numel()
+    assert pages_used is None or (pages_used.dtype == torch.int32 and pages_used.numel() >= 1 and pages_used.device == cu_new.device)
+    st = _on_one_device(stream, cu_new, cached_len, new_len, free_pages, block_table, total_len, positions, slot_map)
+    _check(lib().cb_page_tables(_ptr(cached_len), _ptr(new_len), B, page_size, _ptr(free_pages), _I64(free_pages.numel()),
+                                _ptr(block_table), _I64(block_table.stride(0)), block_table.shape[1], _ptr(cu_new), _ptr(total_len),
+                                _ptr(positions), _ptr(slot_map), _I64(positions.numel()),
+                                ctypes.c_void_p(0 if pages_used is None else pages_used.data_ptr()), st), "cb_page_tables")
+
+
+def cb_paged_store(pool: PagePool, src_k: torch.Tensor, src_v: torch.Tensor, slot_map: torch.Tensor, stream=None) -> None:
+    """Rows [L][T][H][d] (bf16, or fp32 rounded on the way) of all layers into the slots slot_map [T] (int64, -1: skipped)."""
+    L, T, H, d = src_k.shape
+    ss = src_k.stride()
+    assert src_k.dtype == src_v.dtype and src_k.shape == src_v.shape and ss == src_v.stride() and ss[3] == 1
+    assert (L, H, d) == (pool.c.n_layers, pool.c.n_heads, pool.c.head_dim)
+    assert slot_map.dtype == torch.int64 and slot_map.is_contiguous() and slot_map.numel() == T
+    dt = {torch.bfloat16: CB_DTYPE_BF16, torch.float32: CB_DTYPE_F32}[src_k.dtype]
+    st = _on_one_device(stream, pool.k, src_k, src_v, slot_map)
+    _check(lib().cb_paged_store(ctypes.byref(pool.c), _ptr(src_k), _ptr(src_v), dt, _I64(T), _I64(ss[0]), _I64(ss[1]), _I64(ss[2]),
+                                _ptr(slot_map), st), "cb_paged_store")
+
+
+def cb_rope_axes(x: torch.Tensor, out: torch.Tensor, positions: torch.Tensor, sections: Sequence[int], rope_base: float,
+                 interleaved: bool = False, inverse: bool = False, stream=None) -> None:
+    """Rotary embedding of bf16 rows [L][T][H][d] with positions [n_axes][T] (int32); `out` may be `x`."""
+    L, T, H, d = x.shape
+    xs, os_ = x.stride(), out.stride()
+    assert x.dtype == torch.bfloat16 and out.dtype == torch.bfloat16 and x.shape == out.shape and xs[3] == 1 and os_[3] == 1
+    assert positions.dtype == torch.int32 and positions.dim() == 2 and positions.shape == (len(sections), T)
+    assert positions.stride(1) == 1 or T <= 1
+    sec = (ctypes.c_int32 * len(sections))(*sections)
+    st = _on_one_device(stream, x, out, positions)
+    _check(lib().cb_rope_axes(_ptr(x), _ptr(out), L, H, d, _I64(T), _I64(xs[0]), _I64(xs[1]), _I64(xs[2]), _I64(os_[0]), _I64(os_[1]),
+                              _I64(os_[2]), _ptr(positions), _I64(positions.stride(0)), len(sections), sec, 1 if interleaved else 0,
+                              ctypes.c_double(rope_base), 1 if inverse else 0, st), "cb_rope_axes")
+
+
+def cb_paged_attention_workspace_bytes(head_dim: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().cb_paged_attention_workspace_bytes(head_dim, ctypes.byref(n)), "cb_paged_attention_workspace_bytes")
+    return n.value
+
+
+def cb_paged_attention(q: torch.Tensor, out: torch.Tensor, pool: PagePool, layer: int, block_table: torch.Tensor,
+                       cu_new: torch.Tensor, total_len: torch.Tensor, scale: float, workspace: torch.Tensor,
+                       max_new: int = 0, window: int = 0, n_sink: int = 0, stream=None) -> None:
+    """Attention of new rows q [T][Hq][d] (bf16) over layer `layer` of the pool; block_table [B][max_pages], cu_new [B + 1],
+    total_len [B] as cb_page_tables leaves them; workspace: uint8, zero-filled once (torch.zeros)."""
+    T, Hq, d = q.shape
+    qs, os_ = q.stride(), out.stride()
+    assert q.dtype == torch.bfloat16 and out.dtype == torch.bfloat16 and q.shape == out.shape and qs[2] == 1 and os_[2] == 1
+    assert d == pool.c.head_dim and block_table.dim() == 2
+    B, cols = block_table.shape
+    assert block_table.dtype == torch.int32 and cu_new.dtype == torch.int32 and total_len.dtype == torch.int32
+    assert (block_table.stride(1) == 1 or cols <= 1) and cu_new.is_contiguous() and total_len.is_contiguous()
+    assert cu_new.numel() == B + 1 and total_len.numel() == B and workspace.dtype == torch.uint8 and workspace.is_contiguous()
+    st = _on_one_device(stream, q, out, pool.k, block_table, cu_new, total_len, workspace)
+    _check(lib().cb_paged_attention(ctypes.byref(pool.c), layer, _ptr(q), _I64(qs[0]), _I64(qs[1]), _ptr(out), _I64(os_[0]), _I64(os_[1]),
+                                    _I64(T), Hq, _ptr(block_table), _I64(block_table.stride(0)), cols, _ptr(cu_new), _ptr(total_len),
+                                    B, max_new, ctypes.c_float(scale), window, n_sink, _ptr(workspace),
+                                    ctypes.c_size_t(workspace.numel()), st), "cb_paged_attention")
 
 
 def cb_device_status(ctx: Context, stream=None) -> None:

@@ -1,0 +1,123 @@
+// Page tables, slots and positions of a batch from its request lengths.
+//
+// Request b keeps its ceil(cached/ps) pages and takes ceil((cached + new)/ps) minus that many from the free list, in
+// request order; row t of the batch belongs to the request b with cu[b] <= t < cu[b + 1] and goes to position
+// cached[b] + t - cu[b].  Everything follows from two prefix sums over the requests, which every block takes for itself
+// (8 bytes a request, from L2) instead of waiting for another one: one launch, no workspace, no order between blocks.
+// Bound by the launch for decode steps and by the 12 bytes written per row for whole prompts.
+#include "cb_paged.cuh"
+
+namespace cb {
+
+static constexpr int PT_THREADS = 1024;
+static constexpr int PT_SPAN = 2048;        // rows that are worth a block of their own
+
+struct TablesArgs {
+    const int *cached, *fresh;
+    int B, page_log2;
+    const int *free_pages;
+    long long n_free;
+    int *table;
+    long long table_stride;
+    int cols;
+    int *cu, *total, *positions;
+    long long *slot_map;
+    long long n_rows;
+    int *pages_used;
+};
+
+__global__ void __launch_bounds__(PT_THREADS) k_page_tables(const TablesArgs a)
+{
+    __shared__ unsigned long long warp_sums[32];
+    __shared__ unsigned row_at[PT_THREADS + 1], page_at[PT_THREADS + 1];   // within the group of requests
+    __shared__ int s_cached[PT_THREADS], s_held[PT_THREADS];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int ps1 = (1 << a.page_log2) - 1;
+    const long long stride = (long long)gridDim.x * PT_THREADS, mine = (long long)blockIdx.x * PT_THREADS + tid;
+    long long rows0 = 0, pages0 = 0;          // before this group of requests
+    for (int b0 = 0; b0 < a.B; b0 += PT_THREADS) {
+        const int b = b0 + tid;
+        int cached = 0, fresh = 0;
+        if (b < a.B) { cached = max(a.cached[b], 0); fresh = max(a.fresh[b], 0); }
+        const long long sum = (long long)cached + fresh;
+        const int held = (int)(((long long)cached + ps1) >> a.page_log2), need = (int)((sum + ps1) >> a.page_log2);
+        // rows in the low half, pages in the high half: neither passes 2^32 in 1,024 requests that fit a pool
+        unsigned long long incl = (unsigned long long)(unsigned)fresh | ((unsigned long long)(unsigned)(need - held) << 32);
+        const unsigned long long own = incl;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned long long up = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += up;
+        }
+        if (lane == 31) warp_sums[warp] = incl;
+        __syncthreads();
+        unsigned long long before = 0;
+        for (int w = 0; w < warp; ++w) before += warp_sums[w];
+        const unsigned long long excl = before + incl - own;
+        row_at[tid] = (unsigned)excl;
+        page_at[tid] = (unsigned)(excl >> 32);
+        s_cached[tid] = cached;
+        s_held[tid] = held;
+        if (tid == PT_THREADS - 1) { row_at[PT_THREADS] = (unsigned)(excl + own); page_at[PT_THREADS] = (unsigned)((excl + own) >> 32); }
+        if (blockIdx.x == 0 && b < a.B) {
+            a.cu[b] = (int)(rows0 + (unsigned)excl);
+            a.total[b] = (int)sum;
+        }
+        __syncthreads();
+        const unsigned n_rows = row_at[PT_THREADS], n_pages = page_at[PT_THREADS];
+        // new pages: the e-th of the group belongs to the last request whose pages start at or before e
+        for (long long e = mine; e < n_pages; e += stride) {
+            int lo = 0, hi = PT_THREADS - 1;
+            while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (page_at[mid] <= e) lo = mid; else hi = mid - 1; }
+            const int col = s_held[lo] + (int)(e - page_at[lo]);
+            const long long f = pages0 + e;
+            if ((unsigned)col < (unsigned)a.cols) a.table[(long long)(b0 + lo) * a.table_stride + col] = f < a.n_free ? a.free_pages[f] : -1;
+        }
+        for (long long e = mine; e < n_rows && rows0 + e < a.n_rows; e += stride) {
+            int lo = 0, hi = PT_THREADS - 1;
+            while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (row_at[mid] <= e) lo = mid; else hi = mid - 1; }
+            const int pos = s_cached[lo] + (int)(e - row_at[lo]);
+            const int col = pos >> a.page_log2;
+            int page = -1;
+            if ((unsigned)col < (unsigned)a.cols) {
+                if (col < s_held[lo]) {
+                    page = a.table[(long long)(b0 + lo) * a.table_stride + col];
+                } else {
+                    const long long f = pages0 + page_at[lo] + (col - s_held[lo]);
+                    if (f < a.n_free) page = a.free_pages[f];
+                }
+            }
+            a.positions[rows0 + e] = pos;
+            a.slot_map[rows0 + e] = page < 0 ? -1 : ((long long)page << a.page_log2) + (pos & ps1);
+        }
+        rows0 += n_rows;
+        pages0 += n_pages;
+        __syncthreads();
+    }
+    for (long long e = rows0 + mine; e < a.n_rows; e += stride) {       // behind the last request
+        a.positions[e] = 0;
+        a.slot_map[e] = -1;
+    }
+    if (blockIdx.x == 0 && tid == 0) {
+        a.cu[a.B] = (int)rows0;
+        if (a.pages_used) a.pages_used[0] = (int)pages0;
+    }
+}
+
+cudaError_t launch_page_tables(const int *cached, const int *fresh, int n_requests, int page_log2, const int *free_pages,
+                               long long n_free, int *table, long long table_stride, int table_cols, int *cu, int *total,
+                               int *positions, long long *slot_map, long long n_rows, int *pages_used, cudaStream_t st)
+{
+    TablesArgs a{cached, fresh, n_requests, page_log2, free_pages, n_free, table, table_stride, table_cols,
+                 cu, total, positions, slot_map, n_rows, pages_used};
+    long long grid = (n_rows + PT_SPAN - 1) / PT_SPAN;
+    const int sms = device_sm_count();
+    if (grid < 1) grid = 1;
+    if (grid > sms) grid = sms;
+    k_page_tables<<<(unsigned)grid, PT_THREADS, 0, st>>>(a);
+    cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) count_launch();
+    return e;
+}
+
+}  // namespace cb

@@ -1,0 +1,269 @@
+// Paged target cache: declarations shared by the attention kernels and their host side (not part of the C ABI).
+//
+// Attention work is cut into units (request, block of ROWS flattened query rows); a flattened row is token * group + g,
+// so that every query head which shares a KV head sits in one block and the keys are read once for all of them.  A unit
+// and a KV head together own n key tiles; all tiles of all (unit, KV head) pairs are laid out on one line, in unit
+// order, and block c of the grid takes the tiles [c Q, (c + 1) Q): every block has the same number of tiles whatever the
+// lengths are.  A pair whose tiles fall to several blocks is joined by the block that finishes last, in block order.
+#pragma once
+
+#include "cb_internal.cuh"
+
+namespace cb {
+
+constexpr int PA_MAX_GRID = 1024;            // blocks of an attention launch (counters in the workspace)
+constexpr size_t PA_COUNTER_BYTES = PA_MAX_GRID * sizeof(int);
+
+struct PagedArgs {
+    const __nv_bfloat16 *q;
+    __nv_bfloat16 *out;
+    long long q_st, q_sh, o_st, o_sh;        // element strides of a token and of a head
+    const int *table;                        // device [n_requests][table_cols]
+    long long table_stride;
+    int table_cols;
+    const int *cu;                           // device [n_requests + 1]: first row of every request
+    const int *total;                        // device [n_requests]: rows in the cache, the new ones included
+    int n_requests, n_rows;                  // n_rows: rows of q and out
+    int Hkv, group;
+    int page_log2;
+    int n_pages;
+    int window, n_sink;                      // window 0: none
+    float scale_log2;                        // softmax scale times log2(e)
+    int q_min;                               // least tiles a block takes
+    float *part;                             // partial results of split pairs, two records per block
+    int *counters;                           // [PA_MAX_GRID], zero between calls
+    int *status;
+    unsigned poll_limit;
+    int starve;
+};
+
+cudaError_t launch_paged_attn_few(const PagedArgs &a, int d, const void *k, const void *v, int page_size, long long s_page,
+                                  long long s_slot, long long s_head, int max_new, cudaStream_t st);
+size_t paged_attn_few_workspace(int d);
+
+cudaError_t launch_page_tables(const int *cached, const int *fresh, int n_requests, int page_log2, const int *free_pages,
+                               long long n_free, int *table, long long table_stride, int table_cols, int *cu, int *total,
+                               int *positions, long long *slot_map, long long n_rows, int *pages_used, cudaStream_t st);
+
+struct StoreArgs {
+    const void *src_k, *src_v;
+    int src_f32;
+    long long s_sl, s_st, s_sh;              // source strides (elements): layer, token, head
+    __nv_bfloat16 *k, *v;
+    long long d_sl, d_sp, d_ss, d_sh;        // pool strides (elements): layer, page, slot, head
+    const long long *slot_map;
+    long long n_slots, n_rows;               // n_slots = pages * page size
+    int page_log2, L, H, d;
+};
+cudaError_t launch_paged_store(const StoreArgs &a, cudaStream_t st);
+
+cudaError_t launch_rope_axes(const void *x, void *out, int L, int H, int d, long long T, const long long xs[3],
+                             const long long os[3], const int *positions, long long axis_stride, const unsigned char *axis_of_pair,
+                             double base, int inverse, cudaStream_t st);
+
+#ifdef __CUDACC__
+// One unit's place in the batch and its key tiles of KT keys.
+struct PaUnit {
+    int b, qt, nq;          // request, row block, row blocks of the request
+    int row0, rows;         // first flattened row, rows in the block
+    int tok0;               // first row of the request in q
+    int base;               // position of the request's first new row (negative if the cache is shorter than the chunk)
+    int p0, p1;             // positions of the block's first and last row
+    int hi_key;             // keys [0, hi_key) can be seen by some row
+    int lo_key;             // without the sinks, keys from lo_key on
+    int ns, lo_tile, n;     // tiles that hold sinks, first tile of the window, number of tiles (at least 1)
+};
+
+template <int ROWS, int KT>
+__device__ __forceinline__ bool pa_unit(const PagedArgs &a, const int *cu, const int *total, int b, int qt, PaUnit &u)
+{
+    const int c0 = cu[b], fresh = cu[b + 1] - c0;
+    const int all = fresh * a.group;
+    u.b = b;
+    u.qt = qt;
+    u.nq = (all + ROWS - 1) / ROWS;
+    if (qt >= u.nq) { u.n = 0; return false; }
+    u.tok0 = c0;
+    u.row0 = qt * ROWS;
+    u.rows = min(ROWS, all - u.row0);
+    const int len = max(total[b], 0);
+    u.base = len - fresh;
+    u.p0 = u.base + u.row0 / a.group;
+    u.p1 = u.base + (u.row0 + u.rows - 1) / a.group;
+    u.hi_key = max(0, u.p1 + 1);
+    const int hi_tile = (u.hi_key + KT - 1) / KT;
+    u.lo_key = 0;
+    u.ns = 0;
+    u.lo_tile = 0;
+    if (a.window > 0) {
+        const long long lo = (long long)u.p0 - a.window + 1;
+        u.lo_key = lo > 0 ? (int)lo : 0;
+        u.ns = (min(a.n_sink, u.hi_key) + KT - 1) / KT;
+        u.lo_tile = max(u.lo_key / KT, u.ns);
+    }
+    u.n = max(1, u.ns + max(0, hi_tile - u.lo_tile));
+    return true;
+}
+__device__ __forceinline__ int pa_tile(const PaUnit &u, int t) { return t < u.ns ? t : u.lo_tile + (t - u.ns); }
+
+// Every key of the tile is seen by every row of the unit.
+template <int KT>
+__device__ __forceinline__ bool pa_tile_full(const PagedArgs &a, const PaUnit &u, int kt)
+{
+    const long long j0 = (long long)kt * KT;
+    if (j0 + KT - 1 > u.p0) return false;
+    return a.window <= 0 || (long long)u.p1 - j0 < a.window || j0 + KT <= a.n_sink;
+}
+__device__ __forceinline__ bool pa_sees(const PagedArgs &a, int p, int j)
+{
+    return j <= p && (a.window <= 0 || p - j < a.window || j < a.n_sink);
+}
+
+// The block's share of the line of tiles, left in shared memory by pa_schedule.
+struct PaShare {
+    long long begin, end;    // tiles of this block
+    long long q;             // tiles per block
+    long long unit_begin;    // where the first unit's tiles begin
+    int b, qt;               // the first unit
+};
+
+// All threads of the block.  `staged`: shared memory for the lengths (cap ints), free until the first tile is copied.
+// Each thread counts the tiles of a run of consecutive units; one scan gives the line, one thread finds the block's start.
+template <int ROWS, int KT, int THREADS>
+__device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int cap, PaShare *share, long long *warp_sums)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    constexpr int NWARP = THREADS / 32;
+    const int *cu = a.cu, *total = a.total;
+    const int B = a.n_requests;
+    if (2 * B + 1 <= cap) {
+        for (int i = tid; i <= B; i += THREADS) staged[i] = a.cu[i];
+        for (int i = tid; i < B; i += THREADS) staged[B + 1 + i] = a.total[i];
+        cu = staged;
+        total = staged + B + 1;
+    }
+    if (tid == 0) { share->begin = 0; share->end = 0; }
+    __syncthreads();
+    // block of unit index u: the last request b with floor(cu[b] group / ROWS) + b <= u (some indices are no unit)
+    const int n_units = (int)((long long)a.n_rows * a.group / ROWS) + B;
+    const int per = (n_units + THREADS - 1) / THREADS;
+    const int u0 = min(n_units, tid * per), u1 = min(n_units, u0 + per);
+    int b0 = 0;
+    if (u0 < u1) {
+        int lo = 0, hi = B - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if ((int)((long long)cu[mid] * a.group / ROWS) + mid <= u0) lo = mid; else hi = mid - 1;
+        }
+        b0 = lo;
+    }
+    PaUnit un;
+    long long mine = 0;
+    {
+        int b = b0;
+        for (int u = u0; u < u1; ++u) {
+            while (b + 1 < B && (int)((long long)cu[b + 1] * a.group / ROWS) + b + 1 <= u) ++b;
+            const int qt = u - ((int)((long long)cu[b] * a.group / ROWS) + b);
+            if (pa_unit<ROWS, KT>(a, cu, total, b, qt, un)) mine += un.n;
+        }
+    }
+    long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long up = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += up;
+    }
+    if (lane == 31) warp_sums[warp] = incl;
+    __syncthreads();
+    long long before = 0, all = 0;
+    for (int w = 0; w < NWARP; ++w) {
+        const long long s = warp_sums[w];
+        if (w < warp) before += s;
+        all += s;
+    }
+    const long long line = all * a.Hkv;
+    long long q = (line + gridDim.x - 1) / gridDim.x;
+    if (q < a.q_min) q = a.q_min;
+    const long long begin = (long long)blockIdx.x * q;
+    long long pre = (before + incl - mine) * a.Hkv;
+    if (begin < line && begin >= pre && begin < pre + mine * a.Hkv) {
+        int b = b0;
+        for (int u = u0; u < u1; ++u) {
+            while (b + 1 < B && (int)((long long)cu[b + 1] * a.group / ROWS) + b + 1 <= u) ++b;
+            const int qt = u - ((int)((long long)cu[b] * a.group / ROWS) + b);
+            if (!pa_unit<ROWS, KT>(a, cu, total, b, qt, un)) continue;
+            if (begin < pre + (long long)un.n * a.Hkv) {
+                share->b = b;
+                share->qt = qt;
+                share->unit_begin = pre;
+                share->q = q;
+                share->begin = begin;
+                share->end = begin + q < line ? begin + q : line;
+                break;
+            }
+            pre += (long long)un.n * a.Hkv;
+        }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the staged lengths' memory goes to the copies next
+    __syncthreads();
+}
+
+// Walks the pieces of a block's share: a piece is a run of tiles of one (unit, KV head).
+template <int ROWS, int KT>
+struct PaWalk {
+    PaUnit u;
+    int h, t, t1;            // KV head, tiles [t, t1) of the unit
+    long long at, end, q;    // position on the line
+    long long pair_begin;    // where the tiles of (unit, h) begin
+    __device__ __forceinline__ bool open(const PagedArgs &a, const PaShare &s)
+    {
+        at = s.begin;
+        end = s.end;
+        q = s.q;
+        if (at >= end) return false;
+        pa_unit<ROWS, KT>(a, a.cu, a.total, s.b, s.qt, u);
+        const long long off = at - s.unit_begin;
+        h = (int)(off / u.n);
+        pair_begin = s.unit_begin + (long long)h * u.n;
+        piece();
+        return true;
+    }
+    __device__ __forceinline__ void piece()
+    {
+        t = (int)(at - pair_begin);
+        t1 = (int)min((long long)u.n, end - pair_begin);
+    }
+    __device__ __forceinline__ bool next(const PagedArgs &a)
+    {
+        at += t1 - t;
+        if (at >= end) return false;
+        pair_begin += u.n;
+        if (++h == a.Hkv) {
+            h = 0;
+            int b = u.b, qt = u.qt + 1;
+            if (qt >= u.nq) {
+                qt = 0;
+                do { ++b; } while (b < a.n_requests && a.cu[b + 1] == a.cu[b]);
+                if (b >= a.n_requests) return false;
+            }
+            pa_unit<ROWS, KT>(a, a.cu, a.total, b, qt, u);
+        }
+        piece();
+        return true;
+    }
+    __device__ __forceinline__ bool whole() const { return t == 0 && t1 == u.n; }
+    __device__ __forceinline__ int first_block() const { return (int)(pair_begin / q); }
+    __device__ __forceinline__ int last_block() const { return (int)((pair_begin + u.n - 1) / q); }
+    // Record of block c's part of this pair: a block has at most one part that began before it and one that ends after it.
+    __device__ __forceinline__ int record(int c) const { return 2 * c + (pair_begin <= (long long)c * q ? 0 : 1); }
+};
+
+__device__ __forceinline__ float pa_exp2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+#endif
+
+}  // namespace cb

@@ -1,0 +1,402 @@
+// Attention of a few new rows per request over a paged cache (decode steps, short chunks):
+//   out_t = sum_j softmax_j(scale q_t . k_j) v_j   over the keys j <= p_t that the window or the sinks leave visible.
+//
+// Bound by the bytes of K and V: with up to 64 flattened rows (new rows x query heads of a KV head) every key and value
+// is read once for all of them, at 8 to 64 operations a byte, so the warp-level matrix instruction is fast enough and
+// the tile's rows need not be padded to the 128 of the tensor-memory one.
+//   producer warp   TMA, one box per page (page size rows of one KV head, both halves of the channels), three stages of
+//                   64 keys; a page id outside the pool reads as zeros, so no table entry can make the copy fault.
+//   4 consumer warps   a warp owns 16 rows and 64 MT / 4 keys of a tile and carries its own running maximum, sum and
+//                   output, so that the main loop has no barrier between warps; they are joined at the end of a piece.
+// A wait that runs out is not followed by another one: the block runs through to its end, so that every barrier and join
+// counter is served as in a good run, and sets the status word; its rows are then not valid.
+// Scores, maxima, sums and outputs are fp32; the weights exp2(s - m) are rounded to bf16 for the product with V, which is
+// bf16 as well (relative 2^-9 per weight, of the size of the output's own rounding).
+#include "cb_paged.cuh"
+#include "cb_ptx.cuh"
+#include "cb_math.cuh"
+
+namespace cb {
+
+using namespace ptx;
+
+template <int D, int MT>
+struct FewCfg {
+    static constexpr int ROWS = 16 * MT;
+    static constexpr int KT = 64;
+    static constexpr int KS = 4 / MT;                  // key groups of a tile
+    static constexpr int WK = KT / KS;                 // keys of one warp in a tile
+    static constexpr int NB = D / 64;
+    static constexpr int HALF = KT * D * 2;            // bytes of K (or V) in a stage
+    static constexpr int STAGE = 2 * HALF;
+    static constexpr int NS = D == 128 ? 3 : 6;
+    static constexpr int THREADS = 160;
+    static constexpr int RED_PITCH = 36;               // floats per row of the join buffer (32 + 4: no bank conflict)
+    static constexpr int RED_BYTES = 4 * 16 * RED_PITCH * 4;
+    static constexpr size_t SMEM = 1024 + (size_t)NS * STAGE + RED_BYTES + 4 * 16 * 2 * 4 + 1024;
+    static constexpr int REC = ROWS * (D + 2);         // floats of a partial record: output rows, maxima, sums
+};
+
+struct FewParams {
+    CUtensorMap k, v;
+    PagedArgs a;
+};
+
+__device__ __forceinline__ void ldsm_x4(uint32_t addr, uint32_t (&r)[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void bar_consumers() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
+template <int D, int MT>
+__global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant__ FewParams P)
+{
+    using C = FewCfg<D, MT>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    float *red = reinterpret_cast<float *>(smem + (size_t)C::NS * C::STAGE);
+    float *stat_m = red + C::RED_BYTES / 4;                 // [4 warps][16 rows]
+    float *stat_l = stat_m + 64;
+    uint64_t *full = reinterpret_cast<uint64_t *>(stat_l + 64);
+    uint64_t *empty = full + C::NS;
+    long long *warp_sums = reinterpret_cast<long long *>(empty + C::NS);
+    PaShare *share = reinterpret_cast<PaShare *>(warp_sums + 8);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(share + 1);
+    volatile int *last_flag = abort_flag + 2;
+
+    const PagedArgs &a = P.a;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int i = 0; i < C::NS; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 4); }
+        abort_flag[0] = 0;
+        abort_flag[1] = (int)a.poll_limit;
+        mbar_fence_init();
+        tma_prefetch_desc(&P.k);
+        tma_prefetch_desc(&P.v);
+    }
+    pa_schedule<C::ROWS, C::KT, C::THREADS>(a, reinterpret_cast<int *>(smem), C::NS * C::STAGE / 4, share, warp_sums);
+
+    PaWalk<C::ROWS, C::KT> w;
+    const bool any = w.open(a, *share);
+    const int box_log2 = a.page_log2 < 6 ? a.page_log2 : 6;      // rows of one copy
+    bool dead = false;       // a wait ran out: no more waits, the rest runs through on whatever is there
+    if (warp == 4) {
+        // ================================ producer ================================
+        if (any && !a.starve) {
+            Ring<C::NS> st;
+            int issued = 0;
+            const int n_box = 2 << (6 - box_log2);               // copies of a tile: K's, then V's
+            const int comp = lane >= n_box / 2;
+            const int i = lane - comp * (n_box / 2);
+            const uint32_t box_bytes = (uint32_t)C::NB << (box_log2 + 7);
+            bool more = true;
+            while (more) {
+                const int *row = a.table + (long long)w.u.b * a.table_stride;
+                for (int t = w.t; t < w.t1; ++t) {
+                    const int key = pa_tile(w.u, t) * C::KT + (i << box_log2);
+                    int page = a.n_pages;                        // outside the pool: the copy writes zeros
+                    if (lane < n_box && key < w.u.hi_key) {
+                        const int col = key >> a.page_log2;
+                        if (col < a.table_cols) page = __ldg(row + col);
+                    }
+                    if (!mbar_wait_warp(&empty[st.idx], st.phase ^ 1, abort_flag, lane, true)) { dead = true; break; }
+                    if (lane == 0) mbar_arrive_expect_tx(&full[st.idx], C::STAGE);
+                    __syncwarp();
+                    if (lane < n_box)
+                        tma_load_5d(smem + (size_t)st.idx * C::STAGE + comp * C::HALF + (size_t)i * box_bytes, comp ? &P.v : &P.k,
+                                    &full[st.idx], 0, key & ((1 << a.page_log2) - 1), 0, w.h, page);
+                    st.next();
+                    ++issued;
+                }
+                more = !dead && w.next(a);
+            }
+            // after a time-out the copies in flight land before the block ends
+            for (int i = dead ? min(issued, C::NS) : 0; i > 0; --i) {
+                mbar_wait_warp(&full[st.idx], st.phase ^ 1, abort_flag, lane, true);
+                st.next();
+            }
+        }
+    } else if (any) {
+        // ================================ consumers ================================
+        const int mt = warp / C::KS, ks = warp % C::KS;
+        const int g = lane >> 2, c2 = (lane & 3) * 2;
+        const uint32_t smem_base = smem_u32(smem);
+        // ldmatrix rows of this lane: K (keys x channels) and V (keys x channels, transposed on the way)
+        const int k_key = ((lane >> 4) << 3) + (lane & 7), k_ch = (lane >> 3) & 1;
+        const int v_key = (((lane >> 3) & 1) << 3) + (lane & 7), v_ch = lane >> 4;
+        Ring<C::NS> st;
+        bool more = true;
+        while (more) {
+            const PaUnit &u = w.u;
+            // this lane's two rows of the warp's 16, and their positions
+            int pos[2];
+            bool live[2];
+            uint32_t qf[D / 16][4];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = mt * 16 + g + e * 8;
+                const int fr = u.row0 + r;
+                const int tok = fr / a.group;
+                live[e] = r < u.rows && (unsigned)(u.tok0 + tok) < (unsigned)a.n_rows;
+                pos[e] = live[e] ? u.base + tok : -1;
+                const __nv_bfloat16 *qp = a.q + (long long)(u.tok0 + tok) * a.q_st + (long long)(w.h * a.group + fr % a.group) * a.q_sh + c2;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    qf[k][e] = live[e] ? *reinterpret_cast<const uint32_t *>(qp + k * 16) : 0u;
+                    qf[k][e + 2] = live[e] ? *reinterpret_cast<const uint32_t *>(qp + k * 16 + 8) : 0u;
+                }
+            }
+            float o[D / 8][4];
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
+            float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
+            for (int t = w.t; t < w.t1; ++t) {
+                const int kt = pa_tile(u, t);
+                const bool edge = !pa_tile_full<C::KT>(a, u, kt);
+                if (!dead && !mbar_wait_warp(&full[st.idx], st.phase, abort_flag, lane)) dead = true;
+                const uint32_t kb = smem_base + st.idx * C::STAGE, vb = kb + C::HALF;
+                float s[C::WK / 8][4];
+#pragma unroll
+                for (int n = 0; n < C::WK / 8; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+#pragma unroll
+                for (int n = 0; n < C::WK / 16; ++n) {
+                    const int key = ks * C::WK + n * 16 + k_key;
+                    const int pg = key >> box_log2, rr = key & ((1 << box_log2) - 1);
+                    const uint32_t row = kb + ((uint32_t)(pg * C::NB) << (box_log2 + 7)) + rr * 128;
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        uint32_t b[4];
+                        const int ch = (k & 3) * 2 + k_ch;
+                        ldsm_x4(row + ((uint32_t)(k >> 2) << (box_log2 + 7)) + (uint32_t)((ch ^ (rr & 7)) << 4), b);
+                        mma_16816(s[2 * n], qf[k], b[0], b[1]);
+                        mma_16816(s[2 * n + 1], qf[k], b[2], b[3]);
+                    }
+                }
+                const int j0 = kt * C::KT + ks * C::WK;
+                float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                for (int n = 0; n < C::WK / 8; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float x = s[n][e] * a.scale_log2;
+                        if (edge && !pa_sees(a, pos[e >> 1], j0 + n * 8 + c2 + (e & 1))) x = -INFINITY;
+                        s[n][e] = x;
+                        mx[e >> 1] = fmaxf(mx[e >> 1], x);
+                    }
+                float f[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 1));
+                    mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2));
+                    const float mn = fmaxf(m[e], mx[e]);
+                    const float ref = mn == -INFINITY ? 0.f : mn;      // a row that has seen nothing yet: all weights 0
+                    f[e] = pa_exp2(m[e] - ref);
+                    m[e] = mn;
+                    mx[e] = ref;
+                    l[e] *= f[e];
+                }
+                uint32_t pf[C::WK / 16][4];
+#pragma unroll
+                for (int n = 0; n < C::WK / 8; ++n) {
+                    float p[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p[e] = pa_exp2(s[n][e] - mx[e >> 1]);
+                        l[e >> 1] += p[e];
+                    }
+                    pf[n >> 1][(n & 1) * 2] = pack_bf16x2(p[0], p[1]);
+                    pf[n >> 1][(n & 1) * 2 + 1] = pack_bf16x2(p[2], p[3]);
+                }
+                if (!__all_sync(0xffffffffu, f[0] == 1.f && f[1] == 1.f)) {
+#pragma unroll
+                    for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[n][e] *= f[e >> 1];
+                }
+#pragma unroll
+                for (int n = 0; n < C::WK / 16; ++n) {
+                    const int key = ks * C::WK + n * 16 + v_key;
+                    const int pg = key >> box_log2, rr = key & ((1 << box_log2) - 1);
+                    const uint32_t row = vb + ((uint32_t)(pg * C::NB) << (box_log2 + 7)) + rr * 128;
+                    // rows of the tile that no query sees (behind the end, between the sinks and the window) may hold
+                    // anything: their values become zeros, or 0 * NaN would reach the output
+                    uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
+                    if (edge) {
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int j = j0 + n * 16 + e * 8 + c2;
+                            const bool v0 = j < u.hi_key && (j >= u.lo_key || j < a.n_sink);
+                            const bool v1 = j + 1 < u.hi_key && (j + 1 >= u.lo_key || j + 1 < a.n_sink);
+                            keep[e] = (v0 ? 0xffffu : 0u) | (v1 ? 0xffff0000u : 0u);
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        uint32_t b[4];
+                        const int ch = (k & 3) * 2 + v_ch;
+                        ldmatrix_x4_trans(row + ((uint32_t)(k >> 2) << (box_log2 + 7)) + (uint32_t)((ch ^ (rr & 7)) << 4), b);
+                        mma_16816(o[2 * k], pf[n], b[0] & keep[0], b[1] & keep[1]);
+                        mma_16816(o[2 * k + 1], pf[n], b[2] & keep[0], b[3] & keep[1]);
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&empty[st.idx]);
+                st.next();
+            }
+
+            // ---- the piece's result: join the key groups, then write the rows or a partial record ----
+            const bool whole = w.whole();
+            const int rec = w.record(blockIdx.x);
+            float *prec = a.part + (size_t)rec * C::REC;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                l[e] += __shfl_xor_sync(0xffffffffu, l[e], 1);
+                l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
+            }
+            if ((lane & 3) == 0) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    stat_m[warp * 16 + g + e * 8] = m[e];
+                    stat_l[warp * 16 + g + e * 8] = l[e];
+                }
+            }
+            bar_consumers();
+            float mj[2], lj[2], sc[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                mj[e] = -INFINITY;
+                for (int k = 0; k < C::KS; ++k) mj[e] = fmaxf(mj[e], stat_m[(mt * C::KS + k) * 16 + g + e * 8]);
+                const float ref = mj[e] == -INFINITY ? 0.f : mj[e];
+                lj[e] = 0.f;
+                for (int k = 0; k < C::KS; ++k)
+                    lj[e] += stat_l[(mt * C::KS + k) * 16 + g + e * 8] * pa_exp2(stat_m[(mt * C::KS + k) * 16 + g + e * 8] - ref);
+                sc[e] = pa_exp2(m[e] - ref);
+                if (whole) sc[e] = lj[e] > 0.f ? sc[e] / lj[e] : (lj[e] == 0.f ? 0.f : lj[e]);   // NaN stays NaN
+            }
+            if (!whole && ks == 0 && (lane & 3) == 0) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = mt * 16 + g + e * 8;
+                    if (r < u.rows) {
+                        prec[C::ROWS * D + r] = mj[e];
+                        prec[C::ROWS * D + C::ROWS + r] = lj[e];
+                    }
+                }
+            }
+#pragma unroll
+            for (int cc = 0; cc < D / 32; ++cc) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        *reinterpret_cast<float2 *>(red + (warp * 16 + g + e * 8) * C::RED_PITCH + n * 8 + c2) =
+                            make_float2(o[cc * 4 + n][e * 2] * sc[e], o[cc * 4 + n][e * 2 + 1] * sc[e]);
+                }
+                bar_consumers();
+                for (int i = tid; i < C::ROWS * 8; i += 128) {
+                    const int r = i >> 3, c4 = (i & 7) * 4;
+                    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int k = 0; k < C::KS; ++k) {
+                        const float4 y = *reinterpret_cast<const float4 *>(red + (((r >> 4) * C::KS + k) * 16 + (r & 15)) * C::RED_PITCH + c4);
+                        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                    }
+                    if (r < u.rows) {
+                        if (whole) {
+                            const int fr = u.row0 + r, tok = u.tok0 + fr / a.group;
+                            if ((unsigned)tok < (unsigned)a.n_rows)
+                                *reinterpret_cast<uint2 *>(a.out + (long long)tok * a.o_st + (long long)(w.h * a.group + fr % a.group) * a.o_sh + cc * 32 + c4) =
+                                    make_uint2(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w));
+                        } else {
+                            *reinterpret_cast<float4 *>(prec + r * D + cc * 32 + c4) = x;
+                        }
+                    }
+                }
+                bar_consumers();
+            }
+            if (!whole) {
+                // the block that writes the last part of the pair joins all of them, in block order
+                const int b0 = w.first_block(), b1 = w.last_block();
+                __threadfence();
+                bar_consumers();
+                if (tid == 0) {
+                    const int n = atomicAdd(&a.counters[b0], 1);
+                    const int last = n == b1 - b0;
+                    if (last) a.counters[b0] = 0;
+                    *last_flag = last;
+                }
+                bar_consumers();
+                if (*last_flag) {
+                    __threadfence();
+                    for (int i = tid; i < u.rows * (D / 4); i += 128) {
+                        const int r = i / (D / 4), c4 = (i % (D / 4)) * 4;
+                        float mm = -INFINITY;
+                        for (int c = b0; c <= b1; ++c) mm = fmaxf(mm, __ldcg(a.part + (size_t)w.record(c) * C::REC + C::ROWS * D + r));
+                        const float ref = mm == -INFINITY ? 0.f : mm;
+                        float ll = 0.f;
+                        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                        for (int c = b0; c <= b1; ++c) {
+                            const float *rc = a.part + (size_t)w.record(c) * C::REC;
+                            const float f = pa_exp2(__ldcg(rc + C::ROWS * D + r) - ref);
+                            ll += f * __ldcg(rc + C::ROWS * D + C::ROWS + r);
+                            const float4 y = __ldcg(reinterpret_cast<const float4 *>(rc + r * D + c4));
+                            x.x += f * y.x; x.y += f * y.y; x.z += f * y.z; x.w += f * y.w;
+                        }
+                        const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
+                        const int fr = u.row0 + r, tok = u.tok0 + fr / a.group;
+                        if ((unsigned)tok < (unsigned)a.n_rows)
+                            *reinterpret_cast<uint2 *>(a.out + (long long)tok * a.o_st + (long long)(w.h * a.group + fr % a.group) * a.o_sh + c4) =
+                                make_uint2(pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv));
+                    }
+                }
+            }
+            more = w.next(a);
+        }
+    }
+    __syncthreads();
+    if (tid == 0 && abort_flag[0]) atomicExch(a.status, DEV_TIMEOUT);
+}
+
+size_t paged_attn_few_workspace(int d) { return (size_t)2 * 2 * device_sm_count() * 64 * (d + 2) * sizeof(float); }
+
+template <int D, int MT>
+static cudaError_t launch_few(const FewParams &P, cudaStream_t st)
+{
+    using C = FewCfg<D, MT>;
+    static bool attr[MAX_DEVICES] = {};
+    cudaError_t e = opt_in_smem(k_paged_attn_few<D, MT>, C::SMEM, attr);
+    if (e != cudaSuccess) return e;
+    k_paged_attn_few<D, MT><<<2 * device_sm_count(), C::THREADS, C::SMEM, st>>>(P);
+    e = cudaGetLastError();
+    if (e == cudaSuccess) count_launch();
+    return e;
+}
+
+cudaError_t launch_paged_attn_few(const PagedArgs &a, int d, const void *k, const void *v, int page_size, long long s_page,
+                                  long long s_slot, long long s_head, int max_new, cudaStream_t st)
+{
+    FewParams P;
+    P.a = a;
+    const int box = page_size < 64 ? page_size : 64;
+    if (!make_kv_tensor_map(&P.k, k, d, a.Hkv, page_size, a.n_pages, s_head, s_slot, s_page, box) ||
+        !make_kv_tensor_map(&P.v, v, d, a.Hkv, page_size, a.n_pages, s_head, s_slot, s_page, box))
+        return cudaErrorInvalidValue;
+    const long long rows = (long long)max_new * a.group;
+    if (d == 128) return rows <= 16 ? launch_few<128, 1>(P, st) : rows <= 32 ? launch_few<128, 2>(P, st) : launch_few<128, 4>(P, st);
+    return rows <= 16 ? launch_few<64, 1>(P, st) : rows <= 32 ? launch_few<64, 2>(P, st) : launch_few<64, 4>(P, st);
+}
+
+}  // namespace cb

@@ -1,6 +1,8 @@
 // Stand-alone rotary embedding of a strided bf16 key tensor, in place (Section 2.2, Section 3.1): removes (inverse) or
 // restores the position-dependent rotation outside the fused paths.  Pure streaming: one read and one write of K.
 #include "cb_internal.cuh"
+#include "cb_math.cuh"
+#include "cb_paged.cuh"
 #include "cb_rope.cuh"
 
 namespace cb {
@@ -61,6 +63,104 @@ cudaError_t launch_rope_rotate(void *k, int L, int H, int d, long long T, long l
     const int rows = 256 / (d / 16);
     dim3 grid((unsigned)((T + rows - 1) / rows), (unsigned)(L * H));
     k_rope_rotate<<<grid, 256, 0, stream>>>(a);
+    cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) count_launch();
+    return e;
+}
+
+// Rotary embedding with several position axes (time, height, width, ...), out of place or in place.  Every pair of
+// channels turns by the position of its own axis.  The cosines and sines of a row serve all its layers and heads: a
+// thread computes those of its eight pairs once and then streams over layers and heads, so that the angle arithmetic
+// (~25 operations a pair) stays below the time of the 8 bytes per pair that have to move.
+// Angles are turns in 0.64 fixed point: pos * f modulo 2^64 is exact for every 32-bit position, so the angle is off by
+// at most pos * 2^-56 turns (the frequency's own rounding from double) plus the 2^-24 turns of the sine's argument.
+struct RopeAxesArgs {
+    const __nv_bfloat16 *x;
+    __nv_bfloat16 *out;
+    long long x_sl, x_st, x_sh, o_sl, o_st, o_sh;
+    int H, d, LH, per;            // per: (layer, head) pairs of a block's threads
+    long long T;
+    const int *pos;
+    long long axis_stride;
+    int inverse;
+    unsigned char axis[ROPE_MAX_FREQ];
+    unsigned long long f[ROPE_MAX_FREQ];
+};
+
+// grid (row blocks, groups of (layer, head) pairs); 256 threads = (d / 16 chunk pairs) x rows
+__global__ void __launch_bounds__(256) k_rope_axes(const __grid_constant__ RopeAxesArgs a)
+{
+    const int HC = a.d / 16;
+    const int lc = threadIdx.x % HC;
+    const long long t = (long long)blockIdx.x * (256 / HC) + threadIdx.x / HC;
+    if (t >= a.T) return;
+    float cs[8], sn[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int i = lc * 8 + e;
+        const long long p = a.pos[(long long)a.axis[i] * a.axis_stride + t];
+        rope_cs_turns((uint32_t)(((unsigned long long)p * a.f[i]) >> 32), cs[e], sn[e]);
+        if (a.inverse) sn[e] = -sn[e];
+    }
+    const int lh1 = min(a.LH, (int)(blockIdx.y + 1) * a.per);
+    constexpr int BATCH = 4;      // rows in flight: all are loaded before the first is stored (x and out may be the same)
+    for (int lh0 = blockIdx.y * a.per; lh0 < lh1; lh0 += BATCH) {
+        uint4 vlo[BATCH], vhi[BATCH];
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            const int lh = lh0 + k;
+            if (lh >= lh1) break;
+            const int l = lh / a.H, h = lh - l * a.H;
+            const __nv_bfloat16 *row = a.x + l * a.x_sl + t * a.x_st + h * a.x_sh + lc * 8;
+            vlo[k] = *reinterpret_cast<const uint4 *>(row);
+            vhi[k] = *reinterpret_cast<const uint4 *>(row + a.d / 2);
+        }
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            const int lh = lh0 + k;
+            if (lh >= lh1) break;
+            const int l = lh / a.H, h = lh - l * a.H;
+            __nv_bfloat16 *to = a.out + l * a.o_sl + t * a.o_st + h * a.o_sh + lc * 8;
+            const unsigned ulo[4] = {vlo[k].x, vlo[k].y, vlo[k].z, vlo[k].w}, uhi[4] = {vhi[k].x, vhi[k].y, vhi[k].z, vhi[k].w};
+            unsigned olo[4], ohi[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float l0 = __uint_as_float(ulo[e] << 16), l1 = __uint_as_float(ulo[e] & 0xffff0000u);
+                const float h0 = __uint_as_float(uhi[e] << 16), h1 = __uint_as_float(uhi[e] & 0xffff0000u);
+                olo[e] = pack_bf16x2(l0 * cs[2 * e] - h0 * sn[2 * e], l1 * cs[2 * e + 1] - h1 * sn[2 * e + 1]);
+                ohi[e] = pack_bf16x2(l0 * sn[2 * e] + h0 * cs[2 * e], l1 * sn[2 * e + 1] + h1 * cs[2 * e + 1]);
+            }
+            *reinterpret_cast<uint4 *>(to) = make_uint4(olo[0], olo[1], olo[2], olo[3]);
+            *reinterpret_cast<uint4 *>(to + a.d / 2) = make_uint4(ohi[0], ohi[1], ohi[2], ohi[3]);
+        }
+    }
+}
+
+cudaError_t launch_rope_axes(const void *x, void *out, int L, int H, int d, long long T, const long long xs[3],
+                             const long long os[3], const int *positions, long long axis_stride, const unsigned char *axis_of_pair,
+                             double base, int inverse, cudaStream_t st)
+{
+    RopeAxesArgs a;
+    a.x = static_cast<const __nv_bfloat16 *>(x);
+    a.out = static_cast<__nv_bfloat16 *>(out);
+    a.x_sl = xs[0]; a.x_st = xs[1]; a.x_sh = xs[2];
+    a.o_sl = os[0]; a.o_st = os[1]; a.o_sh = os[2];
+    a.H = H; a.d = d; a.LH = L * H; a.T = T; a.pos = positions; a.axis_stride = axis_stride; a.inverse = inverse;
+    for (int i = 0; i < ROPE_MAX_FREQ; ++i) {
+        a.axis[i] = i < d / 2 ? axis_of_pair[i] : 0;
+        const double turns = i < d / 2 ? pow(base, -2.0 * (double)i / (double)d) / 6.283185307179586476925286766559 : 0.0;
+        a.f[i] = (unsigned long long)ldexp(turns, 64);          // turns < 0.16: no wrap
+    }
+    const long long rows = 256 / (d / 16), blocks = (T + rows - 1) / rows;
+    // enough blocks for four per SM, at most eight (layer, head) pairs a thread
+    const long long want = 4ll * device_sm_count();
+    long long groups = (want + blocks - 1) / blocks;
+    const long long least = (a.LH + 7) / 8;
+    if (groups < least) groups = least;
+    if (groups > a.LH) groups = a.LH;
+    a.per = (int)((a.LH + groups - 1) / groups);
+    dim3 grid((unsigned)blocks, (unsigned)((a.LH + a.per - 1) / a.per));
+    k_rope_axes<<<grid, 256, 0, st>>>(a);
     cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) count_launch();
     return e;

@@ -43,12 +43,11 @@ __device__ __forceinline__ void rope_cs(uint32_t f, int pos, float &c, float &s)
     s = -__sinf(ang);
 }
 
-// The same on the FMA pipe only (measured: the special-function unit delivers ~4 sine or cosine results per clock per
-// SM, the FMA pipe 128 operations): quadrant by the magic-number rounding of 4 t, then degree-7 / degree-8 polynomials
+// The same, of an angle in turns (0.32 fixed point), on the FMA pipe only (measured: the special-function unit delivers
+// ~4 sine or cosine results per clock per SM, the FMA pipe 128 operations): quadrant by the magic-number rounding of 4 t, then degree-7 / degree-8 polynomials
 // on [-pi/4, pi/4] (error ~1e-7), then the quadrant's swap and signs.  ~21 operations for the pair.
-__device__ __forceinline__ void rope_cs_poly(uint32_t f, int pos, float &c, float &s)
+__device__ __forceinline__ void rope_cs_turns(uint32_t wrapped, float &c, float &s)
 {
-    const uint32_t wrapped = (uint32_t)pos * f;
     const float t = __uint_as_float(0x3f800000u | (wrapped >> 9)) - 1.5f;      // angle - 1/2 turn, in [-0.5, 0.5) turns
     const float m = fmaf(t, 4.f, 12582912.f);                                   // 1.5 * 2^23: rounds 4 t to an integer
     const int q = __float_as_int(m);                                            // low bits = quadrant (two's complement)
@@ -71,6 +70,7 @@ __device__ __forceinline__ void rope_cs_poly(uint32_t f, int pos, float &c, floa
     c = __uint_as_float(__float_as_uint(cb) ^ cneg);
     s = __uint_as_float(__float_as_uint(sb) ^ sneg);
 }
+__device__ __forceinline__ void rope_cs_poly(uint32_t f, int pos, float &c, float &s) { rope_cs_turns((uint32_t)pos * f, c, s); }
 #endif
 
 }  // namespace cb
