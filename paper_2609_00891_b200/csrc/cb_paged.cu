@@ -1,5 +1,6 @@
 // Host side of the paged target cache: argument checks and launches (page tables, store, rotary positions with several
 // axes, attention).
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
@@ -140,7 +141,7 @@ cb_status cb_paged_attention_workspace_bytes(int32_t head_dim, size_t *bytes)
 {
     if (!bytes) return CB_ERR_INVALID_ARG;
     if (head_dim != 64 && head_dim != 128) return CB_ERR_UNSUPPORTED;
-    *bytes = PA_COUNTER_BYTES + paged_attn_few_workspace(head_dim);
+    *bytes = PA_COUNTER_BYTES + std::max(paged_attn_few_workspace(head_dim), paged_attn_tc_workspace(head_dim));
     return CB_OK;
 }
 
@@ -187,8 +188,12 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
     if (max_new == 0 || max_new > n_rows) max_new = (int32_t)n_rows;
     const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(pool->k) + layer * pool->stride_layer;
     const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(pool->v) + layer * pool->stride_layer;
-    if (const cudaError_t e = launch_paged_attn_few(a, pool->head_dim, k, v, pool->page_size, pool->stride_page, pool->stride_slot,
-                                                    pool->stride_head, max_new, static_cast<cudaStream_t>(stream)); e != cudaSuccess) return cuda_failed(e);
+    // up to 64 flattened rows per request and KV head: the warp-level kernel, which reads K and V at their bandwidth
+    const bool few = (long long)max_new * a.group <= 64;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = few ? launch_paged_attn_few(a, pool->head_dim, k, v, pool->page_size, pool->stride_page, pool->stride_slot, pool->stride_head, max_new, st)
+                              : launch_paged_attn_tc(a, pool->head_dim, k, v, pool->page_size, pool->stride_page, pool->stride_slot, pool->stride_head, st);
+    if (e != cudaSuccess) return cuda_failed(e);
     return CB_OK;
 }
 

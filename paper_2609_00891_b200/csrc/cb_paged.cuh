@@ -40,6 +40,9 @@ struct PagedArgs {
 cudaError_t launch_paged_attn_few(const PagedArgs &a, int d, const void *k, const void *v, int page_size, long long s_page,
                                   long long s_slot, long long s_head, int max_new, cudaStream_t st);
 size_t paged_attn_few_workspace(int d);
+cudaError_t launch_paged_attn_tc(const PagedArgs &a, int d, const void *k, const void *v, int page_size, long long s_page,
+                                 long long s_slot, long long s_head, cudaStream_t st);
+size_t paged_attn_tc_workspace(int d);
 
 cudaError_t launch_page_tables(const int *cached, const int *fresh, int n_requests, int page_log2, const int *free_pages,
                                long long n_free, int *table, long long table_stride, int table_cols, int *cu, int *total,

@@ -1,0 +1,442 @@
+// Attention of chunks of new rows over a paged cache on the tensor cores (tcgen05): the same sum as cb_paged_attn.cu for
+// more than 64 flattened rows per request and KV head, where the products bound the time.
+//
+// A unit is 256 flattened rows (new rows x the query heads of a KV head) as two tiles of 128, which share every key tile
+// of 128 keys.  Per thread block:
+//   producer warp    TMA, one box per page and 64-channel half, ring of K and V tiles (a page id outside the pool reads as
+//                    zeros).  Rows of a V tile that no row of the unit sees are set to zero before the tile is handed on.
+//   MMA thread       S_i = Q_i K^T into tensor memory, then O_i += P_i V with P_i read from tensor memory, i = 0, 1 in
+//                    turn: while the softmax warps work on one tile the tensor cores work on the other.
+//   2 x 4 softmax warps   one thread per row: scores to registers, running maximum, exp2, weights as bf16 back over the
+//                    scores in tensor memory.  The output is rescaled only when a maximum grows by more than 2^8 (weights
+//                    stay below 2^8, sums and outputs are fp32), which after the first tiles is hardly ever.
+// The tensor pipe runs a thread's products in order, so that S_i of the next tile may overwrite P_i, and its completion
+// also says that P_i V of the tile before is complete.
+#include "cb_paged.cuh"
+#include "cb_ptx.cuh"
+#include "cb_math.cuh"
+
+namespace cb {
+
+using namespace ptx;
+
+template <int D>
+struct TcAttnCfg {
+    static constexpr int ROWS = 256, KT = 128;
+    static constexpr int NB = D / 64;
+    static constexpr int BLK = 128 * 128;                  // bytes of 128 rows of 64 channels
+    static constexpr int TILE = NB * BLK;                  // a Q, K or V tile
+    static constexpr int NS = D == 128 ? 5 : 10;           // K and V tiles in flight
+    static constexpr int THREADS = 320;
+    static constexpr int TMEM_COLS = 512;                  // S0, S1: 128 columns each, then O0, O1: D columns each
+    static constexpr size_t SMEM = 1024 + 2 * (size_t)TILE + (size_t)NS * TILE + 512;
+    static constexpr int REC = 256 * (D + 2);              // floats of a partial record: [D / 4][256 rows][4], maxima, sums
+};
+
+struct TcAttnParams {
+    CUtensorMap k, v;
+    PagedArgs a;
+};
+
+__device__ __forceinline__ void bar_group(int i) { asm volatile("bar.sync %0, 128;" ::"r"(1 + i) : "memory"); }
+
+template <int D>
+__global__ void __launch_bounds__(320, 1) k_paged_attn_tc(const __grid_constant__ TcAttnParams P)
+{
+    using C = TcAttnCfg<D>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t *qs = smem;                                     // [2][TILE]
+    uint8_t *kv = smem + 2 * (size_t)C::TILE;               // [NS][TILE]
+    uint64_t *full = reinterpret_cast<uint64_t *>(kv + (size_t)C::NS * C::TILE);
+    uint64_t *empty = full + C::NS;
+    uint64_t *q_full = empty + C::NS;      // [2] Q tile written (4 warps)
+    uint64_t *s_full = q_full + 2;         // [2] scores complete
+    uint64_t *p_ready = s_full + 2;        // [2] weights written (4 warps)
+    uint64_t *o_full = p_ready + 2;        // [2] last product with V of a piece complete
+    uint64_t *fix = o_full + 2;            // a V tile that the producer clears rows of
+    uint64_t *drain = fix + 1;
+    long long *warp_sums = reinterpret_cast<long long *>(drain + 1);
+    PaShare *share = reinterpret_cast<PaShare *>(warp_sums + 10);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(share + 1);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+    volatile int *last_flag = abort_flag + 2;               // [2]
+
+    const PagedArgs &a = P.a;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int i = 0; i < C::NS; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&q_full[i], 4);
+            mbar_init(&s_full[i], 1);
+            mbar_init(&p_ready[i], 4);
+            mbar_init(&o_full[i], 1);
+        }
+        mbar_init(fix, 1);
+        mbar_init(drain, 1);
+        abort_flag[0] = 0;
+        abort_flag[1] = (int)a.poll_limit;
+        mbar_fence_init();
+        tma_prefetch_desc(&P.k);
+        tma_prefetch_desc(&P.v);
+    }
+    if (warp == 9) tmem_alloc(tmem_slot, C::TMEM_COLS);
+    tc_fence_before();
+    pa_schedule<C::ROWS, C::KT, C::THREADS>(a, reinterpret_cast<int *>(smem), (2 + C::NS) * C::TILE / 4, share, warp_sums);
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    PaWalk<C::ROWS, C::KT> w;
+    const bool any = w.open(a, *share);
+    const int box_log2 = a.page_log2 < 7 ? a.page_log2 : 7;
+    bool dead = false;       // a wait ran out: no more waits, the rest runs through on whatever is there
+
+    if (warp == 8) {
+        // ================================ producer ================================
+        if (any && !a.starve) {
+            Ring<C::NS> st;
+            int issued = 0;
+            uint32_t n_fix = 0;
+            const int n_page = 1 << (7 - box_log2);
+            const int cb = lane / n_page, i = lane - cb * n_page;        // 64-channel block and box of this lane
+            bool more = true;
+            while (more) {
+                const int *row = a.table + (long long)w.u.b * a.table_stride;
+                for (int t = w.t; t < w.t1 && !dead; ++t) {
+                    const int j0 = pa_tile(w.u, t) * C::KT;
+                    const int key = j0 + (i << box_log2);
+                    int page = a.n_pages;                                // outside the pool: the copy writes zeros
+                    if (cb < C::NB && key < w.u.hi_key) {
+                        const int col = key >> a.page_log2;
+                        if (col < a.table_cols) page = __ldg(row + col);
+                    }
+                    const int slot = key & ((1 << a.page_log2) - 1);
+                    // keys of the tile outside [lo_key, hi_key) and behind the sinks: nobody sees them
+                    const bool clear = j0 + C::KT > w.u.hi_key || (j0 < w.u.lo_key && j0 + C::KT > a.n_sink);
+                    for (int comp = 0; comp < 2; ++comp) {
+                        if (!mbar_wait_warp(&empty[st.idx], st.phase ^ 1, abort_flag, lane, true)) { dead = true; break; }
+                        uint64_t *bar = comp && clear ? fix : &full[st.idx];
+                        uint8_t *dst = kv + (size_t)st.idx * C::TILE;
+                        if (lane == 0) mbar_arrive_expect_tx(bar, C::TILE);
+                        __syncwarp();
+                        if (cb < C::NB)
+                            tma_load_5d(dst + cb * C::BLK + ((size_t)i << (box_log2 + 7)), comp ? &P.v : &P.k, bar, 0, slot, cb, w.h, page);
+                        if (comp && clear) {
+                            if (!mbar_wait_warp(fix, n_fix & 1, abort_flag, lane)) dead = true;
+                            ++n_fix;
+                            const int c0 = max(0, w.u.hi_key - j0);                                  // rows [c0, 128)
+                            const int g0 = max(0, a.n_sink - j0), g1 = min(C::KT, w.u.lo_key - j0);  // rows [g0, g1)
+                            for (int r = lane; r < C::KT * C::NB * 8; r += 32) {
+                                const int key_row = (r >> 3) & (C::KT - 1);
+                                if (key_row >= c0 || (key_row >= g0 && key_row < g1))
+                                    *reinterpret_cast<uint4 *>(dst + (r >> 10) * C::BLK + key_row * 128 + (r & 7) * 16) = make_uint4(0, 0, 0, 0);
+                            }
+                            fence_async_smem();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&full[st.idx]);
+                        }
+                        st.next();
+                        ++issued;
+                        if (dead) break;
+                    }
+                }
+                more = !dead && w.next(a);
+            }
+            // after a time-out the copies in flight land before the block ends
+            for (int k = dead ? min(issued, C::NS) : 0; k > 0; --k) {
+                mbar_wait_warp(&full[st.idx], st.phase ^ 1, abort_flag, lane, true);
+                st.next();
+            }
+        }
+    } else if (warp == 9) {
+        // ================================ MMA issuer (one thread) ================================
+        if (lane == 0 && any) {
+            constexpr uint32_t idesc_s = umma_idesc_bf16(128, C::KT, false, false);   // both K-major
+            constexpr uint32_t idesc_o = umma_idesc_bf16(128, D, false, true);        // V: MN-major
+            const uint64_t proto_k = umma_smem_desc_sw128(0, 16, 1024);
+            const uint64_t proto_v = umma_smem_desc_sw128(0, C::BLK, 1024);
+            const uint32_t q_addr = (smem_u32(qs) & 0x3FFFFu) >> 4, kv_addr = (smem_u32(kv) & 0x3FFFFu) >> 4;
+            Ring<C::NS> st;
+            uint32_t piece = 0, np[2] = {0, 0};
+            bool more = true;
+            auto scores = [&](int i, uint32_t stage) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t off = (k >> 2) * (C::BLK >> 4) + (k & 3) * 2;
+                    umma_bf16_ss(tmem + i * 128, proto_k | (uint64_t)(q_addr + i * (C::TILE >> 4) + off),
+                                 proto_k | (uint64_t)(kv_addr + stage * (C::TILE >> 4) + off), idesc_s, k == 0 ? 0u : 1u);
+                }
+                umma_commit(&s_full[i]);
+            };
+            auto values = [&](int i, uint32_t stage, bool first) {
+#pragma unroll
+                for (int k = 0; k < C::KT / 16; ++k)
+                    umma_bf16_ts(tmem + 256 + i * D, tmem + i * 128 + k * 8, proto_v | (uint64_t)(kv_addr + stage * (C::TILE >> 4) + k * 128), idesc_o,
+                                 first && k == 0 ? 0u : 1u);
+            };
+            uint32_t nq[2] = {0, 0};
+            while (more && !dead) {
+                const int tiles = w.u.rows > 128 ? 2 : 1;
+                // K of the piece's first tile
+                uint32_t ks = st.idx;
+                if (!mbar_wait(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
+                st.next();
+                for (int i = 0; i < tiles; ++i) {
+                    if (!mbar_wait(&q_full[i], nq[i]++ & 1, abort_flag)) { dead = true; break; }
+                    tc_fence_after();
+                    scores(i, ks);
+                }
+                if (dead) break;
+                umma_commit(&empty[ks]);
+                for (int t = w.t; t < w.t1 && !dead; ++t) {
+                    const bool last = t + 1 == w.t1;
+                    const uint32_t vs = st.idx;
+                    if (!mbar_wait(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
+                    st.next();
+                    for (int i = 0; i < tiles; ++i) {
+                        if (!mbar_wait(&p_ready[i], np[i]++ & 1, abort_flag)) { dead = true; break; }
+                        tc_fence_after();
+                        values(i, vs, t == w.t);
+                        if (last) umma_commit(&o_full[i]);
+                        if (i == tiles - 1) umma_commit(&empty[vs]);
+                        if (!last) {
+                            if (i == 0) {
+                                ks = st.idx;
+                                if (!mbar_wait(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
+                                st.next();
+                            }
+                            scores(i, ks);
+                            if (i == tiles - 1) umma_commit(&empty[ks]);
+                        }
+                    }
+                }
+                ++piece;
+                more = !dead && w.next(a);
+            }
+            if (dead) {                                    // products in flight end before tensor memory is freed
+                umma_commit(drain);
+                mbar_wait(drain, 0, abort_flag, 1u << 20);
+            }
+        }
+    } else if (any) {
+        // ================================ softmax warps: one thread per row ================================
+        const int i = warp >> 2;                           // tile
+        const int r = tid & 127;                           // row in the tile
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_tm = tmem + i * 128 + lanes, o_tm = tmem + 256 + i * D + lanes;
+        const float c = a.scale_log2;
+        uint32_t ns = 0, no = 0;
+        bool more = true;
+        while (more) {
+            const PaUnit &u = w.u;
+            const int rr = i * 128 + r;                    // row in the unit
+            if (i * 128 < u.rows) {
+                const int fr = u.row0 + rr, tok = u.tok0 + fr / a.group, head = w.h * a.group + fr % a.group;
+                const bool live = rr < u.rows && (unsigned)tok < (unsigned)a.n_rows;
+                const int pos = live ? u.base + fr / a.group : -1;
+                // the piece's Q tile; the products that read the one before it are complete
+                {
+                    const uint4 *src = reinterpret_cast<const uint4 *>(a.q + (long long)tok * a.q_st + (long long)head * a.q_sh);
+                    uint8_t *dst = qs + i * C::TILE + r * 128;
+#pragma unroll
+                    for (int x = 0; x < D / 8; ++x)
+                        *reinterpret_cast<uint4 *>(dst + (x >> 3) * C::BLK + (((x & 7) ^ (r & 7)) << 4)) = live ? src[x] : make_uint4(0, 0, 0, 0);
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&q_full[i]);
+                }
+                float m = -INFINITY, l = 0.f;              // reference maximum (raw score), sum of weights
+                for (int t = w.t; t < w.t1; ++t) {
+                    const int kt = pa_tile(u, t);
+                    if (!dead && !mbar_wait_warp(&s_full[i], ns & 1, abort_flag, lane)) dead = true;
+                    ++ns;
+                    tc_fence_after();
+                    uint32_t s[4][32];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) tmem_ld_32x32(s_tm + x * 32, s[x]);
+                    tmem_wait_ld();
+                    if (!pa_tile_full<C::KT>(a, u, kt)) {
+                        const int j0 = kt * C::KT;
+                        const int hi = pos - j0;                                               // last column seen
+                        const int lo = a.window > 0 ? (int)max((long long)pos - a.window + 1 - j0, -1ll) : -1;   // first one, without
+                        const int sink = a.window > 0 ? a.n_sink - j0 : 0;                     // the sinks
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+#pragma unroll
+                            for (int y = 0; y < 32; ++y) {
+                                const int col = x * 32 + y;
+                                if (col > hi || (col < lo && col >= sink)) s[x][y] = 0xff800000u;
+                            }
+                    }
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int y = 0; y < 32; ++y)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) mx[x] = fmaxf(mx[x], __uint_as_float(s[x][y]));
+                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                    float f = 1.f;
+                    if ((top - m) * c > 8.f) {             // also the first maximum of a row: m is -inf
+                        f = pa_exp2((m - top) * c);
+                        m = top;
+                        l *= f;
+                    }
+                    if (t > w.t && __any_sync(0xffffffffu, f != 1.f)) {
+#pragma unroll 1
+                        for (int x = 0; x < D / 32; ++x) {
+                            uint32_t o[32];
+                            tmem_ld_32x32(o_tm + x * 32, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int y = 0; y < 32; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * f);
+                            tmem_st_32x32(o_tm + x * 32, o);
+                        }
+                    }
+                    const float mc = m == -INFINITY ? 0.f : -m * c;
+                    float sum[2] = {0.f, 0.f};
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int y = 0; y < 16; ++y) {
+                            const float p0 = pa_exp2(fmaf(__uint_as_float(s[x][2 * y]), c, mc));
+                            const float p1 = pa_exp2(fmaf(__uint_as_float(s[x][2 * y + 1]), c, mc));
+                            sum[0] += p0;
+                            sum[1] += p1;
+                            p[y] = pack_bf16x2(p0, p1);
+                        }
+                        tmem_st_32x16(s_tm + x * 16, p);
+                    }
+                    l += sum[0] + sum[1];
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_ready[i]);
+                }
+
+                // ---- the piece's result ----
+                if (!dead && !mbar_wait_warp(&o_full[i], no & 1, abort_flag, lane)) dead = true;
+                ++no;
+                tc_fence_after();
+                __nv_bfloat16 *orow = a.out + (long long)tok * a.o_st + (long long)head * a.o_sh;
+                if (w.whole()) {
+                    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+#pragma unroll 1
+                    for (int x = 0; x < D / 32; ++x) {
+                        uint32_t o[32];
+                        tmem_ld_32x32(o_tm + x * 32, o);
+                        tmem_wait_ld();
+                        if (live) {
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) {
+                                uint4 v;
+                                v.x = pack_bf16x2(__uint_as_float(o[y * 8 + 0]) * inv, __uint_as_float(o[y * 8 + 1]) * inv);
+                                v.y = pack_bf16x2(__uint_as_float(o[y * 8 + 2]) * inv, __uint_as_float(o[y * 8 + 3]) * inv);
+                                v.z = pack_bf16x2(__uint_as_float(o[y * 8 + 4]) * inv, __uint_as_float(o[y * 8 + 5]) * inv);
+                                v.w = pack_bf16x2(__uint_as_float(o[y * 8 + 6]) * inv, __uint_as_float(o[y * 8 + 7]) * inv);
+                                *reinterpret_cast<uint4 *>(orow + x * 32 + y * 8) = v;
+                            }
+                        }
+                    }
+                    tc_fence_before();
+                } else {
+                    float *rec = a.part + (size_t)w.record(blockIdx.x) * C::REC;
+#pragma unroll 1
+                    for (int x = 0; x < D / 32; ++x) {
+                        uint32_t o[32];
+                        tmem_ld_32x32(o_tm + x * 32, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int y = 0; y < 8; ++y)
+                            *reinterpret_cast<float4 *>(rec + ((size_t)(x * 8 + y) * 256 + rr) * 4) =
+                                make_float4(__uint_as_float(o[y * 4]), __uint_as_float(o[y * 4 + 1]), __uint_as_float(o[y * 4 + 2]), __uint_as_float(o[y * 4 + 3]));
+                    }
+                    tc_fence_before();
+                    rec[256 * D + rr] = m * c;             // c > 0: -inf stays -inf
+                    rec[256 * D + 256 + rr] = l;
+                    // the block that writes the last part of the pair joins all of them, in block order
+                    const int b0 = w.first_block(), b1 = w.last_block();
+                    __threadfence();
+                    bar_group(i);
+                    if (r == 0) {
+                        const int n = atomicAdd(&a.counters[2 * b0 + i], 1);
+                        const int last = n == b1 - b0;
+                        if (last) a.counters[2 * b0 + i] = 0;
+                        last_flag[i] = last;
+                    }
+                    bar_group(i);
+                    if (last_flag[i]) {
+                        __threadfence();
+                        float mm = -INFINITY;
+                        for (int b = b0; b <= b1; ++b) mm = fmaxf(mm, __ldcg(a.part + (size_t)w.record(b) * C::REC + 256 * D + rr));
+                        const float ref = mm == -INFINITY ? 0.f : mm;
+                        float ll = 0.f;
+                        for (int b = b0; b <= b1; ++b) {
+                            const float *rc = a.part + (size_t)w.record(b) * C::REC + 256 * D + rr;
+                            ll += pa_exp2(__ldcg(rc) - ref) * __ldcg(rc + 256);
+                        }
+                        const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
+#pragma unroll 1
+                        for (int x = 0; x < D / 32; ++x) {
+                            float acc[32];
+#pragma unroll
+                            for (int y = 0; y < 32; ++y) acc[y] = 0.f;
+                            for (int b = b0; b <= b1; ++b) {
+                                const float *rc = a.part + (size_t)w.record(b) * C::REC;
+                                const float f = pa_exp2(__ldcg(rc + 256 * D + rr) - ref) * inv;
+#pragma unroll
+                                for (int y = 0; y < 8; ++y) {
+                                    const float4 v = __ldcg(reinterpret_cast<const float4 *>(rc + ((size_t)(x * 8 + y) * 256 + rr) * 4));
+                                    acc[y * 4] += f * v.x; acc[y * 4 + 1] += f * v.y; acc[y * 4 + 2] += f * v.z; acc[y * 4 + 3] += f * v.w;
+                                }
+                            }
+                            if (live) {
+#pragma unroll
+                                for (int y = 0; y < 4; ++y)
+                                    *reinterpret_cast<uint4 *>(orow + x * 32 + y * 8) =
+                                        make_uint4(pack_bf16x2(acc[y * 8], acc[y * 8 + 1]), pack_bf16x2(acc[y * 8 + 2], acc[y * 8 + 3]),
+                                                   pack_bf16x2(acc[y * 8 + 4], acc[y * 8 + 5]), pack_bf16x2(acc[y * 8 + 6], acc[y * 8 + 7]));
+                            }
+                        }
+                    }
+                    bar_group(i);                          // last_flag is read before the next piece writes it
+                }
+            }
+            more = w.next(a);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (tid == 0 && abort_flag[0]) atomicExch(a.status, DEV_TIMEOUT);
+    if (warp == 9) tmem_dealloc(tmem, C::TMEM_COLS);
+}
+
+size_t paged_attn_tc_workspace(int d) { return (size_t)2 * device_sm_count() * 256 * (d + 2) * sizeof(float); }
+
+template <int D>
+static cudaError_t launch_tc_attn(const TcAttnParams &P, cudaStream_t st)
+{
+    using C = TcAttnCfg<D>;
+    static bool attr[MAX_DEVICES] = {};
+    cudaError_t e = opt_in_smem(k_paged_attn_tc<D>, C::SMEM, attr);
+    if (e != cudaSuccess) return e;
+    k_paged_attn_tc<D><<<device_sm_count(), C::THREADS, C::SMEM, st>>>(P);
+    e = cudaGetLastError();
+    if (e == cudaSuccess) count_launch();
+    return e;
+}
+
+cudaError_t launch_paged_attn_tc(const PagedArgs &a, int d, const void *k, const void *v, int page_size, long long s_page,
+                                 long long s_slot, long long s_head, cudaStream_t st)
+{
+    TcAttnParams P;
+    P.a = a;
+    const int box = page_size < 128 ? page_size : 128;
+    if (!make_kv_tensor_map(&P.k, k, d, a.Hkv, page_size, a.n_pages, s_head, s_slot, s_page, box, 1) ||
+        !make_kv_tensor_map(&P.v, v, d, a.Hkv, page_size, a.n_pages, s_head, s_slot, s_page, box, 1))
+        return cudaErrorInvalidValue;
+    return d == 128 ? launch_tc_attn<128>(P, st) : launch_tc_attn<64>(P, st);
+}
+
+}  // namespace cb
