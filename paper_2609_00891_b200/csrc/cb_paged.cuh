@@ -117,6 +117,12 @@ __device__ __forceinline__ bool pa_tile_full(const PagedArgs &a, const PaUnit &u
     if (j0 + KT - 1 > u.p0) return false;
     return a.window <= 0 || (long long)u.p1 - j0 < a.window || j0 + KT <= a.n_sink;
 }
+// Some key of the tile at j0 is seen by no row of the unit.
+template <int KT>
+__device__ __forceinline__ bool pa_clears(const PagedArgs &a, const PaUnit &u, int j0)
+{
+    return j0 + KT > u.hi_key || (j0 < u.lo_key && j0 + KT > a.n_sink);
+}
 __device__ __forceinline__ bool pa_sees(const PagedArgs &a, int p, int j)
 {
     return j <= p && (a.window <= 0 || p - j < a.window || j < a.n_sink);

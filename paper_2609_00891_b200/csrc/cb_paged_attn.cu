@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
                         const int col = key >> a.page_log2;
                         if (col < a.table_cols) page = __ldg(row + col);
                     }
-                    if (!mbar_wait_warp(&empty[st.idx], st.phase ^ 1, abort_flag, lane, true)) { dead = true; break; }
+                    if (!mbar_wait_suspended_warp(&empty[st.idx], st.phase ^ 1, abort_flag)) { dead = true; break; }
                     if (lane == 0) mbar_arrive_expect_tx(&full[st.idx], C::STAGE);
                     __syncwarp();
                     if (lane < n_box)
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
             }
             // after a time-out the copies in flight land before the block ends
             for (int i = dead ? min(issued, C::NS) : 0; i > 0; --i) {
-                mbar_wait_warp(&full[st.idx], st.phase ^ 1, abort_flag, lane, true);
+                mbar_wait_suspended_warp(&full[st.idx], st.phase ^ 1, abort_flag);
                 st.next();
             }
         }
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
             for (int t = w.t; t < w.t1; ++t) {
                 const int kt = pa_tile(u, t);
                 const bool edge = !pa_tile_full<C::KT>(a, u, kt);
-                if (!dead && !mbar_wait_warp(&full[st.idx], st.phase, abort_flag, lane)) dead = true;
+                if (!dead && !mbar_wait_suspended_warp(&full[st.idx], st.phase, abort_flag)) dead = true;
                 const uint32_t kb = smem_base + st.idx * C::STAGE, vb = kb + C::HALF;
                 float s[C::WK / 8][4];
 #pragma unroll

@@ -4,7 +4,9 @@
 // A unit is 256 flattened rows (new rows x the query heads of a KV head) as two tiles of 128, which share every key tile
 // of 128 keys.  Per thread block:
 //   producer warp    TMA, one box per page and 64-channel half, ring of K and V tiles (a page id outside the pool reads as
-//                    zeros).  Rows of a V tile that no row of the unit sees are set to zero before the tile is handed on.
+//                    zeros).
+//   clearing warp    rows of a V tile that no row of the unit sees may hold anything and 0 * NaN is NaN: a tile that has
+//                    such rows lands on a barrier of its own, and this warp sets them to zero before it hands it on.
 //   MMA thread       S_i = Q_i K^T into tensor memory, then O_i += P_i V with P_i read from tensor memory, i = 0, 1 in
 //                    turn: while the softmax warps work on one tile the tensor cores work on the other.
 //   2 x 4 softmax warps   one thread per row: scores to registers, running maximum, exp2, weights as bf16 back over the
@@ -27,9 +29,9 @@ struct TcAttnCfg {
     static constexpr int BLK = 128 * 128;                  // bytes of 128 rows of 64 channels
     static constexpr int TILE = NB * BLK;                  // a Q, K or V tile
     static constexpr int NS = D == 128 ? 5 : 10;           // K and V tiles in flight
-    static constexpr int THREADS = 320;
+    static constexpr int THREADS = 384;
     static constexpr int TMEM_COLS = 512;                  // S0, S1: 128 columns each, then O0, O1: D columns each
-    static constexpr size_t SMEM = 1024 + 2 * (size_t)TILE + (size_t)NS * TILE + 512;
+    static constexpr size_t SMEM = 1024 + 2 * (size_t)TILE + (size_t)NS * TILE + 1536;
     static constexpr int REC = 256 * (D + 2);              // floats of a partial record: [D / 4][256 rows][4], maxima, sums
 };
 
@@ -40,8 +42,31 @@ struct TcAttnParams {
 
 __device__ __forceinline__ void bar_group(int i) { asm volatile("bar.sync %0, 128;" ::"r"(1 + i) : "memory"); }
 
+// Columns 0 .. n - 1 of 32 as a bit mask (n may be anything).
+__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
+// 2^x of a pair on the FMA pipe: x = n + f with n = round(x) by the magic-number addition, 2^f by a cubic with p(0) = 1
+// fitted to 2^f on [-1/2, 1/2] (relative error 1.0e-4 = 2^-13, a weight's rounding to bf16 is 2^-8), n added to the
+// exponent bits.  x <= 8; below -127 the result is exactly 0 (p(0) = 1 meets the exponent -127), so -inf gives 0.
+__device__ __forceinline__ void exp2_fma(uint64_t x, float &p0, float &p1)
+{
+    float x0, x1, n0, n1;
+    f2_unpack(x, x0, x1);
+    x = f2_pack(fmaxf(x0, -127.f), fmaxf(x1, -127.f));
+    const uint64_t n = f2_add(x, f2_pack(12582912.f, 12582912.f));
+    const uint64_t f = f2_fma(f2_add(n, f2_pack(-12582912.f, -12582912.f)), f2_pack(-1.f, -1.f), x);
+    uint64_t p = f2_fma(f, f2_pack(0.0550089292f, 0.0550089292f), f2_pack(0.242210969f, 0.242210969f));
+    p = f2_fma(p, f, f2_pack(0.693282902f, 0.693282902f));
+    p = f2_fma(p, f, f2_pack(1.f, 1.f));
+    f2_unpack(p, p0, p1);
+    f2_unpack(n, n0, n1);
+    p0 = __int_as_float(__float_as_int(p0) + (__float_as_int(n0) << 23));
+    p1 = __int_as_float(__float_as_int(p1) + (__float_as_int(n1) << 23));
+}
+constexpr int EMULATED = 1;       // of every four pairs of a row
+
 template <int D>
-__global__ void __launch_bounds__(320, 1) k_paged_attn_tc(const __grid_constant__ TcAttnParams P)
+__global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant__ TcAttnParams P)
 {
     using C = TcAttnCfg<D>;
     extern __shared__ uint8_t smem_raw[];
@@ -52,27 +77,29 @@ __global__ void __launch_bounds__(320, 1) k_paged_attn_tc(const __grid_constant_
     uint64_t *empty = full + C::NS;
     uint64_t *q_full = empty + C::NS;      // [2] Q tile written (4 warps)
     uint64_t *s_full = q_full + 2;         // [2] scores complete
-    uint64_t *p_ready = s_full + 2;        // [2] weights written (4 warps)
-    uint64_t *o_full = p_ready + 2;        // [2] last product with V of a piece complete
-    uint64_t *fix = o_full + 2;            // a V tile that the producer clears rows of
-    uint64_t *drain = fix + 1;
+    uint64_t *p_ready = s_full + 2;        // [2][2] weights of the first and second 64 keys written (4 warps)
+    uint64_t *o_full = p_ready + 4;        // [2] last product with V of a piece complete
+    uint64_t *landed = o_full + 2;         // [NS] a V tile that has rows to clear: copied
+    uint64_t *drain = landed + C::NS;
     long long *warp_sums = reinterpret_cast<long long *>(drain + 1);
-    PaShare *share = reinterpret_cast<PaShare *>(warp_sums + 10);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(share + 1);
+    PaShare *share = reinterpret_cast<PaShare *>(warp_sums + 12);
+    using Walk = PaWalk<C::ROWS, C::KT>;
+    Walk *walks = reinterpret_cast<Walk *>(share + 1);      // [8] of the softmax warps, whose registers hold scores
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(walks + 8);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     volatile int *last_flag = abort_flag + 2;               // [2]
 
     const PagedArgs &a = P.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        for (int i = 0; i < C::NS; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+        for (int i = 0; i < C::NS; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&landed[i], 1); }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&q_full[i], 4);
             mbar_init(&s_full[i], 1);
-            mbar_init(&p_ready[i], 4);
+            mbar_init(&p_ready[2 * i], 4);
+            mbar_init(&p_ready[2 * i + 1], 4);
             mbar_init(&o_full[i], 1);
         }
-        mbar_init(fix, 1);
         mbar_init(drain, 1);
         abort_flag[0] = 0;
         abort_flag[1] = (int)a.poll_limit;
@@ -86,17 +113,20 @@ __global__ void __launch_bounds__(320, 1) k_paged_attn_tc(const __grid_constant_
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
 
-    PaWalk<C::ROWS, C::KT> w;
-    const bool any = w.open(a, *share);
+    const bool any = share->begin < share->end;
     const int box_log2 = a.page_log2 < 7 ? a.page_log2 : 7;
     bool dead = false;       // a wait ran out: no more waits, the rest runs through on whatever is there
 
+    // the softmax warps hold a row of 128 scores each: 208 + 208 + 88 registers a thread of the 3 x 168 launched with
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    Walk w;
+    if (any) w.open(a, *share);
     if (warp == 8) {
         // ================================ producer ================================
         if (any && !a.starve) {
             Ring<C::NS> st;
             int issued = 0;
-            uint32_t n_fix = 0;
             const int n_page = 1 << (7 - box_log2);
             const int cb = lane / n_page, i = lane - cb * n_page;        // 64-channel block and box of this lane
             bool more = true;
@@ -111,41 +141,58 @@ __global__ void __launch_bounds__(320, 1) k_paged_attn_tc(const __grid_constant_
                         if (col < a.table_cols) page = __ldg(row + col);
                     }
                     const int slot = key & ((1 << a.page_log2) - 1);
-                    // keys of the tile outside [lo_key, hi_key) and behind the sinks: nobody sees them
-                    const bool clear = j0 + C::KT > w.u.hi_key || (j0 < w.u.lo_key && j0 + C::KT > a.n_sink);
+                    const bool clear = pa_clears<C::KT>(a, w.u, j0);
                     for (int comp = 0; comp < 2; ++comp) {
-                        if (!mbar_wait_warp(&empty[st.idx], st.phase ^ 1, abort_flag, lane, true)) { dead = true; break; }
-                        uint64_t *bar = comp && clear ? fix : &full[st.idx];
+                        if (!mbar_wait_suspended_warp(&empty[st.idx], st.phase ^ 1, abort_flag)) { dead = true; break; }
+                        uint64_t *bar = comp && clear ? &landed[st.idx] : &full[st.idx];
                         uint8_t *dst = kv + (size_t)st.idx * C::TILE;
                         if (lane == 0) mbar_arrive_expect_tx(bar, C::TILE);
                         __syncwarp();
                         if (cb < C::NB)
                             tma_load_5d(dst + cb * C::BLK + ((size_t)i << (box_log2 + 7)), comp ? &P.v : &P.k, bar, 0, slot, cb, w.h, page);
-                        if (comp && clear) {
-                            if (!mbar_wait_warp(fix, n_fix & 1, abort_flag, lane)) dead = true;
-                            ++n_fix;
-                            const int c0 = max(0, w.u.hi_key - j0);                                  // rows [c0, 128)
-                            const int g0 = max(0, a.n_sink - j0), g1 = min(C::KT, w.u.lo_key - j0);  // rows [g0, g1)
-                            for (int r = lane; r < C::KT * C::NB * 8; r += 32) {
-                                const int key_row = (r >> 3) & (C::KT - 1);
-                                if (key_row >= c0 || (key_row >= g0 && key_row < g1))
-                                    *reinterpret_cast<uint4 *>(dst + (r >> 10) * C::BLK + key_row * 128 + (r & 7) * 16) = make_uint4(0, 0, 0, 0);
-                            }
-                            fence_async_smem();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(&full[st.idx]);
-                        }
                         st.next();
                         ++issued;
-                        if (dead) break;
                     }
                 }
                 more = !dead && w.next(a);
             }
             // after a time-out the copies in flight land before the block ends
             for (int k = dead ? min(issued, C::NS) : 0; k > 0; --k) {
-                mbar_wait_warp(&full[st.idx], st.phase ^ 1, abort_flag, lane, true);
+                mbar_wait_suspended_warp(&full[st.idx], st.phase ^ 1, abort_flag);
                 st.next();
+            }
+        }
+    } else if (warp == 10) {
+        // ================================ clears rows of V tiles ================================
+        if (any) {
+            uint32_t stage = 0, uses = 0;                  // position in the ring; bit s: parity of stage s's next landing
+            bool more = true;
+            while (more) {
+                for (int t = w.t; t < w.t1 && !dead; ++t) {
+                    const int j0 = pa_tile(w.u, t) * C::KT;
+                    stage = (stage + 1) % C::NS;           // past the K tile
+                    if (pa_clears<C::KT>(a, w.u, j0)) {
+                        if (!mbar_wait_suspended_warp(&landed[stage], (uses >> stage) & 1, abort_flag)) { dead = true; break; }
+                        uses ^= 1u << stage;
+                        uint8_t *dst = kv + (size_t)stage * C::TILE;
+                        // keys outside [lo_key, hi_key) and behind the sinks: nobody sees them
+                        const int c0 = max(0, w.u.hi_key - j0);                                  // rows [c0, 128)
+                        const int g0 = max(0, a.n_sink - j0), g1 = min(C::KT, w.u.lo_key - j0);  // rows [g0, g1)
+                        const int r0 = g0 < g1 ? min(c0, g0) : c0;
+                        for (int r = r0 * 8 + lane; r < C::KT * 8; r += 32) {
+                            const int key_row = r >> 3;
+                            if (key_row >= c0 || (key_row >= g0 && key_row < g1)) {
+#pragma unroll
+                                for (int cb = 0; cb < C::NB; ++cb) *reinterpret_cast<uint4 *>(dst + cb * C::BLK + r * 16) = make_uint4(0, 0, 0, 0);
+                            }
+                        }
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&full[stage]);
+                    }
+                    stage = (stage + 1) % C::NS;
+                }
+                more = !dead && w.next(a);
             }
         }
     } else if (warp == 9) {
@@ -157,7 +204,7 @@ __global__ void __launch_bounds__(320, 1) k_paged_attn_tc(const __grid_constant_
             const uint64_t proto_v = umma_smem_desc_sw128(0, C::BLK, 1024);
             const uint32_t q_addr = (smem_u32(qs) & 0x3FFFFu) >> 4, kv_addr = (smem_u32(kv) & 0x3FFFFu) >> 4;
             Ring<C::NS> st;
-            uint32_t piece = 0, np[2] = {0, 0};
+            uint32_t np[2] = {0, 0};
             bool more = true;
             auto scores = [&](int i, uint32_t stage) {
 #pragma unroll
@@ -168,21 +215,23 @@ __global__ void __launch_bounds__(320, 1) k_paged_attn_tc(const __grid_constant_
                 }
                 umma_commit(&s_full[i]);
             };
-            auto values = [&](int i, uint32_t stage, bool first) {
+            auto values = [&](int i, uint32_t stage, bool first, int half) {
 #pragma unroll
-                for (int k = 0; k < C::KT / 16; ++k)
-                    umma_bf16_ts(tmem + 256 + i * D, tmem + i * 128 + k * 8, proto_v | (uint64_t)(kv_addr + stage * (C::TILE >> 4) + k * 128), idesc_o,
-                                 first && k == 0 ? 0u : 1u);
+                for (int k = 0; k < C::KT / 32; ++k) {
+                    const int kk = half * (C::KT / 32) + k;
+                    umma_bf16_ts(tmem + 256 + i * D, tmem + i * 128 + kk * 8, proto_v | (uint64_t)(kv_addr + stage * (C::TILE >> 4) + kk * 128), idesc_o,
+                                 first && kk == 0 ? 0u : 1u);
+                }
             };
             uint32_t nq[2] = {0, 0};
             while (more && !dead) {
                 const int tiles = w.u.rows > 128 ? 2 : 1;
                 // K of the piece's first tile
                 uint32_t ks = st.idx;
-                if (!mbar_wait(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
+                if (!mbar_wait_suspended(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
                 st.next();
                 for (int i = 0; i < tiles; ++i) {
-                    if (!mbar_wait(&q_full[i], nq[i]++ & 1, abort_flag)) { dead = true; break; }
+                    if (!mbar_wait_suspended(&q_full[i], nq[i]++ & 1, abort_flag)) { dead = true; break; }
                     tc_fence_after();
                     scores(i, ks);
                 }
@@ -191,18 +240,21 @@ __global__ void __launch_bounds__(320, 1) k_paged_attn_tc(const __grid_constant_
                 for (int t = w.t; t < w.t1 && !dead; ++t) {
                     const bool last = t + 1 == w.t1;
                     const uint32_t vs = st.idx;
-                    if (!mbar_wait(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
+                    if (!mbar_wait_suspended(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
                     st.next();
                     for (int i = 0; i < tiles; ++i) {
-                        if (!mbar_wait(&p_ready[i], np[i]++ & 1, abort_flag)) { dead = true; break; }
+                        if (!mbar_wait_suspended(&p_ready[2 * i], np[i] & 1, abort_flag)) { dead = true; break; }
                         tc_fence_after();
-                        values(i, vs, t == w.t);
+                        values(i, vs, t == w.t, 0);
+                        if (!mbar_wait_suspended(&p_ready[2 * i + 1], np[i]++ & 1, abort_flag)) { dead = true; break; }
+                        tc_fence_after();
+                        values(i, vs, t == w.t, 1);
                         if (last) umma_commit(&o_full[i]);
                         if (i == tiles - 1) umma_commit(&empty[vs]);
                         if (!last) {
                             if (i == 0) {
                                 ks = st.idx;
-                                if (!mbar_wait(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
+                                if (!mbar_wait_suspended(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
                                 st.next();
                             }
                             scores(i, ks);
@@ -210,23 +262,28 @@ __global__ void __launch_bounds__(320, 1) k_paged_attn_tc(const __grid_constant_
                         }
                     }
                 }
-                ++piece;
                 more = !dead && w.next(a);
             }
             if (dead) {                                    // products in flight end before tensor memory is freed
                 umma_commit(drain);
-                mbar_wait(drain, 0, abort_flag, 1u << 20);
+                mbar_wait_suspended(drain, 0, abort_flag);
             }
         }
-    } else if (any) {
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // ================================ softmax warps: one thread per row ================================
         const int i = warp >> 2;                           // tile
         const int r = tid & 127;                           // row in the tile
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_tm = tmem + i * 128 + lanes, o_tm = tmem + 256 + i * D + lanes;
         const float c = a.scale_log2;
+        const uint64_t cc = f2_pack(c, c);
         uint32_t ns = 0, no = 0;
-        bool more = true;
+        Walk &w = walks[warp];
+        if (any) w.open(a, *share);                        // every lane writes the same
+        __syncwarp();
+        bool more = any;
         while (more) {
             const PaUnit &u = w.u;
             const int rr = i * 128 + r;                    // row in the unit
@@ -246,33 +303,36 @@ __global__ void __launch_bounds__(320, 1) k_paged_attn_tc(const __grid_constant_
                     if (lane == 0) mbar_arrive(&q_full[i]);
                 }
                 float m = -INFINITY, l = 0.f;              // reference maximum (raw score), sum of weights
-                for (int t = w.t; t < w.t1; ++t) {
+                const int t0 = w.t, t1 = w.t1;
+                for (int t = t0; t < t1; ++t) {
                     const int kt = pa_tile(u, t);
-                    if (!dead && !mbar_wait_warp(&s_full[i], ns & 1, abort_flag, lane)) dead = true;
+                    const bool edge = !pa_tile_full<C::KT>(a, u, kt);
+                    if (!dead && !mbar_wait_suspended_warp(&s_full[i], ns & 1, abort_flag)) dead = true;
                     ++ns;
                     tc_fence_after();
                     uint32_t s[4][32];
 #pragma unroll
                     for (int x = 0; x < 4; ++x) tmem_ld_32x32(s_tm + x * 32, s[x]);
                     tmem_wait_ld();
-                    if (!pa_tile_full<C::KT>(a, u, kt)) {
+                    if (edge) {
                         const int j0 = kt * C::KT;
-                        const int hi = pos - j0;                                               // last column seen
+                        const int hi = min(pos - j0, C::KT - 1);                               // last column seen
                         const int lo = a.window > 0 ? (int)max((long long)pos - a.window + 1 - j0, -1ll) : -1;   // first one, without
                         const int sink = a.window > 0 ? a.n_sink - j0 : 0;                     // the sinks
 #pragma unroll
-                        for (int x = 0; x < 4; ++x)
+                        for (int x = 0; x < 4; ++x) {
+                            // bit y: column 32 x + y is seen
+                            uint32_t see = below(hi + 1 - x * 32) & ~(below(lo - x * 32) & ~below(sink - x * 32));
 #pragma unroll
-                            for (int y = 0; y < 32; ++y) {
-                                const int col = x * 32 + y;
-                                if (col > hi || (col < lo && col >= sink)) s[x][y] = 0xff800000u;
-                            }
+                            for (int y = 0; y < 32; ++y)
+                                if (!(see & (1u << y))) s[x][y] = 0xff800000u;
+                        }
                     }
                     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int y = 0; y < 32; ++y)
+                    for (int y = 0; y < 32; y += 2)
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) mx[x] = fmaxf(mx[x], __uint_as_float(s[x][y]));
+                        for (int x = 0; x < 4; ++x) mx[x] = fmaxf(fmaxf(mx[x], __uint_as_float(s[x][y])), __uint_as_float(s[x][y + 1]));
                     const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                     float f = 1.f;
                     if ((top - m) * c > 8.f) {             // also the first maximum of a row: m is -inf
@@ -280,41 +340,53 @@ __global__ void __launch_bounds__(320, 1) k_paged_attn_tc(const __grid_constant_
                         m = top;
                         l *= f;
                     }
-                    if (t > w.t && __any_sync(0xffffffffu, f != 1.f)) {
+                    if (t > t0 && __any_sync(0xffffffffu, f != 1.f)) {
 #pragma unroll 1
-                        for (int x = 0; x < D / 32; ++x) {
-                            uint32_t o[32];
-                            tmem_ld_32x32(o_tm + x * 32, o);
+                        for (int x = 0; x < D / 16; ++x) {
+                            uint32_t o[16];
+                            tmem_ld_32x16(o_tm + x * 16, o);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int y = 0; y < 32; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * f);
-                            tmem_st_32x32(o_tm + x * 32, o);
+                            for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * f);
+                            tmem_st_32x16(o_tm + x * 16, o);
                         }
                     }
                     const float mc = m == -INFINITY ? 0.f : -m * c;
-                    float sum[2] = {0.f, 0.f};
+                    const uint64_t mm = f2_pack(mc, mc);
+                    uint64_t sum[2] = {0, 0};
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        uint32_t p[16];
+                    for (int half = 0; half < 2; ++half) {
 #pragma unroll
-                        for (int y = 0; y < 16; ++y) {
-                            const float p0 = pa_exp2(fmaf(__uint_as_float(s[x][2 * y]), c, mc));
-                            const float p1 = pa_exp2(fmaf(__uint_as_float(s[x][2 * y + 1]), c, mc));
-                            sum[0] += p0;
-                            sum[1] += p1;
-                            p[y] = pack_bf16x2(p0, p1);
+                        for (int x = 2 * half; x < 2 * half + 2; ++x) {
+                            uint32_t p[16];
+#pragma unroll
+                            for (int y = 0; y < 16; ++y) {
+                                const uint64_t e = f2_fma(f2_pack(__uint_as_float(s[x][2 * y]), __uint_as_float(s[x][2 * y + 1])), cc, mm);
+                                float p0, p1;
+                                if ((y & 3) < EMULATED) {
+                                    exp2_fma(e, p0, p1);
+                                } else {
+                                    f2_unpack(e, p0, p1);
+                                    p0 = pa_exp2(p0);
+                                    p1 = pa_exp2(p1);
+                                }
+                                sum[y & 1] = f2_add(sum[y & 1], f2_pack(p0, p1));
+                                p[y] = pack_bf16x2(p0, p1);
+                            }
+                            tmem_st_32x16(s_tm + x * 16, p);
                         }
-                        tmem_st_32x16(s_tm + x * 16, p);
+                        tmem_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&p_ready[2 * i + half]);
                     }
-                    l += sum[0] + sum[1];
-                    tmem_wait_st();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&p_ready[i]);
+                    float s0, s1;
+                    f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
+                    l += s0 + s1;
                 }
 
                 // ---- the piece's result ----
-                if (!dead && !mbar_wait_warp(&o_full[i], no & 1, abort_flag, lane)) dead = true;
+                if (!dead && !mbar_wait_suspended_warp(&o_full[i], no & 1, abort_flag)) dead = true;
                 ++no;
                 tc_fence_after();
                 __nv_bfloat16 *orow = a.out + (long long)tok * a.o_st + (long long)head * a.o_sh;
@@ -401,7 +473,10 @@ __global__ void __launch_bounds__(320, 1) k_paged_attn_tc(const __grid_constant_
                     bar_group(i);                          // last_flag is read before the next piece writes it
                 }
             }
-            more = w.next(a);
+            __syncwarp();
+            if (lane == 0) more = w.next(a);
+            __syncwarp();
+            more = __shfl_sync(0xffffffffu, more ? 1 : 0, 0) != 0;
         }
     }
     __syncwarp();

@@ -79,6 +79,37 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t *bar, uint32_t parity, v
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, fast_polls, sleep_ns)) != 0;
 }
 
+// The same bounded wait for kernels whose waiting warps share a scheduler with warps that compute: the thread is suspended
+// in the barrier unit for up to ~1 ms per poll instead of polling (a spinning warp takes issue slots: measured, the
+// exponentials of an attention tile took 1,300 cycles beside a spinning warp and 600 without one).  abort_flag as above;
+// the limit counts in units of 1,024 polls, so that it stays a few seconds.
+__device__ __forceinline__ bool mbar_wait_suspended(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
+{
+    if (mbar_try_wait(bar, parity)) return true;
+    const uint32_t limit = 1u + ((uint32_t)abort_flag[1] >> 10);
+    for (uint32_t i = 0; i < limit; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t"
+            ".reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t"
+            "}"
+            : "=r"(ok)
+            : "r"(smem_u32(bar)), "r"(parity), "r"(1000000u)
+            : "memory");
+        if (ok) return true;
+        if (abort_flag[0]) return false;
+    }
+    abort_flag[0] = 1;
+    return false;
+}
+// Warp-wide, with a warp-uniform outcome; all 32 lanes must call it.
+__device__ __forceinline__ bool mbar_wait_suspended_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
+{
+    return __all_sync(0xffffffffu, mbar_wait_suspended(bar, parity, abort_flag)) != 0;
+}
+
 // Make this thread's generic-proxy writes to shared memory visible to the async proxy (TMA, tensor cores).
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
