@@ -79,6 +79,13 @@ def lib() -> ctypes.CDLL:
             if name not in ("cb_status_string", "cb_launch_count", "cb_destroy"):
                 getattr(L, name).restype = ctypes.c_int
         L.cb_destroy.restype = None
+        p, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+        # the calls of a serving step: declared once, so that plain numbers pass without a wrapper each
+        L.cb_page_tables.argtypes = [p, p, i32, i32, p, i64, p, i64, i32, p, p, p, p, i64, p, p]
+        L.cb_paged_store.argtypes = [p, p, p, i32, i64, i64, i64, i64, p, p]
+        L.cb_rope_axes.argtypes = [p, p, i32, i32, i32, i64, i64, i64, i64, i64, i64, i64, p, i64, i32, p, i32, ctypes.c_double, i32, p]
+        L.cb_paged_attention.argtypes = [p, i32, p, i64, i64, p, i64, i64, i64, i32, p, i64, i32, p, p, i32, i32, ctypes.c_float, i32, i32,
+                                         p, ctypes.c_size_t, p]
         _lib = L
     return _lib
 
@@ -656,26 +663,24 @@ class PagePool:
         self.k, self.v = k, v
         L, N, S, H, d = k.shape
         self.c = _PagePool(k.data_ptr(), v.data_ptr(), L, H, d, S, N, strides[0], strides[1], strides[2], strides[3])
+        self.ptr = ctypes.addressof(self.c)
 
 
-def _on_one_device(stream, *tensors):
+def _on_one_device(stream, *tensors) -> int:
     """All tensors on one CUDA device, and that the current one (a launch goes to the current device); the stream handle."""
-    dev = tensors[0].device
+    dev = tensors[0].get_device()
     for t in tensors:
-        if not t.is_cuda or t.device != dev:
-            raise ValueError("all tensors of a call must be on one CUDA device")
+        if t.get_device() != dev:
+            dev = -1
+    if dev < 0:
+        raise ValueError("all tensors of a call must be on one CUDA device")
+    if dev != torch.cuda.current_device():
+        raise ValueError("the tensors' device must be the current device")
     if stream is None:
-        stream = torch.cuda.current_stream(dev)
-    if dev.index != torch.cuda.current_device() or stream.device != dev:
-        raise ValueError("the tensors' device must be the current device and the stream's")
-    return ctypes.c_void_p(stream.cuda_stream)
-
-
-def _ptr(t: torch.Tensor) -> ctypes.c_void_p:
-    return ctypes.c_void_p(t.data_ptr())
-
-
-_I64 = ctypes.c_int64
+        return torch.cuda.current_stream(dev).cuda_stream
+    if stream.device.index != dev:
+        raise ValueError("the stream must belong to the tensors' device")
+    return stream.cuda_stream
 
 
 def cb_page_tables(cached_len: torch.Tensor, new_len: torch.Tensor, page_size: int, free_pages: torch.Tensor,
@@ -683,20 +688,19 @@ def cb_page_tables(cached_len: torch.Tensor, new_len: torch.Tensor, page_size: i
                    slot_map: torch.Tensor, pages_used: Optional[torch.Tensor] = None, stream=None) -> None:
     """Block tables, slots and positions of a batch from its request lengths: device int32 tensors (slot_map int64);
     block_table [B][max_pages] is completed in place, cu_new [B + 1], total_len [B], positions and slot_map [rows]."""
-    B = cached_len.numel()
-    for t in (cached_len, new_len, free_pages, block_table, cu_new, total_len, positions):
-        assert t.dtype == torch.int32
-    for t in (cached_len, new_len, free_pages, cu_new, total_len, positions, slot_map):
-        assert t.is_contiguous()
-    assert slot_map.dtype == torch.int64 and new_len.numel() == B and total_len.numel() == B and cu_new.numel() == B + 1
-    assert block_table.dim() == 2 and block_table.shape[0] == B and (block_table.stride(1) == 1 or block_table.shape[1] <= 1)
-    assert slot_map.numel() == positions.numel()
-    assert pages_used is None or (pages_used.dtype == torch.int32 and pages_used.numel() >= 1 and pages_used.device == cu_new.device)
-    st = _on_one_device(stream, cu_new, cached_len, new_len, free_pages, block_table, total_len, positions, slot_map)
-    _check(lib().cb_page_tables(_ptr(cached_len), _ptr(new_len), B, page_size, _ptr(free_pages), _I64(free_pages.numel()),
-                                _ptr(block_table), _I64(block_table.stride(0)), block_table.shape[1], _ptr(cu_new), _ptr(total_len),
-                                _ptr(positions), _ptr(slot_map), _I64(positions.numel()),
-                                ctypes.c_void_p(0 if pages_used is None else pages_used.data_ptr()), st), "cb_page_tables")
+    B, rows = cached_len.numel(), positions.numel()
+    used = free_pages if pages_used is None else pages_used
+    for t in (cached_len, new_len, free_pages, cu_new, total_len, positions, used):
+        assert t.dtype == torch.int32 and t.is_contiguous()
+    assert slot_map.dtype == torch.int64 and slot_map.is_contiguous() and slot_map.numel() == rows
+    assert new_len.numel() == B and total_len.numel() == B and cu_new.numel() == B + 1 and (pages_used is None or used.numel() >= 1)
+    n, cols = block_table.shape
+    assert block_table.dtype == torch.int32 and n == B and (cols <= 1 or block_table.stride(1) == 1)
+    st = _on_one_device(stream, cu_new, cached_len, new_len, free_pages, block_table, total_len, positions, slot_map, used)
+    _check(lib().cb_page_tables(cached_len.data_ptr(), new_len.data_ptr(), B, page_size, free_pages.data_ptr(), free_pages.numel(),
+                                block_table.data_ptr(), block_table.stride(0), cols, cu_new.data_ptr(), total_len.data_ptr(),
+                                positions.data_ptr(), slot_map.data_ptr(), rows, None if pages_used is None else used.data_ptr(), st),
+           "cb_page_tables")
 
 
 def cb_paged_store(pool: PagePool, src_k: torch.Tensor, src_v: torch.Tensor, slot_map: torch.Tensor, stream=None) -> None:
@@ -706,10 +710,10 @@ def cb_paged_store(pool: PagePool, src_k: torch.Tensor, src_v: torch.Tensor, slo
     assert src_k.dtype == src_v.dtype and src_k.shape == src_v.shape and ss == src_v.stride() and ss[3] == 1
     assert (L, H, d) == (pool.c.n_layers, pool.c.n_heads, pool.c.head_dim)
     assert slot_map.dtype == torch.int64 and slot_map.is_contiguous() and slot_map.numel() == T
-    dt = {torch.bfloat16: CB_DTYPE_BF16, torch.float32: CB_DTYPE_F32}[src_k.dtype]
+    dt = CB_DTYPE_BF16 if src_k.dtype == torch.bfloat16 else {torch.float32: CB_DTYPE_F32}[src_k.dtype]
     st = _on_one_device(stream, pool.k, src_k, src_v, slot_map)
-    _check(lib().cb_paged_store(ctypes.byref(pool.c), _ptr(src_k), _ptr(src_v), dt, _I64(T), _I64(ss[0]), _I64(ss[1]), _I64(ss[2]),
-                                _ptr(slot_map), st), "cb_paged_store")
+    _check(lib().cb_paged_store(pool.ptr, src_k.data_ptr(), src_v.data_ptr(), dt, T, ss[0], ss[1], ss[2], slot_map.data_ptr(), st),
+           "cb_paged_store")
 
 
 def cb_rope_axes(x: torch.Tensor, out: torch.Tensor, positions: torch.Tensor, sections: Sequence[int], rope_base: float,
@@ -718,13 +722,11 @@ def cb_rope_axes(x: torch.Tensor, out: torch.Tensor, positions: torch.Tensor, se
     L, T, H, d = x.shape
     xs, os_ = x.stride(), out.stride()
     assert x.dtype == torch.bfloat16 and out.dtype == torch.bfloat16 and x.shape == out.shape and xs[3] == 1 and os_[3] == 1
-    assert positions.dtype == torch.int32 and positions.dim() == 2 and positions.shape == (len(sections), T)
-    assert positions.stride(1) == 1 or T <= 1
-    sec = (ctypes.c_int32 * len(sections))(*sections)
+    n = len(sections)
+    assert positions.dtype == torch.int32 and positions.shape == (n, T) and (T <= 1 or positions.stride(1) == 1)
     st = _on_one_device(stream, x, out, positions)
-    _check(lib().cb_rope_axes(_ptr(x), _ptr(out), L, H, d, _I64(T), _I64(xs[0]), _I64(xs[1]), _I64(xs[2]), _I64(os_[0]), _I64(os_[1]),
-                              _I64(os_[2]), _ptr(positions), _I64(positions.stride(0)), len(sections), sec, 1 if interleaved else 0,
-                              ctypes.c_double(rope_base), 1 if inverse else 0, st), "cb_rope_axes")
+    _check(lib().cb_rope_axes(x.data_ptr(), out.data_ptr(), L, H, d, T, xs[0], xs[1], xs[2], os_[0], os_[1], os_[2], positions.data_ptr(),
+                              positions.stride(0), n, (ctypes.c_int32 * n)(*sections), interleaved, rope_base, inverse, st), "cb_rope_axes")
 
 
 def cb_paged_attention_workspace_bytes(head_dim: int) -> int:
@@ -741,16 +743,14 @@ def cb_paged_attention(q: torch.Tensor, out: torch.Tensor, pool: PagePool, layer
     T, Hq, d = q.shape
     qs, os_ = q.stride(), out.stride()
     assert q.dtype == torch.bfloat16 and out.dtype == torch.bfloat16 and q.shape == out.shape and qs[2] == 1 and os_[2] == 1
-    assert d == pool.c.head_dim and block_table.dim() == 2
     B, cols = block_table.shape
-    assert block_table.dtype == torch.int32 and cu_new.dtype == torch.int32 and total_len.dtype == torch.int32
-    assert (block_table.stride(1) == 1 or cols <= 1) and cu_new.is_contiguous() and total_len.is_contiguous()
+    assert d == pool.c.head_dim and block_table.dtype == cu_new.dtype == total_len.dtype == torch.int32
+    assert (cols <= 1 or block_table.stride(1) == 1) and cu_new.is_contiguous() and total_len.is_contiguous()
     assert cu_new.numel() == B + 1 and total_len.numel() == B and workspace.dtype == torch.uint8 and workspace.is_contiguous()
     st = _on_one_device(stream, q, out, pool.k, block_table, cu_new, total_len, workspace)
-    _check(lib().cb_paged_attention(ctypes.byref(pool.c), layer, _ptr(q), _I64(qs[0]), _I64(qs[1]), _ptr(out), _I64(os_[0]), _I64(os_[1]),
-                                    _I64(T), Hq, _ptr(block_table), _I64(block_table.stride(0)), cols, _ptr(cu_new), _ptr(total_len),
-                                    B, max_new, ctypes.c_float(scale), window, n_sink, _ptr(workspace),
-                                    ctypes.c_size_t(workspace.numel()), st), "cb_paged_attention")
+    _check(lib().cb_paged_attention(pool.ptr, layer, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1], T, Hq, block_table.data_ptr(),
+                                    block_table.stride(0), cols, cu_new.data_ptr(), total_len.data_ptr(), B, max_new, scale, window, n_sink,
+                                    workspace.data_ptr(), workspace.numel(), st), "cb_paged_attention")
 
 
 def cb_device_status(ctx: Context, stream=None) -> None:

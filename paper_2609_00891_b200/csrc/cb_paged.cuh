@@ -109,14 +109,20 @@ __device__ __forceinline__ bool pa_unit(const PagedArgs &a, const int *cu, const
 }
 __device__ __forceinline__ int pa_tile(const PaUnit &u, int t) { return t < u.ns ? t : u.lo_tile + (t - u.ns); }
 
-// Every key of the tile is seen by every row of the unit.
+// The tiles [t0, t1) of the unit of which every key is seen by every row (tiles of the sinks are not counted as such).
 template <int KT>
-__device__ __forceinline__ bool pa_tile_full(const PagedArgs &a, const PaUnit &u, int kt)
+__device__ __forceinline__ void pa_full_tiles(const PagedArgs &a, const PaUnit &u, int &t0, int &t1)
 {
-    const long long j0 = (long long)kt * KT;
-    if (j0 + KT - 1 > u.p0) return false;
-    return a.window <= 0 || (long long)u.p1 - j0 < a.window || j0 + KT <= a.n_sink;
+    int k0 = 0;
+    const int k1 = u.p0 < 0 ? 0 : (u.p0 + 1) / KT;
+    if (a.window > 0) {
+        const long long lo = (long long)u.p1 - a.window + 1;      // first key that the last row sees
+        k0 = lo > 0 ? (int)((lo + KT - 1) / KT) : 0;
+    }
+    t0 = max(u.ns, k0 - u.lo_tile + u.ns);
+    t1 = k1 - u.lo_tile + u.ns;
 }
+
 // Some key of the tile at j0 is seen by no row of the unit.
 template <int KT>
 __device__ __forceinline__ bool pa_clears(const PagedArgs &a, const PaUnit &u, int j0)

@@ -160,9 +160,10 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
                 for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
             float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
+            int full0, full1;                              // tiles [full0, full1) need no mask
+            pa_full_tiles<C::KT>(a, u, full0, full1);
             for (int t = w.t; t < w.t1; ++t) {
-                const int kt = pa_tile(u, t);
-                const bool edge = !pa_tile_full<C::KT>(a, u, kt);
+                const bool edge = t < full0 || t >= full1;
                 if (!dead && !mbar_wait_suspended_warp(&full[st.idx], st.phase, abort_flag)) dead = true;
                 const uint32_t kb = smem_base + st.idx * C::STAGE, vb = kb + C::HALF;
                 float s[C::WK / 8][4];
@@ -184,7 +185,7 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
                         mma_16816(s[2 * n + 1], qf[k], b[2], b[3]);
                     }
                 }
-                const int j0 = kt * C::KT + ks * C::WK;
+                const int j0 = pa_tile(u, t) * C::KT + ks * C::WK;
                 float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
                 for (int n = 0; n < C::WK / 8; ++n)

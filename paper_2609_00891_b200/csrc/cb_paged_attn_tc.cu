@@ -45,25 +45,13 @@ __device__ __forceinline__ void bar_group(int i) { asm volatile("bar.sync %0, 12
 // Columns 0 .. n - 1 of 32 as a bit mask (n may be anything).
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
-// 2^x of a pair on the FMA pipe: x = n + f with n = round(x) by the magic-number addition, 2^f by a cubic with p(0) = 1
-// fitted to 2^f on [-1/2, 1/2] (relative error 1.0e-4 = 2^-13, a weight's rounding to bf16 is 2^-8), n added to the
-// exponent bits.  x <= 8; below -127 the result is exactly 0 (p(0) = 1 meets the exponent -127), so -inf gives 0.
-__device__ __forceinline__ void exp2_fma(uint64_t x, float &p0, float &p1)
+// Largest of three (one instruction on sm_100).
+__device__ __forceinline__ float max3(float x, float y, float z)
 {
-    float x0, x1, n0, n1;
-    f2_unpack(x, x0, x1);
-    x = f2_pack(fmaxf(x0, -127.f), fmaxf(x1, -127.f));
-    const uint64_t n = f2_add(x, f2_pack(12582912.f, 12582912.f));
-    const uint64_t f = f2_fma(f2_add(n, f2_pack(-12582912.f, -12582912.f)), f2_pack(-1.f, -1.f), x);
-    uint64_t p = f2_fma(f, f2_pack(0.0550089292f, 0.0550089292f), f2_pack(0.242210969f, 0.242210969f));
-    p = f2_fma(p, f, f2_pack(0.693282902f, 0.693282902f));
-    p = f2_fma(p, f, f2_pack(1.f, 1.f));
-    f2_unpack(p, p0, p1);
-    f2_unpack(n, n0, n1);
-    p0 = __int_as_float(__float_as_int(p0) + (__float_as_int(n0) << 23));
-    p1 = __int_as_float(__float_as_int(p1) + (__float_as_int(n1) << 23));
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    return r;
 }
-constexpr int EMULATED = 1;       // of every four pairs of a row
 
 template <int D>
 __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant__ TcAttnParams P)
@@ -304,9 +292,9 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                 }
                 float m = -INFINITY, l = 0.f;              // reference maximum (raw score), sum of weights
                 const int t0 = w.t, t1 = w.t1;
+                int full0, full1;                          // tiles [full0, full1) need no mask
+                pa_full_tiles<C::KT>(a, u, full0, full1);
                 for (int t = t0; t < t1; ++t) {
-                    const int kt = pa_tile(u, t);
-                    const bool edge = !pa_tile_full<C::KT>(a, u, kt);
                     if (!dead && !mbar_wait_suspended_warp(&s_full[i], ns & 1, abort_flag)) dead = true;
                     ++ns;
                     tc_fence_after();
@@ -314,8 +302,8 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
 #pragma unroll
                     for (int x = 0; x < 4; ++x) tmem_ld_32x32(s_tm + x * 32, s[x]);
                     tmem_wait_ld();
-                    if (edge) {
-                        const int j0 = kt * C::KT;
+                    if (t < full0 || t >= full1) {
+                        const int j0 = pa_tile(u, t) * C::KT;
                         const int hi = min(pos - j0, C::KT - 1);                               // last column seen
                         const int lo = a.window > 0 ? (int)max((long long)pos - a.window + 1 - j0, -1ll) : -1;   // first one, without
                         const int sink = a.window > 0 ? a.n_sink - j0 : 0;                     // the sinks
@@ -332,7 +320,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
 #pragma unroll
                     for (int y = 0; y < 32; y += 2)
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) mx[x] = fmaxf(fmaxf(mx[x], __uint_as_float(s[x][y])), __uint_as_float(s[x][y + 1]));
+                        for (int x = 0; x < 4; ++x) mx[x] = max3(mx[x], __uint_as_float(s[x][y]), __uint_as_float(s[x][y + 1]));
                     const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                     float f = 1.f;
                     if ((top - m) * c > 8.f) {             // also the first maximum of a row: m is -inf
@@ -363,13 +351,9 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                             for (int y = 0; y < 16; ++y) {
                                 const uint64_t e = f2_fma(f2_pack(__uint_as_float(s[x][2 * y]), __uint_as_float(s[x][2 * y + 1])), cc, mm);
                                 float p0, p1;
-                                if ((y & 3) < EMULATED) {
-                                    exp2_fma(e, p0, p1);
-                                } else {
-                                    f2_unpack(e, p0, p1);
-                                    p0 = pa_exp2(p0);
-                                    p1 = pa_exp2(p1);
-                                }
+                                f2_unpack(e, p0, p1);
+                                p0 = pa_exp2(p0);
+                                p1 = pa_exp2(p1);
                                 sum[y & 1] = f2_add(sum[y & 1], f2_pack(p0, p1));
                                 p[y] = pack_bf16x2(p0, p1);
                             }
