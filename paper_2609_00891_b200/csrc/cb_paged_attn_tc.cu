@@ -184,77 +184,93 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
             }
         }
     } else if (warp == 9) {
-        // ================================ MMA issuer (one thread) ================================
-        if (lane == 0 && any) {
+        // ================================ MMA issuer ================================
+        // The whole warp walks and one elected lane issues (see elect_one).
+        if (any) {
             constexpr uint32_t idesc_s = umma_idesc_bf16(128, C::KT, false, false);   // both K-major
             constexpr uint32_t idesc_o = umma_idesc_bf16(128, D, false, true);        // V: MN-major
             const uint64_t proto_k = umma_smem_desc_sw128(0, 16, 1024);
             const uint64_t proto_v = umma_smem_desc_sw128(0, C::BLK, 1024);
             const uint32_t q_addr = (smem_u32(qs) & 0x3FFFFu) >> 4, kv_addr = (smem_u32(kv) & 0x3FFFFu) >> 4;
+            const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+            const bool leader = elect_one();
             Ring<C::NS> st;
-            uint32_t np[2] = {0, 0};
+            uint32_t nq[2] = {0, 0}, np[2] = {0, 0};
             bool more = true;
             auto scores = [&](int i, uint32_t stage) {
+                const uint64_t qd = proto_k | (uint64_t)(q_addr + i * (C::TILE >> 4));
+                const uint64_t kd = proto_k | (uint64_t)(kv_addr + __shfl_sync(0xffffffffu, stage, 0) * (C::TILE >> 4));
+                if (leader) {
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t off = (k >> 2) * (C::BLK >> 4) + (k & 3) * 2;
-                    umma_bf16_ss(tmem + i * 128, proto_k | (uint64_t)(q_addr + i * (C::TILE >> 4) + off),
-                                 proto_k | (uint64_t)(kv_addr + stage * (C::TILE >> 4) + off), idesc_s, k == 0 ? 0u : 1u);
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t off = (k >> 2) * (C::BLK >> 4) + (k & 3) * 2;
+                        umma_bf16_ss(tm + i * 128, qd + off, kd + off, idesc_s, k == 0 ? 0u : 1u);
+                    }
+                    umma_commit(&s_full[i]);
                 }
-                umma_commit(&s_full[i]);
+                __syncwarp();
             };
-            auto values = [&](int i, uint32_t stage, bool first, int half) {
+            // 64 keys of the tile; `first`: nothing is in the output yet
+            auto values = [&](int i, uint32_t stage, int half, uint32_t first) {
+                const uint64_t vd = proto_v | (uint64_t)(kv_addr + __shfl_sync(0xffffffffu, stage, 0) * (C::TILE >> 4));
+                if (leader) {
 #pragma unroll
-                for (int k = 0; k < C::KT / 32; ++k) {
-                    const int kk = half * (C::KT / 32) + k;
-                    umma_bf16_ts(tmem + 256 + i * D, tmem + i * 128 + kk * 8, proto_v | (uint64_t)(kv_addr + stage * (C::TILE >> 4) + kk * 128), idesc_o,
-                                 first && kk == 0 ? 0u : 1u);
+                    for (int k = 4 * half; k < 4 * half + 4; ++k)
+                        umma_bf16_ts(tm + 256 + i * D, tm + i * 128 + k * 8, vd + k * 128, idesc_o, k == 0 ? 1u - first : 1u);
                 }
+                __syncwarp();
             };
-            uint32_t nq[2] = {0, 0};
+            auto commit = [&](uint64_t *bar) {
+                if (leader) umma_commit(bar);
+                __syncwarp();
+            };
             while (more && !dead) {
                 const int tiles = w.u.rows > 128 ? 2 : 1;
                 // K of the piece's first tile
                 uint32_t ks = st.idx;
-                if (!mbar_wait_suspended(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
+                if (!mbar_wait_suspended_warp(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
                 st.next();
-                for (int i = 0; i < tiles; ++i) {
-                    if (!mbar_wait_suspended(&q_full[i], nq[i]++ & 1, abort_flag)) { dead = true; break; }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (i >= tiles || dead) break;
+                    if (!mbar_wait_suspended_warp(&q_full[i], nq[i]++ & 1, abort_flag)) { dead = true; break; }
                     tc_fence_after();
                     scores(i, ks);
                 }
                 if (dead) break;
-                umma_commit(&empty[ks]);
+                commit(&empty[ks]);
                 for (int t = w.t; t < w.t1 && !dead; ++t) {
                     const bool last = t + 1 == w.t1;
                     const uint32_t vs = st.idx;
-                    if (!mbar_wait_suspended(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
+                    if (!mbar_wait_suspended_warp(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
                     st.next();
-                    for (int i = 0; i < tiles; ++i) {
-                        if (!mbar_wait_suspended(&p_ready[2 * i], np[i] & 1, abort_flag)) { dead = true; break; }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if (i >= tiles || dead) break;
+                        if (!mbar_wait_suspended_warp(&p_ready[2 * i], np[i] & 1, abort_flag)) { dead = true; break; }
                         tc_fence_after();
-                        values(i, vs, t == w.t, 0);
-                        if (!mbar_wait_suspended(&p_ready[2 * i + 1], np[i]++ & 1, abort_flag)) { dead = true; break; }
+                        values(i, vs, 0, t == w.t ? 1u : 0u);
+                        if (!mbar_wait_suspended_warp(&p_ready[2 * i + 1], np[i]++ & 1, abort_flag)) { dead = true; break; }
                         tc_fence_after();
-                        values(i, vs, t == w.t, 1);
-                        if (last) umma_commit(&o_full[i]);
-                        if (i == tiles - 1) umma_commit(&empty[vs]);
+                        values(i, vs, 1, 0);
+                        if (last) commit(&o_full[i]);
+                        if (i == tiles - 1) commit(&empty[vs]);
                         if (!last) {
                             if (i == 0) {
                                 ks = st.idx;
-                                if (!mbar_wait_suspended(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
+                                if (!mbar_wait_suspended_warp(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
                                 st.next();
                             }
                             scores(i, ks);
-                            if (i == tiles - 1) umma_commit(&empty[ks]);
+                            if (i == tiles - 1) commit(&empty[ks]);
                         }
                     }
                 }
                 more = !dead && w.next(a);
             }
             if (dead) {                                    // products in flight end before tensor memory is freed
-                umma_commit(drain);
-                mbar_wait_suspended(drain, 0, abort_flag);
+                commit(drain);
+                mbar_wait_suspended_warp(drain, 0, abort_flag);
             }
         }
     }

@@ -11,6 +11,16 @@ namespace ptx {
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
+// True in one lane of a converged warp, always the same one.  The compiler keeps the operands of what follows under it in
+// uniform registers when they are warp-uniform; under `lane == 0` it moves them there one by one for every instruction,
+// which, beside busy warps, made a tcgen05.mma take 80 cycles to issue instead of the 48 to 64 it runs for (measured).
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+    return ok != 0;
+}
+
 // ---- mbarrier ----------------------------------------------------------------------------------------
 __device__ __forceinline__ void mbar_init(uint64_t *bar, uint32_t count)
 {
