@@ -497,7 +497,8 @@ cb_status cb_rope_axes(const void *x, void *out, int32_t n_layers, int32_t n_hea
 
 /*
  * Attention of new rows over one layer of a paged cache.  Request b owns rows [cu_new[b], cu_new[b+1]) of q and out
- * (bf16, row t of query head h at t*stride_token + h*stride_head, multiples of 8, 16-byte aligned); they are the LAST
+ * (bf16, row t of query head h at t*stride_token + h*stride_head, multiples of 8, a stride of 0 only on a dimension of
+ * size 1, 16-byte aligned; q and out must not overlap); they are the LAST
  * rows of its total_len[b] rows in the cache (their own keys and values are stored already), so row i of the request has
  * position p = total_len - new + i, and
  *     out = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale q . k_j)   over the keys j <= p with

@@ -536,6 +536,21 @@ static PFN_cuTensorMapEncodeTiled_v12000 encode_fn()
 // 5-D map over (64 channels, token, 64-channel block, head, layer).  One box = box_tokens tokens of one head of
 // one layer, laid out in shared memory as [channel block][token][64 channels] with the 128-byte swizzle.
 // box_cblocks: 64-channel blocks per box (0: all d / 64 of them; 1: one block, selected by the copy's third coordinate).
+bool make_q_tensor_map(CUtensorMap *map, const void *base, int d, int H, long long T, long long sh, long long st, int box_heads,
+                       int box_tokens)
+{
+    PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
+    if (!enc) return false;
+    auto stride = [&](long long elems, long long size) -> cuuint64_t {
+        return (size == 1 || elems == 0) ? (cuuint64_t)d * 2 : (cuuint64_t)elems * 2;   // size-1 dimension: any valid stride
+    };
+    cuuint64_t gdim[4] = {64, (cuuint64_t)H, (cuuint64_t)T, (cuuint64_t)(d / 64)};
+    cuuint64_t gstr[3] = {stride(sh, H), stride(st, T), 128};
+    cuuint32_t box[4] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens, 1}, estr[4] = {1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool make_kv_tensor_map(CUtensorMap *map, const void *base, int d, int H, long long T, int L,
                         long long sh, long long st, long long sl, int box_tokens, int box_cblocks)
 {

@@ -141,6 +141,11 @@ void count_launch(int n = 1);
 bool make_kv_tensor_map(CUtensorMap *map, const void *base, int d, int H, long long T, int L,
                         long long sh, long long st, long long sl, int box_tokens, int box_cblocks = 0);
 
+// 4-D tensor map over (64 channels, head, token, 64-channel block) of strided bf16 query rows: one box = 64 channels of
+// box_heads heads of box_tokens tokens, in shared memory as [token][head][64 channels] with the 128-byte swizzle.
+bool make_q_tensor_map(CUtensorMap *map, const void *base, int d, int H, long long T, long long sh, long long st, int box_heads,
+                       int box_tokens);
+
 // Host-side argument checks shared by the entry points (status codes of the C ABI).
 cb_status check_problem(const cb_problem *p);
 cb_status check_view(const cb_kv_view *v, int L, int H, int d);

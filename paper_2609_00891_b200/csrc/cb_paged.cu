@@ -159,7 +159,8 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
     if (n_q_heads % pool->n_heads || !(scale > 0.f) || !std::isfinite(scale)) return CB_ERR_INVALID_ARG;
     if (q_stride_token < 0 || q_stride_head < 0 || o_stride_token < 0 || o_stride_head < 0) return CB_ERR_INVALID_ARG;
     if ((q_stride_token | q_stride_head | o_stride_token | o_stride_head) & 7) return CB_ERR_INVALID_ARG;
-    if ((n_rows > 1 && o_stride_token == 0) || (n_q_heads > 1 && o_stride_head == 0)) return CB_ERR_UNSUPPORTED;
+    if ((n_rows > 1 && (o_stride_token == 0 || q_stride_token == 0)) || (n_q_heads > 1 && (o_stride_head == 0 || q_stride_head == 0))) return CB_ERR_UNSUPPORTED;
+    if (q_stride_token >= (1ll << 39) || q_stride_head >= (1ll << 39)) return CB_ERR_UNSUPPORTED;
     // flattened rows and units are counted in 32 bits
     if (n_rows >= (1ll << 31) || n_rows * n_q_heads + n_requests >= (1ll << 31)) return CB_ERR_UNSUPPORTED;
     if (n_requests > 1 && table_stride < max_pages) return CB_ERR_INVALID_ARG;
@@ -176,6 +177,15 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
     a.table = block_table; a.table_stride = table_stride; a.table_cols = max_pages;
     a.cu = cu_new; a.total = total_len; a.n_requests = n_requests; a.n_rows = (int)n_rows;
     a.Hkv = pool->n_heads; a.group = n_q_heads / pool->n_heads;
+    // n / d == mulhi(n, ceil(2^32 / d)) as long as n (d - 1) < 2^32
+    auto reciprocal = [](int64_t d, int64_t most) {
+        return d > 1 && (unsigned __int128)most * d < ((unsigned __int128)1 << 32) ? (unsigned)(((1ull << 32) + d - 1) / d) : 0u;
+    };
+    a.group_mul = reciprocal(a.group, n_rows * a.group);
+    // tensor-core kernel: a tile of 128 rows holds whole tokens, so that one copy brings it
+    a.unit_tokens = a.group <= 128 ? 2 * (128 / a.group) : 1;
+    a.unit_rows = a.unit_tokens * a.group;
+    a.unit_mul = reciprocal(a.unit_tokens, n_rows + a.unit_tokens);
     a.page_log2 = page_log2_of(pool->page_size);
     a.n_pages = (int)pool->n_pages;
     a.window = window; a.n_sink = window > 0 ? n_sink : 0;
@@ -188,8 +198,9 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
     if (max_new == 0 || max_new > n_rows) max_new = (int32_t)n_rows;
     const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(pool->k) + layer * pool->stride_layer;
     const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(pool->v) + layer * pool->stride_layer;
-    // up to 64 flattened rows per request and KV head: the warp-level kernel, which reads K and V at their bandwidth
-    const bool few = (long long)max_new * a.group <= 64;
+    // up to 64 flattened rows per request and KV head: the warp-level kernel, which reads K and V at their bandwidth (and
+    // more than 128 query heads per KV head, which do not fit a tile)
+    const bool few = (long long)max_new * a.group <= 64 || a.group > 128;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const cudaError_t e = few ? launch_paged_attn_few(a, pool->head_dim, k, v, pool->page_size, pool->stride_page, pool->stride_slot, pool->stride_head, max_new, st)
                               : launch_paged_attn_tc(a, pool->head_dim, k, v, pool->page_size, pool->stride_page, pool->stride_slot, pool->stride_head, st);

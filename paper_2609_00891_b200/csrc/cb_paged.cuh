@@ -25,6 +25,9 @@ struct PagedArgs {
     const int *total;                        // device [n_requests]: rows in the cache, the new ones included
     int n_requests, n_rows;                  // n_rows: rows of q and out
     int Hkv, group;
+    unsigned group_mul;                      // ceil(2^32 / group) where that divides every row index exactly, else 0
+    int unit_tokens, unit_rows;              // tensor-core kernel: new rows of a unit, and flattened
+    unsigned unit_mul;                       // as group_mul, for unit_tokens
     int page_log2;
     int n_pages;
     int window, n_sink;                      // window 0: none
@@ -65,6 +68,26 @@ cudaError_t launch_rope_axes(const void *x, void *out, int L, int H, int d, long
                              double base, int inverse, cudaStream_t st);
 
 #ifdef __CUDACC__
+// Flattened row -> row of the request (n / group): an integer division is ~30 dependent instructions, and several of them
+// stand between the launch and the first copy.
+__device__ __forceinline__ int pa_token(const PagedArgs &a, int n)
+{
+    return a.group_mul ? (int)__umulhi((unsigned)n, a.group_mul) : a.group == 1 ? n : n / a.group;
+}
+// Quotient of two non-negative numbers, in 32 bits where both fit.
+__device__ __forceinline__ long long pa_div(long long n, long long d)
+{
+    return ((n | d) >> 32) == 0 ? (long long)((unsigned)n / (unsigned)d) : n / d;
+}
+
+// The unit at or before request row n, of units counted from row 0; ROWS flattened rows a unit, or a.unit_tokens rows (0).
+template <int ROWS>
+__device__ __forceinline__ int pa_unit_of(const PagedArgs &a, int n)
+{
+    if (ROWS) return (int)((unsigned)n * (unsigned)a.group / (ROWS ? ROWS : 1));
+    return a.unit_mul ? (int)__umulhi((unsigned)n, a.unit_mul) : n / a.unit_tokens;
+}
+
 // One unit's place in the batch and its key tiles of KT keys.
 struct PaUnit {
     int b, qt, nq;          // request, row block, row blocks of the request
@@ -84,15 +107,16 @@ __device__ __forceinline__ bool pa_unit(const PagedArgs &a, const int *cu, const
     const int all = fresh * a.group;
     u.b = b;
     u.qt = qt;
-    u.nq = (all + ROWS - 1) / ROWS;
+    const int per = ROWS ? ROWS : a.unit_rows;
+    u.nq = ROWS ? (all + ROWS - 1) / (ROWS ? ROWS : 1) : pa_unit_of<0>(a, max(fresh, 0) + a.unit_tokens - 1);
     if (qt >= u.nq) { u.n = 0; return false; }
     u.tok0 = c0;
-    u.row0 = qt * ROWS;
-    u.rows = min(ROWS, all - u.row0);
+    u.row0 = qt * per;
+    u.rows = min(per, all - u.row0);
     const int len = max(total[b], 0);
     u.base = len - fresh;
-    u.p0 = u.base + u.row0 / a.group;
-    u.p1 = u.base + (u.row0 + u.rows - 1) / a.group;
+    u.p0 = u.base + pa_token(a, u.row0);
+    u.p1 = u.base + pa_token(a, u.row0 + u.rows - 1);
     u.hi_key = max(0, u.p1 + 1);
     const int hi_tile = (u.hi_key + KT - 1) / KT;
     u.lo_key = 0;
@@ -123,6 +147,11 @@ __device__ __forceinline__ void pa_full_tiles(const PagedArgs &a, const PaUnit &
     t1 = k1 - u.lo_tile + u.ns;
 }
 
+// Some key in [key, key + n) is seen by some row of the unit.
+__device__ __forceinline__ bool pa_wanted(const PagedArgs &a, const PaUnit &u, int key, int n)
+{
+    return key < u.hi_key && (key + n > u.lo_key || key < a.n_sink);
+}
 // Some key of the tile at j0 is seen by no row of the unit.
 template <int KT>
 __device__ __forceinline__ bool pa_clears(const PagedArgs &a, const PaUnit &u, int j0)
@@ -139,14 +168,20 @@ struct PaShare {
     long long begin, end;    // tiles of this block
     long long q;             // tiles per block
     long long unit_begin;    // where the first unit's tiles begin
-    int b, qt;               // the first unit
+    PaUnit u;                // the first unit
+    int even;                // > 0: every pair takes this many places on the line, and no pair is split
 };
 
 // All threads of the block.  `staged`: shared memory for the lengths (cap ints), free until the first tile is copied.
-// Each thread counts the tiles of a run of consecutive units; one scan gives the line, one thread finds the block's start.
+// `sums`: [3 x warps].  Each thread counts the tiles of a run of consecutive units; one scan gives the line, one thread
+// finds the block's start.
+// Where there are no more pairs than blocks and the longest one is at most EVEN tiles above an equal share, every pair goes
+// to a block of its own: joining two parts costs about that much (32 requests with a window of 1,024 keys, 256 pairs of 17
+// or 18 tiles of 64 keys: 38 us split, see k_paged_attn_few).
 template <int ROWS, int KT, int THREADS>
-__device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int cap, PaShare *share, long long *warp_sums)
+__device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int cap, PaShare *share, long long *sums)
 {
+    constexpr int EVEN = 4;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     constexpr int NWARP = THREADS / 32;
     const int *cu = a.cu, *total = a.total;
@@ -159,8 +194,10 @@ __device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int
     }
     if (tid == 0) { share->begin = 0; share->end = 0; }
     __syncthreads();
-    // block of unit index u: the last request b with floor(cu[b] group / ROWS) + b <= u (some indices are no unit)
-    const int n_units = (int)((long long)a.n_rows * a.group / ROWS) + B;
+    // unit index u: the last request b with floor(cu[b] group / ROWS) + b <= u (some indices are no unit); 32 bits hold
+    // rows * query heads, checked by the host
+    auto first_unit = [&](int b) { return pa_unit_of<ROWS>(a, max(cu[b], 0)) + b; };
+    const int n_units = pa_unit_of<ROWS>(a, a.n_rows) + B;
     const int per = (n_units + THREADS - 1) / THREADS;
     const int u0 = min(n_units, tid * per), u1 = min(n_units, u0 + per);
     int b0 = 0;
@@ -168,55 +205,72 @@ __device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int
         int lo = 0, hi = B - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if ((int)((long long)cu[mid] * a.group / ROWS) + mid <= u0) lo = mid; else hi = mid - 1;
+            if (first_unit(mid) <= u0) lo = mid; else hi = mid - 1;
         }
         b0 = lo;
     }
     PaUnit un;
     long long mine = 0;
+    int count = 0, most = 0;                     // units of this thread, tiles of the longest
     {
         int b = b0;
         for (int u = u0; u < u1; ++u) {
-            while (b + 1 < B && (int)((long long)cu[b + 1] * a.group / ROWS) + b + 1 <= u) ++b;
-            const int qt = u - ((int)((long long)cu[b] * a.group / ROWS) + b);
-            if (pa_unit<ROWS, KT>(a, cu, total, b, qt, un)) mine += un.n;
+            while (b + 1 < B && first_unit(b + 1) <= u) ++b;
+            if (pa_unit<ROWS, KT>(a, cu, total, b, u - first_unit(b), un)) { mine += un.n; ++count; most = max(most, un.n); }
         }
     }
     long long incl = mine;
+    int incl_units = count;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const long long up = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += up;
+        const int upu = __shfl_up_sync(0xffffffffu, incl_units, o);
+        if (lane >= o) { incl += up; incl_units += upu; }
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
     }
-    if (lane == 31) warp_sums[warp] = incl;
+    if (lane == 31) { sums[warp] = incl; sums[NWARP + warp] = incl_units; sums[2 * NWARP + warp] = most; }
     __syncthreads();
     long long before = 0, all = 0;
+    int before_units = 0, all_units = 0;
+    most = 0;
+#pragma unroll
     for (int w = 0; w < NWARP; ++w) {
-        const long long s = warp_sums[w];
-        if (w < warp) before += s;
+        const long long s = sums[w];
+        const int su = (int)sums[NWARP + w];
+        if (w < warp) { before += s; before_units += su; }
         all += s;
+        all_units += su;
+        most = max(most, (int)sums[2 * NWARP + w]);
     }
-    const long long line = all * a.Hkv;
-    long long q = (line + gridDim.x - 1) / gridDim.x;
+    long long line = all * a.Hkv;
+    long long q = pa_div(line + gridDim.x - 1, gridDim.x);
     if (q < a.q_min) q = a.q_min;
-    const long long begin = (long long)blockIdx.x * q;
     long long pre = (before + incl - mine) * a.Hkv;
+    int even = 0;
+    if ((long long)all_units * a.Hkv <= gridDim.x && most <= q + EVEN && most > 0) {
+        even = most;
+        q = most;
+        line = (long long)all_units * a.Hkv * q;
+        pre = (long long)(before_units + incl_units - count) * a.Hkv * q;
+        mine = (long long)count * even;
+    }
+    const long long begin = (long long)blockIdx.x * q;
     if (begin < line && begin >= pre && begin < pre + mine * a.Hkv) {
         int b = b0;
         for (int u = u0; u < u1; ++u) {
-            while (b + 1 < B && (int)((long long)cu[b + 1] * a.group / ROWS) + b + 1 <= u) ++b;
-            const int qt = u - ((int)((long long)cu[b] * a.group / ROWS) + b);
-            if (!pa_unit<ROWS, KT>(a, cu, total, b, qt, un)) continue;
-            if (begin < pre + (long long)un.n * a.Hkv) {
-                share->b = b;
-                share->qt = qt;
+            while (b + 1 < B && first_unit(b + 1) <= u) ++b;
+            if (!pa_unit<ROWS, KT>(a, cu, total, b, u - first_unit(b), un)) continue;
+            const long long len = (long long)(even ? even : un.n) * a.Hkv;
+            if (begin < pre + len) {
+                share->u = un;
                 share->unit_begin = pre;
                 share->q = q;
                 share->begin = begin;
                 share->end = begin + q < line ? begin + q : line;
+                share->even = even;
                 break;
             }
-            pre += (long long)un.n * a.Hkv;
+            pre += len;
         }
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the staged lengths' memory goes to the copies next
@@ -228,18 +282,20 @@ template <int ROWS, int KT>
 struct PaWalk {
     PaUnit u;
     int h, t, t1;            // KV head, tiles [t, t1) of the unit
+    int len, even;           // places of the pair on the line
     long long at, end, q;    // position on the line
-    long long pair_begin;    // where the tiles of (unit, h) begin
+    long long pair_begin;    // where the places of (unit, h) begin
     __device__ __forceinline__ bool open(const PagedArgs &a, const PaShare &s)
     {
         at = s.begin;
         end = s.end;
         q = s.q;
+        even = s.even;
         if (at >= end) return false;
-        pa_unit<ROWS, KT>(a, a.cu, a.total, s.b, s.qt, u);
-        const long long off = at - s.unit_begin;
-        h = (int)(off / u.n);
-        pair_begin = s.unit_begin + (long long)h * u.n;
+        u = s.u;
+        len = even ? even : u.n;
+        h = (int)pa_div(at - s.unit_begin, len);
+        pair_begin = s.unit_begin + (long long)h * len;
         piece();
         return true;
     }
@@ -250,25 +306,26 @@ struct PaWalk {
     }
     __device__ __forceinline__ bool next(const PagedArgs &a)
     {
-        at += t1 - t;
+        at = pair_begin + len;
         if (at >= end) return false;
-        pair_begin += u.n;
+        pair_begin += len;
         if (++h == a.Hkv) {
             h = 0;
             int b = u.b, qt = u.qt + 1;
             if (qt >= u.nq) {
                 qt = 0;
-                do { ++b; } while (b < a.n_requests && a.cu[b + 1] == a.cu[b]);
+                do { ++b; } while (b < a.n_requests && a.cu[b + 1] <= a.cu[b]);
                 if (b >= a.n_requests) return false;
             }
             pa_unit<ROWS, KT>(a, a.cu, a.total, b, qt, u);
+            len = even ? even : u.n;
         }
         piece();
         return true;
     }
     __device__ __forceinline__ bool whole() const { return t == 0 && t1 == u.n; }
-    __device__ __forceinline__ int first_block() const { return (int)(pair_begin / q); }
-    __device__ __forceinline__ int last_block() const { return (int)((pair_begin + u.n - 1) / q); }
+    __device__ __forceinline__ int first_block() const { return (int)pa_div(pair_begin, q); }
+    __device__ __forceinline__ int last_block() const { return (int)pa_div(pair_begin + len - 1, q); }
     // Record of block c's part of this pair: a block has at most one part that began before it and one that ends after it.
     __device__ __forceinline__ int record(int c) const { return 2 * c + (pair_begin <= (long long)c * q ? 0 : 1); }
 };

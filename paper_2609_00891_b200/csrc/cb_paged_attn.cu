@@ -31,9 +31,13 @@ struct FewCfg {
     static constexpr int STAGE = 2 * HALF;
     static constexpr int NS = D == 128 ? 3 : 6;
     static constexpr int THREADS = 160;
-    static constexpr int RED_PITCH = 36;               // floats per row of the join buffer (32 + 4: no bank conflict)
-    static constexpr int RED_BYTES = 4 * 16 * RED_PITCH * 4;
-    static constexpr size_t SMEM = 1024 + (size_t)NS * STAGE + RED_BYTES + 4 * 16 * 2 * 4 + 1024;
+    static constexpr int PITCH = D / KS + 8;           // floats per row of the join buffer
+    static constexpr int RED_BYTES = 4 * (KS - 1) * 8 * PITCH * 4;   // [row tile][share][the other warps' parts][8 rows]
+    __device__ static constexpr int part(int mt, int share, int from)
+    {
+        return ((mt * KS + share) * (KS - 1) + (from < share ? from : from - 1)) * 8 * PITCH;
+    }
+    static constexpr size_t SMEM = 1024 + (size_t)NS * STAGE + RED_BYTES + 4 * 16 * 2 * 4 + 512;
     static constexpr int REC = ROWS * (D + 2);         // floats of a partial record: output rows, maxima, sums
 };
 
@@ -67,7 +71,7 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
     uint64_t *full = reinterpret_cast<uint64_t *>(stat_l + 64);
     uint64_t *empty = full + C::NS;
     long long *warp_sums = reinterpret_cast<long long *>(empty + C::NS);
-    PaShare *share = reinterpret_cast<PaShare *>(warp_sums + 8);
+    PaShare *share = reinterpret_cast<PaShare *>(warp_sums + 16);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(share + 1);
     volatile int *last_flag = abort_flag + 2;
 
@@ -102,7 +106,7 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
                 for (int t = w.t; t < w.t1; ++t) {
                     const int key = pa_tile(w.u, t) * C::KT + (i << box_log2);
                     int page = a.n_pages;                        // outside the pool: the copy writes zeros
-                    if (lane < n_box && key < w.u.hi_key) {
+                    if (lane < n_box && pa_wanted(a, w.u, key, 1 << box_log2)) {
                         const int col = key >> a.page_log2;
                         if (col < a.table_cols) page = __ldg(row + col);
                     }
@@ -143,10 +147,10 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
             for (int e = 0; e < 2; ++e) {
                 const int r = mt * 16 + g + e * 8;
                 const int fr = u.row0 + r;
-                const int tok = fr / a.group;
+                const int tok = pa_token(a, fr);
                 live[e] = r < u.rows && (unsigned)(u.tok0 + tok) < (unsigned)a.n_rows;
                 pos[e] = live[e] ? u.base + tok : -1;
-                const __nv_bfloat16 *qp = a.q + (long long)(u.tok0 + tok) * a.q_st + (long long)(w.h * a.group + fr % a.group) * a.q_sh + c2;
+                const __nv_bfloat16 *qp = a.q + (long long)(u.tok0 + tok) * a.q_st + (long long)(w.h * a.group + fr - tok * a.group) * a.q_sh + c2;
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     qf[k][e] = live[e] ? *reinterpret_cast<const uint32_t *>(qp + k * 16) : 0u;
@@ -258,108 +262,136 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
             }
 
             // ---- the piece's result: join the key groups, then write the rows or a partial record ----
+            // Every warp takes a quarter of the channels (all of its own rows' channels where it has no partners): it adds
+            // what its partners left in shared memory to its own registers, each part scaled from its own maximum.
             const bool whole = w.whole();
-            const int rec = w.record(blockIdx.x);
-            float *prec = a.part + (size_t)rec * C::REC;
+            float *prec = a.part + (size_t)w.record(blockIdx.x) * C::REC;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 l[e] += __shfl_xor_sync(0xffffffffu, l[e], 1);
                 l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
             }
-            if ((lane & 3) == 0) {
+            constexpr int SN = D / 8 / C::KS;                 // 8-channel groups of a warp's share
+            float mj[2], lj[2], sc[2][C::KS];
+            if (C::KS > 1) {
+                if ((lane & 3) == 0) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    stat_m[warp * 16 + g + e * 8] = m[e];
-                    stat_l[warp * 16 + g + e * 8] = l[e];
+                    for (int e = 0; e < 2; ++e) {
+                        stat_m[warp * 16 + g + e * 8] = m[e];
+                        stat_l[warp * 16 + g + e * 8] = l[e];
+                    }
                 }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) { mj[e] = m[e]; lj[e] = l[e]; sc[e][0] = 1.f; }
             }
-            bar_consumers();
-            float mj[2], lj[2], sc[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                mj[e] = -INFINITY;
-                for (int k = 0; k < C::KS; ++k) mj[e] = fmaxf(mj[e], stat_m[(mt * C::KS + k) * 16 + g + e * 8]);
-                const float ref = mj[e] == -INFINITY ? 0.f : mj[e];
-                lj[e] = 0.f;
-                for (int k = 0; k < C::KS; ++k)
-                    lj[e] += stat_l[(mt * C::KS + k) * 16 + g + e * 8] * pa_exp2(stat_m[(mt * C::KS + k) * 16 + g + e * 8] - ref);
-                sc[e] = pa_exp2(m[e] - ref);
-                if (whole) sc[e] = lj[e] > 0.f ? sc[e] / lj[e] : (lj[e] == 0.f ? 0.f : lj[e]);   // NaN stays NaN
-            }
-            if (!whole && ks == 0 && (lane & 3) == 0) {
+                // rows g and g + 8 in turn: with up to 8 flattened rows (decode with 8 query heads a KV head) one turn does
+                if (e == 1 && u.rows <= 8) break;
+                if (C::KS > 1) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int r = mt * 16 + g + e * 8;
-                    if (r < u.rows) {
-                        prec[C::ROWS * D + r] = mj[e];
-                        prec[C::ROWS * D + C::ROWS + r] = lj[e];
-                    }
-                }
-            }
+                    for (int s = 0; s < C::KS; ++s)
+                        if (s != ks) {
 #pragma unroll
-            for (int cc = 0; cc < D / 32; ++cc) {
+                            for (int n = 0; n < SN; ++n)
+                                *reinterpret_cast<float2 *>(red + C::part(mt, s, ks) + g * C::PITCH + n * 8 + c2) =
+                                    make_float2(o[s * SN + n][e * 2], o[s * SN + n][e * 2 + 1]);
+                        }
+                    bar_consumers();
+                    mj[e] = -INFINITY;
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        *reinterpret_cast<float2 *>(red + (warp * 16 + g + e * 8) * C::RED_PITCH + n * 8 + c2) =
-                            make_float2(o[cc * 4 + n][e * 2] * sc[e], o[cc * 4 + n][e * 2 + 1] * sc[e]);
-                }
-                bar_consumers();
-                for (int i = tid; i < C::ROWS * 8; i += 128) {
-                    const int r = i >> 3, c4 = (i & 7) * 4;
-                    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int k = 0; k < C::KS; ++k) mj[e] = fmaxf(mj[e], stat_m[(mt * C::KS + k) * 16 + g + e * 8]);
+                    const float ref = mj[e] == -INFINITY ? 0.f : mj[e];
+                    lj[e] = 0.f;
 #pragma unroll
                     for (int k = 0; k < C::KS; ++k) {
-                        const float4 y = *reinterpret_cast<const float4 *>(red + (((r >> 4) * C::KS + k) * 16 + (r & 15)) * C::RED_PITCH + c4);
-                        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-                    }
-                    if (r < u.rows) {
-                        if (whole) {
-                            const int fr = u.row0 + r, tok = u.tok0 + fr / a.group;
-                            if ((unsigned)tok < (unsigned)a.n_rows)
-                                *reinterpret_cast<uint2 *>(a.out + (long long)tok * a.o_st + (long long)(w.h * a.group + fr % a.group) * a.o_sh + cc * 32 + c4) =
-                                    make_uint2(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w));
-                        } else {
-                            *reinterpret_cast<float4 *>(prec + r * D + cc * 32 + c4) = x;
-                        }
+                        sc[e][k] = pa_exp2(stat_m[(mt * C::KS + k) * 16 + g + e * 8] - ref);
+                        lj[e] += stat_l[(mt * C::KS + k) * 16 + g + e * 8] * sc[e][k];
                     }
                 }
-                bar_consumers();
+                const float inv = whole ? (lj[e] > 0.f ? 1.f / lj[e] : (lj[e] == 0.f ? 0.f : lj[e])) : 1.f;      // NaN stays NaN
+                const int r = mt * 16 + g + e * 8, fr = u.row0 + r, rt = pa_token(a, fr), tok = u.tok0 + rt;
+                __nv_bfloat16 *orow = a.out + (long long)tok * a.o_st + (long long)(w.h * a.group + fr - rt * a.group) * a.o_sh;
+#pragma unroll
+                for (int s = 0; s < C::KS; ++s)
+                    if (s == ks) {
+#pragma unroll
+                        for (int n = 0; n < SN; ++n) {
+                            float x = o[s * SN + n][e * 2] * sc[e][s], y = o[s * SN + n][e * 2 + 1] * sc[e][s];
+#pragma unroll
+                            for (int k = 0; k < C::KS; ++k)
+                                if (k != s) {
+                                    const float2 z = *reinterpret_cast<const float2 *>(red + C::part(mt, s, k) + g * C::PITCH + n * 8 + c2);
+                                    x = fmaf(z.x, sc[e][k], x);
+                                    y = fmaf(z.y, sc[e][k], y);
+                                }
+                            const int ch = (s * SN + n) * 8 + c2;
+                            if (r < u.rows) {
+                                if (!whole) *reinterpret_cast<float2 *>(prec + r * D + ch) = make_float2(x, y);
+                                else if ((unsigned)tok < (unsigned)a.n_rows) *reinterpret_cast<uint32_t *>(orow + ch) = pack_bf16x2(x * inv, y * inv);
+                            }
+                        }
+                    }
+                if (!whole && ks == 0 && (lane & 3) == 0 && r < u.rows) {
+                    prec[C::ROWS * D + r] = mj[e];
+                    prec[C::ROWS * D + C::ROWS + r] = lj[e];
+                }
+                if (C::KS > 1) bar_consumers();               // the buffer is read before it is written again
             }
             if (!whole) {
                 // the block that writes the last part of the pair joins all of them, in block order
                 const int b0 = w.first_block(), b1 = w.last_block();
-                __threadfence();
                 bar_consumers();
                 if (tid == 0) {
+                    __threadfence();
                     const int n = atomicAdd(&a.counters[b0], 1);
                     const int last = n == b1 - b0;
                     if (last) a.counters[b0] = 0;
+                    __threadfence();
                     *last_flag = last;
                 }
                 bar_consumers();
                 if (*last_flag) {
-                    __threadfence();
+                    const float *first = a.part + (size_t)w.record(b0) * C::REC;
                     for (int i = tid; i < u.rows * (D / 4); i += 128) {
                         const int r = i / (D / 4), c4 = (i % (D / 4)) * 4;
-                        float mm = -INFINITY;
-                        for (int c = b0; c <= b1; ++c) mm = fmaxf(mm, __ldcg(a.part + (size_t)w.record(c) * C::REC + C::ROWS * D + r));
-                        const float ref = mm == -INFINITY ? 0.f : mm;
-                        float ll = 0.f;
+                        float mm = -INFINITY, ll = 0.f;
                         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                        for (int c = b0; c <= b1; ++c) {
-                            const float *rc = a.part + (size_t)w.record(c) * C::REC;
-                            const float f = pa_exp2(__ldcg(rc + C::ROWS * D + r) - ref);
-                            ll += f * __ldcg(rc + C::ROWS * D + C::ROWS + r);
-                            const float4 y = __ldcg(reinterpret_cast<const float4 *>(rc + r * D + c4));
-                            x.x += f * y.x; x.y += f * y.y; x.z += f * y.z; x.w += f * y.w;
+                        // eight parts at a time, so that their loads are in flight together
+                        for (int c = b0; c <= b1; c += 8) {
+                            float pm[8], pl[8];
+                            float4 pv[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                pm[k] = -INFINITY;
+                                pl[k] = 0.f;
+                                pv[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                                if (c + k <= b1) {
+                                    const float *rc = c + k == b0 ? first : a.part + (size_t)(2 * (c + k)) * C::REC;
+                                    pm[k] = __ldcg(rc + C::ROWS * D + r);
+                                    pl[k] = __ldcg(rc + C::ROWS * D + C::ROWS + r);
+                                    pv[k] = __ldcg(reinterpret_cast<const float4 *>(rc + r * D + c4));
+                                }
+                            }
+                            float mn = mm;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) mn = fmaxf(mn, pm[k]);
+                            const float ref = mn == -INFINITY ? 0.f : mn, f0 = pa_exp2(mm - ref);
+                            mm = mn;
+                            ll *= f0;
+                            x.x *= f0; x.y *= f0; x.z *= f0; x.w *= f0;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                const float f = pa_exp2(pm[k] - ref);
+                                ll = fmaf(f, pl[k], ll);
+                                x.x = fmaf(f, pv[k].x, x.x); x.y = fmaf(f, pv[k].y, x.y); x.z = fmaf(f, pv[k].z, x.z); x.w = fmaf(f, pv[k].w, x.w);
+                            }
                         }
                         const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
-                        const int fr = u.row0 + r, tok = u.tok0 + fr / a.group;
+                        const int fr = u.row0 + r, rt = pa_token(a, fr), tok = u.tok0 + rt;
                         if ((unsigned)tok < (unsigned)a.n_rows)
-                            *reinterpret_cast<uint2 *>(a.out + (long long)tok * a.o_st + (long long)(w.h * a.group + fr % a.group) * a.o_sh + c4) =
+                            *reinterpret_cast<uint2 *>(a.out + (long long)tok * a.o_st + (long long)(w.h * a.group + fr - rt * a.group) * a.o_sh + c4) =
                                 make_uint2(pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv));
                     }
                 }

@@ -24,23 +24,30 @@ using namespace ptx;
 
 template <int D>
 struct TcAttnCfg {
-    static constexpr int ROWS = 256, KT = 128;
+    static constexpr int ROWS = 0, KT = 128;               // rows of a unit: 2 x as many whole tokens as 128 rows hold
     static constexpr int NB = D / 64;
     static constexpr int BLK = 128 * 128;                  // bytes of 128 rows of 64 channels
     static constexpr int TILE = NB * BLK;                  // a Q, K or V tile
     static constexpr int NS = D == 128 ? 5 : 10;           // K and V tiles in flight
     static constexpr int THREADS = 384;
     static constexpr int TMEM_COLS = 512;                  // S0, S1: 128 columns each, then O0, O1: D columns each
-    static constexpr size_t SMEM = 1024 + 2 * (size_t)TILE + (size_t)NS * TILE + 1536;
+    static constexpr size_t SMEM = 1024 + 2 * (size_t)TILE + (size_t)NS * TILE + 1280;
     static constexpr int REC = 256 * (D + 2);              // floats of a partial record: [D / 4][256 rows][4], maxima, sums
 };
 
 struct TcAttnParams {
-    CUtensorMap k, v;
+    CUtensorMap q, k, v;
     PagedArgs a;
+    int q_bytes;                                            // of one 64-channel block of a Q tile
 };
 
-__device__ __forceinline__ void bar_group(int i) { asm volatile("bar.sync %0, 128;" ::"r"(1 + i) : "memory"); }
+// What the softmax warps need of a piece; t0 < 0: no more pieces.
+struct alignas(16) TcPiece {
+    int t0, t1, full0, full1;      // key tiles of the piece; those in [full0, full1) need no mask
+    int row0, rows, tok0, base;    // as in PaUnit
+    int h, whole, rec, b0;         // KV head; not split; record of this block's part; first and last block of the pair
+    int b1, rec0, ns, lo_tile;     // record of the first block's part
+};
 
 // Columns 0 .. n - 1 of 32 as a bit mask (n may be anything).
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
@@ -63,17 +70,21 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
     uint8_t *kv = smem + 2 * (size_t)C::TILE;               // [NS][TILE]
     uint64_t *full = reinterpret_cast<uint64_t *>(kv + (size_t)C::NS * C::TILE);
     uint64_t *empty = full + C::NS;
-    uint64_t *q_full = empty + C::NS;      // [2] Q tile written (4 warps)
-    uint64_t *s_full = q_full + 2;         // [2] scores complete
+    uint64_t *q_full = empty + C::NS;      // [2] Q tile written
+    uint64_t *q_empty = q_full + 2;        // [2] its last scores of a piece complete
+    uint64_t *info_full = q_empty + 2;     // [2] a piece's description written
+    uint64_t *info_empty = info_full + 2;  // [2] read by the 8 softmax warps
+    uint64_t *joined = info_empty + 2;     // [2] barrier among a tile's 4 softmax warps
+    uint64_t *s_full = joined + 2;         // [2] scores complete
     uint64_t *p_ready = s_full + 2;        // [2][2] weights of the first and second 64 keys written (4 warps)
     uint64_t *o_full = p_ready + 4;        // [2] last product with V of a piece complete
     uint64_t *landed = o_full + 2;         // [NS] a V tile that has rows to clear: copied
     uint64_t *drain = landed + C::NS;
     long long *warp_sums = reinterpret_cast<long long *>(drain + 1);
-    PaShare *share = reinterpret_cast<PaShare *>(warp_sums + 12);
+    PaShare *share = reinterpret_cast<PaShare *>(warp_sums + 36);
     using Walk = PaWalk<C::ROWS, C::KT>;
-    Walk *walks = reinterpret_cast<Walk *>(share + 1);      // [8] of the softmax warps, whose registers hold scores
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(walks + 8);
+    TcPiece *info = reinterpret_cast<TcPiece *>(((uintptr_t)(share + 1) + 15) & ~(uintptr_t)15);   // [2]
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(info + 2);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     volatile int *last_flag = abort_flag + 2;               // [2]
 
@@ -82,7 +93,11 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
     if (tid == 0) {
         for (int i = 0; i < C::NS; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&landed[i], 1); }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&q_full[i], 4);
+            mbar_init(&q_full[i], 1);
+            mbar_init(&q_empty[i], 1);
+            mbar_init(&info_full[i], 1);
+            mbar_init(&info_empty[i], 8);
+            mbar_init(&joined[i], 4);
             mbar_init(&s_full[i], 1);
             mbar_init(&p_ready[2 * i], 4);
             mbar_init(&p_ready[2 * i + 1], 4);
@@ -92,6 +107,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
         abort_flag[0] = 0;
         abort_flag[1] = (int)a.poll_limit;
         mbar_fence_init();
+        tma_prefetch_desc(&P.q);
         tma_prefetch_desc(&P.k);
         tma_prefetch_desc(&P.v);
     }
@@ -102,6 +118,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
     const uint32_t tmem = *tmem_slot;
 
     const bool any = share->begin < share->end;
+    const int RT = a.unit_rows >> 1;                        // rows of a tile, at most 128
     const int box_log2 = a.page_log2 < 7 ? a.page_log2 : 7;
     bool dead = false;       // a wait ran out: no more waits, the rest runs through on whatever is there
 
@@ -124,7 +141,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                     const int j0 = pa_tile(w.u, t) * C::KT;
                     const int key = j0 + (i << box_log2);
                     int page = a.n_pages;                                // outside the pool: the copy writes zeros
-                    if (cb < C::NB && key < w.u.hi_key) {
+                    if (cb < C::NB && pa_wanted(a, w.u, key, 1 << box_log2)) {
                         const int col = key >> a.page_log2;
                         if (col < a.table_cols) page = __ldg(row + col);
                     }
@@ -183,6 +200,45 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                 more = !dead && w.next(a);
             }
         }
+    } else if (warp == 11) {
+        // ================================ pieces and their Q tiles ================================
+        // Runs ahead of the softmax warps: the next piece's rows are loaded while the last tile of this one is worked on.
+        if (any) {
+            uint32_t n = 0, nq[2] = {0, 0};
+            bool more = true;
+            while (more && !dead) {
+                if (!mbar_wait_suspended_warp(&info_empty[n & 1], ((n >> 1) & 1) ^ 1, abort_flag)) { dead = true; break; }
+                if (lane == 0) {
+                    TcPiece &p = info[n & 1];
+                    p.t0 = w.t; p.t1 = w.t1;
+                    pa_full_tiles<C::KT>(a, w.u, p.full0, p.full1);
+                    p.row0 = w.u.row0; p.rows = w.u.rows; p.tok0 = w.u.tok0; p.base = w.u.base;
+                    p.h = w.h; p.whole = w.whole() ? 1 : 0; p.rec = w.record(blockIdx.x);
+                    p.b0 = w.first_block(); p.b1 = w.last_block(); p.rec0 = w.record(p.b0);
+                    p.ns = w.u.ns; p.lo_tile = w.u.lo_tile;
+                    mbar_arrive(&info_full[n & 1]);
+                }
+                __syncwarp();
+                ++n;
+                const int tiles = w.u.rows > RT ? 2 : 1;
+                for (int i = 0; i < tiles; ++i) {
+                    if (!mbar_wait_suspended_warp(&q_empty[i], (nq[i]++ & 1) ^ 1, abort_flag)) { dead = true; break; }
+                    // rows behind the request's are another one's, or zeros, or an earlier tile's: nobody reads their results
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx(&q_full[i], C::NB * P.q_bytes);
+                        for (int cb = 0; cb < C::NB; ++cb)
+                            tma_load_4d(qs + i * C::TILE + cb * C::BLK, &P.q, &q_full[i], 0, w.h * a.group,
+                                        w.u.tok0 + (w.u.qt * 2 + i) * (a.unit_tokens >> 1), cb);
+                    }
+                    __syncwarp();
+                }
+                more = w.next(a);
+            }
+            if (!dead && mbar_wait_suspended_warp(&info_empty[n & 1], ((n >> 1) & 1) ^ 1, abort_flag) && lane == 0) {
+                info[n & 1].t0 = -1;
+                mbar_arrive(&info_full[n & 1]);
+            }
+        }
     } else if (warp == 9) {
         // ================================ MMA issuer ================================
         // The whole warp walks and one elected lane issues (see elect_one).
@@ -197,7 +253,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
             Ring<C::NS> st;
             uint32_t nq[2] = {0, 0}, np[2] = {0, 0};
             bool more = true;
-            auto scores = [&](int i, uint32_t stage) {
+            auto scores = [&](int i, uint32_t stage, bool last) {
                 const uint64_t qd = proto_k | (uint64_t)(q_addr + i * (C::TILE >> 4));
                 const uint64_t kd = proto_k | (uint64_t)(kv_addr + __shfl_sync(0xffffffffu, stage, 0) * (C::TILE >> 4));
                 if (leader) {
@@ -207,6 +263,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                         umma_bf16_ss(tm + i * 128, qd + off, kd + off, idesc_s, k == 0 ? 0u : 1u);
                     }
                     umma_commit(&s_full[i]);
+                    if (last) umma_commit(&q_empty[i]);    // the piece's last scores of this tile
                 }
                 __syncwarp();
             };
@@ -225,7 +282,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                 __syncwarp();
             };
             while (more && !dead) {
-                const int tiles = w.u.rows > 128 ? 2 : 1;
+                const int tiles = w.u.rows > RT ? 2 : 1;
                 // K of the piece's first tile
                 uint32_t ks = st.idx;
                 if (!mbar_wait_suspended_warp(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
@@ -235,7 +292,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                     if (i >= tiles || dead) break;
                     if (!mbar_wait_suspended_warp(&q_full[i], nq[i]++ & 1, abort_flag)) { dead = true; break; }
                     tc_fence_after();
-                    scores(i, ks);
+                    scores(i, ks, w.t + 1 == w.t1);
                 }
                 if (dead) break;
                 commit(&empty[ks]);
@@ -261,7 +318,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                                 if (!mbar_wait_suspended_warp(&full[st.idx], st.phase, abort_flag)) { dead = true; break; }
                                 st.next();
                             }
-                            scores(i, ks);
+                            scores(i, ks, t + 2 == w.t1);
                             if (i == tiles - 1) commit(&empty[ks]);
                         }
                     }
@@ -283,34 +340,33 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
         const uint32_t s_tm = tmem + i * 128 + lanes, o_tm = tmem + 256 + i * D + lanes;
         const float c = a.scale_log2;
         const uint64_t cc = f2_pack(c, c);
-        uint32_t ns = 0, no = 0;
-        Walk &w = walks[warp];
-        if (any) w.open(a, *share);                        // every lane writes the same
-        __syncwarp();
-        bool more = any;
-        while (more) {
-            const PaUnit &u = w.u;
-            const int rr = i * 128 + r;                    // row in the unit
-            if (i * 128 < u.rows) {
-                const int fr = u.row0 + rr, tok = u.tok0 + fr / a.group, head = w.h * a.group + fr % a.group;
-                const bool live = rr < u.rows && (unsigned)tok < (unsigned)a.n_rows;
-                const int pos = live ? u.base + fr / a.group : -1;
-                // the piece's Q tile; the products that read the one before it are complete
-                {
-                    const uint4 *src = reinterpret_cast<const uint4 *>(a.q + (long long)tok * a.q_st + (long long)head * a.q_sh);
-                    uint8_t *dst = qs + i * C::TILE + r * 128;
-#pragma unroll
-                    for (int x = 0; x < D / 8; ++x)
-                        *reinterpret_cast<uint4 *>(dst + (x >> 3) * C::BLK + (((x & 7) ^ (r & 7)) << 4)) = live ? src[x] : make_uint4(0, 0, 0, 0);
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&q_full[i]);
+        uint32_t ns = 0, no = 0, nj = 0;
+        auto settle = [&](int tile, uint32_t from) {
+            Walk w;
+            bool more = w.open(a, *share);
+            for (uint32_t k = 0; more; ++k, more = w.next(a))
+                if (k >= from && !w.whole() && tile * RT < w.u.rows) {
+                    int *counter = &a.counters[2 * w.first_block() + tile];
+                    if (atomicAdd(counter, 1) == w.last_block() - w.first_block()) *counter = 0;
                 }
+        };
+        for (uint32_t n = 0; any; ++n) {
+            if (!mbar_wait_suspended_warp(&info_full[n & 1], (n >> 1) & 1, abort_flag)) {
+                // time-out: the parts that this block will not write still count, or the next call would wait for them
+                if (r == 0) settle(i, n);
+                break;
+            }
+            const TcPiece p = info[n & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&info_empty[n & 1]);
+            if (p.t0 < 0) break;
+            const int rr = i * 128 + r;                    // place in a partial record
+            if (i * RT < p.rows) {
+                const int fr = p.row0 + i * RT + r, rt = pa_token(a, fr), tok = p.tok0 + rt, head = p.h * a.group + fr - rt * a.group;
+                const bool live = r < RT && i * RT + r < p.rows && (unsigned)tok < (unsigned)a.n_rows;
+                const int pos = live ? p.base + rt : -1;
                 float m = -INFINITY, l = 0.f;              // reference maximum (raw score), sum of weights
-                const int t0 = w.t, t1 = w.t1;
-                int full0, full1;                          // tiles [full0, full1) need no mask
-                pa_full_tiles<C::KT>(a, u, full0, full1);
-                for (int t = t0; t < t1; ++t) {
+                for (int t = p.t0; t < p.t1; ++t) {
                     if (!dead && !mbar_wait_suspended_warp(&s_full[i], ns & 1, abort_flag)) dead = true;
                     ++ns;
                     tc_fence_after();
@@ -318,8 +374,8 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
 #pragma unroll
                     for (int x = 0; x < 4; ++x) tmem_ld_32x32(s_tm + x * 32, s[x]);
                     tmem_wait_ld();
-                    if (t < full0 || t >= full1) {
-                        const int j0 = pa_tile(u, t) * C::KT;
+                    if (t < p.full0 || t >= p.full1) {
+                        const int j0 = (t < p.ns ? t : p.lo_tile + (t - p.ns)) * C::KT;
                         const int hi = min(pos - j0, C::KT - 1);                               // last column seen
                         const int lo = a.window > 0 ? (int)max((long long)pos - a.window + 1 - j0, -1ll) : -1;   // first one, without
                         const int sink = a.window > 0 ? a.n_sink - j0 : 0;                     // the sinks
@@ -339,12 +395,12 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                         for (int x = 0; x < 4; ++x) mx[x] = max3(mx[x], __uint_as_float(s[x][y]), __uint_as_float(s[x][y + 1]));
                     const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                     float f = 1.f;
-                    if ((top - m) * c > 8.f) {             // also the first maximum of a row: m is -inf
+                    if (live && (top - m) * c > 8.f) {     // also the first maximum of a row: m is -inf
                         f = pa_exp2((m - top) * c);
                         m = top;
                         l *= f;
                     }
-                    if (t > t0 && __any_sync(0xffffffffu, f != 1.f)) {
+                    if (t > p.t0 && __any_sync(0xffffffffu, f != 1.f)) {
 #pragma unroll 1
                         for (int x = 0; x < D / 16; ++x) {
                             uint32_t o[16];
@@ -390,7 +446,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                 ++no;
                 tc_fence_after();
                 __nv_bfloat16 *orow = a.out + (long long)tok * a.o_st + (long long)head * a.o_sh;
-                if (w.whole()) {
+                if (p.whole) {
                     const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
 #pragma unroll 1
                     for (int x = 0; x < D / 32; ++x) {
@@ -411,7 +467,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                     }
                     tc_fence_before();
                 } else {
-                    float *rec = a.part + (size_t)w.record(blockIdx.x) * C::REC;
+                    float *rec = a.part + (size_t)p.rec * C::REC;
 #pragma unroll 1
                     for (int x = 0; x < D / 32; ++x) {
                         uint32_t o[32];
@@ -426,39 +482,69 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                     rec[256 * D + rr] = m * c;             // c > 0: -inf stays -inf
                     rec[256 * D + 256 + rr] = l;
                     // the block that writes the last part of the pair joins all of them, in block order
-                    const int b0 = w.first_block(), b1 = w.last_block();
-                    __threadfence();
-                    bar_group(i);
+                    auto meet = [&]() {                    // the tile's four warps
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&joined[i]);
+                        if (!dead && !mbar_wait_suspended_warp(&joined[i], nj & 1, abort_flag)) dead = true;
+                        ++nj;
+                    };
+                    meet();
                     if (r == 0) {
-                        const int n = atomicAdd(&a.counters[2 * b0 + i], 1);
-                        const int last = n == b1 - b0;
-                        if (last) a.counters[2 * b0 + i] = 0;
+                        __threadfence();
+                        const int k = atomicAdd(&a.counters[2 * p.b0 + i], 1);
+                        const int last = k == p.b1 - p.b0;
+                        if (last) a.counters[2 * p.b0 + i] = 0;
+                        __threadfence();
                         last_flag[i] = last;
                     }
-                    bar_group(i);
+                    meet();
                     if (last_flag[i]) {
-                        __threadfence();
-                        float mm = -INFINITY;
-                        for (int b = b0; b <= b1; ++b) mm = fmaxf(mm, __ldcg(a.part + (size_t)w.record(b) * C::REC + 256 * D + rr));
-                        const float ref = mm == -INFINITY ? 0.f : mm;
-                        float ll = 0.f;
-                        for (int b = b0; b <= b1; ++b) {
-                            const float *rc = a.part + (size_t)w.record(b) * C::REC + 256 * D + rr;
-                            ll += pa_exp2(__ldcg(rc) - ref) * __ldcg(rc + 256);
+                        const float *mine = a.part + 256 * D + rr;
+                        auto at = [&](int b) { return (size_t)(b == p.b0 ? p.rec0 : 2 * b) * C::REC; };
+                        float mm = -INFINITY, ll = 0.f;
+                        for (int b = p.b0; b <= p.b1; b += 4) {           // four parts' loads in flight together
+                            float pm[4], pl[4], mn = mm;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                pm[k] = b + k <= p.b1 ? __ldcg(mine + at(b + k)) : -INFINITY;
+                                pl[k] = b + k <= p.b1 ? __ldcg(mine + at(b + k) + 256) : 0.f;
+                            }
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) mn = fmaxf(mn, pm[k]);
+                            const float ref = mn == -INFINITY ? 0.f : mn;
+                            ll *= pa_exp2(mm - ref);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) ll = fmaf(pa_exp2(pm[k] - ref), pl[k], ll);
+                            mm = mn;
                         }
+                        const float ref = mm == -INFINITY ? 0.f : mm;
                         const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
 #pragma unroll 1
                         for (int x = 0; x < D / 32; ++x) {
                             float acc[32];
 #pragma unroll
                             for (int y = 0; y < 32; ++y) acc[y] = 0.f;
-                            for (int b = b0; b <= b1; ++b) {
-                                const float *rc = a.part + (size_t)w.record(b) * C::REC;
-                                const float f = pa_exp2(__ldcg(rc + 256 * D + rr) - ref) * inv;
+                            for (int b = p.b0; b <= p.b1; b += 2) {       // two parts in flight
+                                float4 v[2][8];
+                                float f[2];
 #pragma unroll
-                                for (int y = 0; y < 8; ++y) {
-                                    const float4 v = __ldcg(reinterpret_cast<const float4 *>(rc + ((size_t)(x * 8 + y) * 256 + rr) * 4));
-                                    acc[y * 4] += f * v.x; acc[y * 4 + 1] += f * v.y; acc[y * 4 + 2] += f * v.z; acc[y * 4 + 3] += f * v.w;
+                                for (int k = 0; k < 2; ++k) {
+                                    f[k] = b + k <= p.b1 ? __ldcg(mine + at(b + k)) : -INFINITY;
+#pragma unroll
+                                    for (int y = 0; y < 8; ++y)
+                                        v[k][y] = b + k <= p.b1 ? __ldcg(reinterpret_cast<const float4 *>(a.part + at(b + k) + ((size_t)(x * 8 + y) * 256 + rr) * 4))
+                                                                : make_float4(0.f, 0.f, 0.f, 0.f);
+                                }
+#pragma unroll
+                                for (int k = 0; k < 2; ++k) {
+                                    const float g = pa_exp2(f[k] - ref) * inv;
+#pragma unroll
+                                    for (int y = 0; y < 8; ++y) {
+                                        acc[y * 4] = fmaf(g, v[k][y].x, acc[y * 4]);
+                                        acc[y * 4 + 1] = fmaf(g, v[k][y].y, acc[y * 4 + 1]);
+                                        acc[y * 4 + 2] = fmaf(g, v[k][y].z, acc[y * 4 + 2]);
+                                        acc[y * 4 + 3] = fmaf(g, v[k][y].w, acc[y * 4 + 3]);
+                                    }
                                 }
                             }
                             if (live) {
@@ -470,13 +556,9 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                             }
                         }
                     }
-                    bar_group(i);                          // last_flag is read before the next piece writes it
+                    meet();                                // last_flag is read before the next piece writes it
                 }
             }
-            __syncwarp();
-            if (lane == 0) more = w.next(a);
-            __syncwarp();
-            more = __shfl_sync(0xffffffffu, more ? 1 : 0, 0) != 0;
         }
     }
     __syncwarp();
@@ -508,7 +590,10 @@ cudaError_t launch_paged_attn_tc(const PagedArgs &a, int d, const void *k, const
     TcAttnParams P;
     P.a = a;
     const int box = page_size < 128 ? page_size : 128;
-    if (!make_kv_tensor_map(&P.k, k, d, a.Hkv, page_size, a.n_pages, s_head, s_slot, s_page, box, 1) ||
+    const int q_tokens = a.n_rows < a.unit_tokens / 2 ? a.n_rows : a.unit_tokens / 2;
+    P.q_bytes = q_tokens * a.group * 128;
+    if (!make_q_tensor_map(&P.q, a.q, d, a.Hkv * a.group, a.n_rows, a.q_sh, a.q_st, a.group, q_tokens) ||
+        !make_kv_tensor_map(&P.k, k, d, a.Hkv, page_size, a.n_pages, s_head, s_slot, s_page, box, 1) ||
         !make_kv_tensor_map(&P.v, v, d, a.Hkv, page_size, a.n_pages, s_head, s_slot, s_page, box, 1))
         return cudaErrorInvalidValue;
     return d == 128 ? launch_tc_attn<128>(P, st) : launch_tc_attn<64>(P, st);

@@ -164,11 +164,19 @@ __device__ __forceinline__ void tma_prefetch_desc(const CUtensorMap *map)
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
 
-// ---- asynchronous 4-byte copies (any alignment, zero fill when src_bytes == 0) --------------------------
+// ---- asynchronous copies of 4 and of 16 bytes (zero fill when src_bytes == 0) --------------------------
 __device__ __forceinline__ void cp_async_4(void *dst_smem, const void *src, uint32_t src_bytes)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst_smem)), "l"(src), "r"(src_bytes) : "memory");
 }
+__device__ __forceinline__ void cp_async_16(void *dst_smem, const void *src, uint32_t src_bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst_smem)), "l"(src), "r"(src_bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// All but the N most recent groups of this thread's copies have landed.
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 // The barrier receives one arrival from this thread once all its earlier asynchronous copies have landed; the
 // arrival must be part of the barrier's expected count.
 __device__ __forceinline__ void cp_async_arrive_noinc(uint64_t *bar)

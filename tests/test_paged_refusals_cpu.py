@@ -95,7 +95,7 @@ def _attention(pool=None, layer=1, q=0x1000, qs=(2048, 128), out=0x2000, os=(204
     (dict(heads=15), BAD), (dict(heads=0), BAD), (dict(scale=0.0), BAD), (dict(scale=-1.0), BAD), (dict(scale=float("inf")), BAD),
     (dict(scale=float("nan")), BAD), (dict(window=-1), BAD), (dict(sinks=-1), BAD), (dict(max_new=-1), BAD), (dict(rows=-1), BAD), (dict(B=-1), BAD),
     (dict(cols=0), BAD), (dict(stride=4), BAD), (dict(q=0), BAD), (dict(q=0x1008), BAD), (dict(out=0), BAD), (dict(table=0), BAD), (dict(cu=0), BAD),
-    (dict(total=0x302), BAD), (dict(qs=(2047, 128)), BAD), (dict(os=(0, 128)), UNS), (dict(os=(2048, 0)), UNS), (dict(qs=(0, 0)), CUDA),
+    (dict(total=0x302), BAD), (dict(qs=(2047, 128)), BAD), (dict(os=(0, 128)), UNS), (dict(os=(2048, 0)), UNS), (dict(qs=(0, 128)), UNS), (dict(qs=(2048, 0)), UNS), (dict(rows=1, qs=(0, 128), os=(0, 128)), CUDA),
     (dict(rows=1 << 28), UNS), (dict(ws=0), WS), (dict(ws=0x10010), WS), (dict(ws_bytes=1000), WS)])
 def test_attention(change, want):
     assert _attention(**change) == want
