@@ -24,6 +24,7 @@ struct TablesArgs {
     long long *slot_map;
     long long n_rows;
     int *pages_used;
+    int vector;               // positions and slot_map allow 16-byte stores
 };
 
 __global__ void __launch_bounds__(PT_THREADS) k_page_tables(const TablesArgs a)
@@ -51,8 +52,9 @@ __global__ void __launch_bounds__(PT_THREADS) k_page_tables(const TablesArgs a)
         }
         if (lane == 31) warp_sums[warp] = incl;
         __syncthreads();
-        unsigned long long before = 0;
-        for (int w = 0; w < warp; ++w) before += warp_sums[w];
+        unsigned long long before = lane < warp ? warp_sums[lane] : 0ull;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
         const unsigned long long excl = before + incl - own;
         row_at[tid] = (unsigned)excl;
         page_at[tid] = (unsigned)(excl >> 32);
@@ -73,22 +75,47 @@ __global__ void __launch_bounds__(PT_THREADS) k_page_tables(const TablesArgs a)
             const long long f = pages0 + e;
             if ((unsigned)col < (unsigned)a.cols) a.table[(long long)(b0 + lo) * a.table_stride + col] = f < a.n_free ? a.free_pages[f] : -1;
         }
-        for (long long e = mine; e < n_rows && rows0 + e < a.n_rows; e += stride) {
+        // rows, four neighbours a thread: one search for the four
+        const long long end = min(rows0 + (long long)n_rows, a.n_rows);
+        for (long long t0 = rows0 / 4 * 4 + mine * 4; t0 < end; t0 += stride * 4) {
+            const long long first = max(t0, rows0);
+            unsigned e = (unsigned)(first - rows0);
             int lo = 0, hi = PT_THREADS - 1;
             while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (row_at[mid] <= e) lo = mid; else hi = mid - 1; }
-            const int pos = s_cached[lo] + (int)(e - row_at[lo]);
-            const int col = pos >> a.page_log2;
-            int page = -1;
-            if ((unsigned)col < (unsigned)a.cols) {
-                if (col < s_held[lo]) {
-                    page = a.table[(long long)(b0 + lo) * a.table_stride + col];
-                } else {
+            int pos[4], page[4];
+            const int *from[4];                       // where the row's page id stands
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                pos[k] = 0;
+                from[k] = nullptr;
+                if (t0 + k < first || t0 + k >= end) continue;
+                while (lo < PT_THREADS - 1 && row_at[lo + 1] <= e) ++lo;
+                pos[k] = s_cached[lo] + (int)(e - row_at[lo]);
+                const int col = pos[k] >> a.page_log2;
+                if ((unsigned)col < (unsigned)a.cols) {
                     const long long f = pages0 + page_at[lo] + (col - s_held[lo]);
-                    if (f < a.n_free) page = a.free_pages[f];
+                    if (col < s_held[lo]) from[k] = a.table + (long long)(b0 + lo) * a.table_stride + col;
+                    else if (f < a.n_free) from[k] = a.free_pages + f;
                 }
+                ++e;
             }
-            a.positions[rows0 + e] = pos;
-            a.slot_map[rows0 + e] = page < 0 ? -1 : ((long long)page << a.page_log2) + (pos & ps1);
+            long long slot[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) page[k] = from[k] ? *from[k] : -1;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) slot[k] = page[k] < 0 ? -1ll : ((long long)page[k] << a.page_log2) + (pos[k] & ps1);
+            if (a.vector && t0 >= rows0 && t0 + 4 <= end) {
+                *reinterpret_cast<int4 *>(a.positions + t0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+                *reinterpret_cast<longlong2 *>(a.slot_map + t0) = make_longlong2(slot[0], slot[1]);
+                *reinterpret_cast<longlong2 *>(a.slot_map + t0 + 2) = make_longlong2(slot[2], slot[3]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (t0 + k >= first && t0 + k < end) {
+                        a.positions[t0 + k] = pos[k];
+                        a.slot_map[t0 + k] = slot[k];
+                    }
+            }
         }
         rows0 += n_rows;
         pages0 += n_pages;
@@ -109,7 +136,8 @@ cudaError_t launch_page_tables(const int *cached, const int *fresh, int n_reques
                                int *positions, long long *slot_map, long long n_rows, int *pages_used, cudaStream_t st)
 {
     TablesArgs a{cached, fresh, n_requests, page_log2, free_pages, n_free, table, table_stride, table_cols,
-                 cu, total, positions, slot_map, n_rows, pages_used};
+                 cu, total, positions, slot_map, n_rows, pages_used,
+                 (((uintptr_t)positions | (uintptr_t)slot_map) & 15) == 0};
     long long grid = (n_rows + PT_SPAN - 1) / PT_SPAN;
     const int sms = device_sm_count();
     if (grid < 1) grid = 1;
