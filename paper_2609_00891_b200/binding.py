@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence, Tuple
 
 import numpy as np
@@ -653,17 +654,25 @@ class _PagePool(ctypes.Structure):
                 ("stride_head", ctypes.c_int64)]
 
 
+_PAGE_POOL = struct.Struct("PPiiiiqqqqq")      # the same, packed: building a ctypes structure costs as much as a launch
+
+
 class PagePool:
     """K and V pages, bf16 tensors indexed [layer][page][slot][head][channel] (any strides, channels contiguous)."""
 
+    __slots__ = ("k", "v", "n_layers", "n_heads", "head_dim", "page_size", "n_pages", "c")
+
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
-        assert k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and k.dim() == 5
-        strides = k.stride()
-        assert k.shape == v.shape and strides == v.stride() and strides[4] == 1 and k.device == v.device
-        self.k, self.v = k, v
+        sl, sp, ss, sh, sc = k.stride()
         L, N, S, H, d = k.shape
-        self.c = _PagePool(k.data_ptr(), v.data_ptr(), L, H, d, S, N, strides[0], strides[1], strides[2], strides[3])
-        self.ptr = ctypes.addressof(self.c)
+        assert k.dtype == v.dtype == torch.bfloat16 and k.shape == v.shape and v.stride() == (sl, sp, ss, sh, sc) and sc == 1
+        assert k.device == v.device
+        self.k, self.v = k, v
+        self.n_layers, self.n_pages, self.page_size, self.n_heads, self.head_dim = L, N, S, H, d
+        self.c = _PAGE_POOL.pack(k.data_ptr(), v.data_ptr(), L, H, d, S, N, sl, sp, ss, sh)
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 def _on_one_device(stream, *tensors) -> int:
@@ -677,7 +686,7 @@ def _on_one_device(stream, *tensors) -> int:
     if dev != torch.cuda.current_device():
         raise ValueError("the tensors' device must be the current device")
     if stream is None:
-        return torch.cuda.current_stream(dev).cuda_stream
+        return _raw_stream(dev)
     if stream.device.index != dev:
         raise ValueError("the stream must belong to the tensors' device")
     return stream.cuda_stream
@@ -708,11 +717,11 @@ def cb_paged_store(pool: PagePool, src_k: torch.Tensor, src_v: torch.Tensor, slo
     L, T, H, d = src_k.shape
     ss = src_k.stride()
     assert src_k.dtype == src_v.dtype and src_k.shape == src_v.shape and ss == src_v.stride() and ss[3] == 1
-    assert (L, H, d) == (pool.c.n_layers, pool.c.n_heads, pool.c.head_dim)
+    assert L == pool.n_layers and H == pool.n_heads and d == pool.head_dim
     assert slot_map.dtype == torch.int64 and slot_map.is_contiguous() and slot_map.numel() == T
     dt = CB_DTYPE_BF16 if src_k.dtype == torch.bfloat16 else {torch.float32: CB_DTYPE_F32}[src_k.dtype]
     st = _on_one_device(stream, pool.k, src_k, src_v, slot_map)
-    _check(lib().cb_paged_store(pool.ptr, src_k.data_ptr(), src_v.data_ptr(), dt, T, ss[0], ss[1], ss[2], slot_map.data_ptr(), st),
+    _check(lib().cb_paged_store(pool.c, src_k.data_ptr(), src_v.data_ptr(), dt, T, ss[0], ss[1], ss[2], slot_map.data_ptr(), st),
            "cb_paged_store")
 
 
@@ -744,11 +753,11 @@ def cb_paged_attention(q: torch.Tensor, out: torch.Tensor, pool: PagePool, layer
     qs, os_ = q.stride(), out.stride()
     assert q.dtype == torch.bfloat16 and out.dtype == torch.bfloat16 and q.shape == out.shape and qs[2] == 1 and os_[2] == 1
     B, cols = block_table.shape
-    assert d == pool.c.head_dim and block_table.dtype == cu_new.dtype == total_len.dtype == torch.int32
+    assert d == pool.head_dim and block_table.dtype == cu_new.dtype == total_len.dtype == torch.int32
     assert (cols <= 1 or block_table.stride(1) == 1) and cu_new.is_contiguous() and total_len.is_contiguous()
     assert cu_new.numel() == B + 1 and total_len.numel() == B and workspace.dtype == torch.uint8 and workspace.is_contiguous()
     st = _on_one_device(stream, q, out, pool.k, block_table, cu_new, total_len, workspace)
-    _check(lib().cb_paged_attention(pool.ptr, layer, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1], T, Hq, block_table.data_ptr(),
+    _check(lib().cb_paged_attention(pool.c, layer, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1], T, Hq, block_table.data_ptr(),
                                     block_table.stride(0), cols, cu_new.data_ptr(), total_len.data_ptr(), B, max_new, scale, window, n_sink,
                                     workspace.data_ptr(), workspace.numel(), st), "cb_paged_attention")
 
