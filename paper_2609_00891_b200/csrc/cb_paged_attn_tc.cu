@@ -52,6 +52,12 @@ struct alignas(16) TcPiece {
 // Columns 0 .. n - 1 of 32 as a bit mask (n may be anything).
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
+__device__ __forceinline__ int ld_acquire(const int *p)
+{
+    int v;
+    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
 // Largest of three (one instruction on sm_100).
 __device__ __forceinline__ float max3(float x, float y, float z)
 {
@@ -467,38 +473,52 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                     }
                     tc_fence_before();
                 } else {
-                    float *rec = a.part + (size_t)p.rec * C::REC;
-#pragma unroll 1
-                    for (int x = 0; x < D / 32; ++x) {
-                        uint32_t o[32];
-                        tmem_ld_32x32(o_tm + x * 32, o);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int y = 0; y < 8; ++y)
-                            *reinterpret_cast<float4 *>(rec + ((size_t)(x * 8 + y) * 256 + rr) * 4) =
-                                make_float4(__uint_as_float(o[y * 4]), __uint_as_float(o[y * 4 + 1]), __uint_as_float(o[y * 4 + 2]), __uint_as_float(o[y * 4 + 3]));
-                    }
-                    tc_fence_before();
-                    rec[256 * D + rr] = m * c;             // c > 0: -inf stays -inf
-                    rec[256 * D + 256 + rr] = l;
-                    // the block that writes the last part of the pair joins all of them, in block order
                     auto meet = [&]() {                    // the tile's four warps
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&joined[i]);
                         if (!dead && !mbar_wait_suspended_warp(&joined[i], nj & 1, abort_flag)) dead = true;
                         ++nj;
                     };
-                    meet();
+                    int *counter = &a.counters[2 * p.b0 + i];
+                    // The block that has the last part of the pair joins all of them, in block order.  A block's first piece
+                    // ends a pair that the block before it finishes last, so that the other parts are mostly there already:
+                    // then this part stays in tensor memory and is joined from there.
                     if (r == 0) {
-                        __threadfence();
-                        const int k = atomicAdd(&a.counters[2 * p.b0 + i], 1);
-                        const int last = k == p.b1 - p.b0;
-                        if (last) a.counters[2 * p.b0 + i] = 0;
-                        __threadfence();
-                        last_flag[i] = last;
+                        const int k = ld_acquire(counter);
+                        if (k == p.b1 - p.b0) *counter = 0;
+                        last_flag[i] = k == p.b1 - p.b0;
                     }
                     meet();
-                    if (last_flag[i]) {
+                    bool join = last_flag[i];
+                    const bool fresh = join;               // this block's part is not in memory
+                    if (!fresh) {
+                        float *rec = a.part + (size_t)p.rec * C::REC;
+#pragma unroll 1
+                        for (int x = 0; x < D / 32; ++x) {
+                            uint32_t o[32];
+                            tmem_ld_32x32(o_tm + x * 32, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int y = 0; y < 8; ++y)
+                                *reinterpret_cast<float4 *>(rec + ((size_t)(x * 8 + y) * 256 + rr) * 4) =
+                                    make_float4(__uint_as_float(o[y * 4]), __uint_as_float(o[y * 4 + 1]), __uint_as_float(o[y * 4 + 2]), __uint_as_float(o[y * 4 + 3]));
+                        }
+                        rec[256 * D + rr] = m * c;         // c > 0: -inf stays -inf
+                        rec[256 * D + 256 + rr] = l;
+                        meet();
+                        if (r == 0) {
+                            __threadfence();
+                            const int k = atomicAdd(counter, 1);
+                            const int last = k == p.b1 - p.b0;
+                            if (last) *counter = 0;
+                            __threadfence();
+                            last_flag[i] = last;
+                        }
+                        meet();
+                        join = last_flag[i];
+                    }
+                    if (join) {
+                        const int me = (int)blockIdx.x;
                         const float *mine = a.part + 256 * D + rr;
                         auto at = [&](int b) { return (size_t)(b == p.b0 ? p.rec0 : 2 * b) * C::REC; };
                         float mm = -INFINITY, ll = 0.f;
@@ -506,8 +526,9 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                             float pm[4], pl[4], mn = mm;
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
-                                pm[k] = b + k <= p.b1 ? __ldcg(mine + at(b + k)) : -INFINITY;
-                                pl[k] = b + k <= p.b1 ? __ldcg(mine + at(b + k) + 256) : 0.f;
+                                const bool own = fresh && b + k == me;
+                                pm[k] = own ? m * c : b + k <= p.b1 ? __ldcg(mine + at(b + k)) : -INFINITY;
+                                pl[k] = own ? l : b + k <= p.b1 ? __ldcg(mine + at(b + k) + 256) : 0.f;
                             }
 #pragma unroll
                             for (int k = 0; k < 4; ++k) mn = fmaxf(mn, pm[k]);
@@ -522,18 +543,23 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
 #pragma unroll 1
                         for (int x = 0; x < D / 32; ++x) {
                             float acc[32];
+                            uint32_t o[32];
+                            tmem_ld_32x32(o_tm + x * 32, o);
 #pragma unroll
                             for (int y = 0; y < 32; ++y) acc[y] = 0.f;
+                            tmem_wait_ld();
                             for (int b = p.b0; b <= p.b1; b += 2) {       // two parts in flight
                                 float4 v[2][8];
                                 float f[2];
 #pragma unroll
                                 for (int k = 0; k < 2; ++k) {
-                                    f[k] = b + k <= p.b1 ? __ldcg(mine + at(b + k)) : -INFINITY;
+                                    const bool own = fresh && b + k == me, there = !own && b + k <= p.b1;
+                                    f[k] = own ? m * c : there ? __ldcg(mine + at(b + k)) : -INFINITY;
 #pragma unroll
                                     for (int y = 0; y < 8; ++y)
-                                        v[k][y] = b + k <= p.b1 ? __ldcg(reinterpret_cast<const float4 *>(a.part + at(b + k) + ((size_t)(x * 8 + y) * 256 + rr) * 4))
-                                                                : make_float4(0.f, 0.f, 0.f, 0.f);
+                                        v[k][y] = there ? __ldcg(reinterpret_cast<const float4 *>(a.part + at(b + k) + ((size_t)(x * 8 + y) * 256 + rr) * 4))
+                                                : own ? make_float4(__uint_as_float(o[y * 4]), __uint_as_float(o[y * 4 + 1]), __uint_as_float(o[y * 4 + 2]), __uint_as_float(o[y * 4 + 3]))
+                                                      : make_float4(0.f, 0.f, 0.f, 0.f);
                                 }
 #pragma unroll
                                 for (int k = 0; k < 2; ++k) {
@@ -556,6 +582,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                             }
                         }
                     }
+                    tc_fence_before();
                     meet();                                // last_flag is read before the next piece writes it
                 }
             }
