@@ -315,6 +315,52 @@ def test_attention_window_and_sinks(window, n_sink, new, total):
     _compare(q, k, v, table, cu, total, window, n_sink, max_new=1)
 
 
+@pytest.mark.parametrize("group,d", [(65, 128), (100, 64), (128, 128), (130, 64), (200, 128)])
+def test_attention_many_query_heads_per_kv_head(group, d):
+    """Up to 128 a tile holds whole tokens (one or two of them here); above that the warp-level kernel takes 64 rows a unit."""
+    b = _batch([1, 1, 1], [1, 90, 700], 2, group, d, 16, pad_rows=1)
+    _compare(*b)
+    b = _batch([3, 0, 9], [3, 0, 400], 1, group, d, 32, hnd=True)
+    _compare(*b)
+    _compare(*b, window=50, n_sink=2)
+
+
+@pytest.mark.parametrize("max_new", [1, 0])
+def test_attention_more_requests_than_fit_shared_memory(max_new):
+    """13,000 and 30,000 requests of one row each: the row's output is its own value."""
+    for B in (13000, 30000):
+        d = 64
+        k, v = _pool(1, B, 8, 1, d, False, seed=1)
+        q = torch.randn(B, 1, d, device=DEV).bfloat16()
+        out = torch.zeros_like(q)
+        table = torch.randperm(B, device=DEV).int()[:, None]
+        cu = torch.arange(B + 1, dtype=torch.int32, device=DEV)
+        cb.cb_paged_attention(q, out, cb.PagePool(k, v), 0, table, cu, torch.ones(B, dtype=torch.int32, device=DEV), 0.1, _workspace(d), max_new=max_new)
+        assert torch.equal(out, v[0, table[:, 0].long(), 0])
+
+
+def test_attention_no_rows_in_a_padded_batch():
+    q, k, v, table, cu, total = _batch([0, 0], [20, 0], 2, 4, 128, 16)
+    q = torch.full((5, 8, 128), float("nan"), dtype=torch.bfloat16, device=DEV)
+    for max_new in (1, 0):
+        out = torch.full_like(q, 5.0)
+        _attend(q, k, v, table, cu, total, max_new=max_new, out=out)
+        assert (out == 5).all()
+
+
+@pytest.mark.parametrize("new,total", [([1, 1, 1], [40, 300, 90]), ([70, 1, 90], [100, 300, 90])])
+def test_attention_strides_and_pages_outside_the_pool(new, total):
+    q, k, v, table, cu, total = _batch(new, total, 2, 5, 128, 16, wild=False)
+    k.nan_to_num_()
+    v.nan_to_num_()
+    wide = torch.full((len(new), table.shape[1] + 5), 3, dtype=torch.int32, device=DEV)
+    wide[:, : table.shape[1]] = table
+    table = wide[:, : table.shape[1]]                       # rows of a wider table
+    table[0, 1], table[1, 3], table[2, 0] = -5, k.shape[1], 2**31 - 1
+    heads = torch.randn(10, cu[-1], 128, device=DEV).bfloat16().transpose(0, 1)      # head-major queries
+    _compare(heads, k, v, table, cu, total)
+
+
 def test_attention_rows_that_see_nothing():
     # a cache shorter than the chunk: the first rows have negative positions
     q, k, v, table, cu, _ = _batch([6, 80, 3], [6, 80, 3], 2, 4, 128, 16)
@@ -398,6 +444,71 @@ def test_attention_time_out_is_reported_and_leaves_the_workspace_usable():
 
 
 # ---------------------------------------------------------------------------------------------------- together
+def test_a_decode_step_captured_once_and_replayed_as_requests_grow():
+    """Tables, rotation, store and attention in one graph; the host only rotates the free list between replays."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(21)
+    B, H, group, d, page, L = 3, 2, 8, 128, 8, 2
+    pages, cols, steps = 64, 12, 20
+    k, v = _pool(L, pages, page, H, d, False, fill=float("nan"))
+    pool = cb.PagePool(k, v)
+    lens = [5, 8, 15]
+    ids = torch.randperm(pages, generator=g, device=DEV).int()
+    table = torch.full((B, cols), -1, dtype=torch.int32, device=DEV)
+    table[0, :1], table[1, :1], table[2, :2] = ids[:1], ids[1:2], ids[2:4]
+    free = ids[4:].clone()
+    dense_k, dense_v = (torch.zeros(L, B, 15 + steps, H, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    for b, n in enumerate(lens):
+        j = torch.arange(n, device=DEV)
+        for x, y in ((k, dense_k), (v, dense_v)):
+            rows = torch.randn(L, n, H, d, generator=g, device=DEV).bfloat16()
+            x[:, table[b, j // page].long(), j % page] = rows
+            y[:, b, :n] = rows
+    room = B + 2                                            # two padded rows behind the batch
+    nk, nv = (torch.zeros(L, room, H, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    rk = torch.zeros_like(nk)
+    q = torch.zeros(1, room, H * group, d, dtype=torch.bfloat16, device=DEV)
+    rq, out = torch.zeros_like(q), torch.full((L, room, H * group, d), 5.0, dtype=torch.bfloat16, device=DEV)
+    cached, new = _i32(lens), _i32([1] * B)
+    cu, total, used = _i32([0] * (B + 1)), _i32([0] * B), _i32([0])
+    pos, slot = torch.zeros(1, room, dtype=torch.int32, device=DEV), torch.zeros(room, dtype=torch.int64, device=DEV)
+    ws = _workspace(d)
+
+    def step():
+        cb.cb_page_tables(cached, new, page, free, table, cu, total, pos[0], slot, used)
+        cb.cb_rope_axes(nk, rk, pos, [64], 1e6)
+        cb.cb_rope_axes(q, rq, pos, [64], 1e6)
+        cb.cb_paged_store(pool, rk, nv, slot)
+        for layer in range(L):
+            cb.cb_paged_attention(rq[0], out[layer], pool, layer, table, cu, total, d ** -0.5, ws, max_new=1)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        keep = table.clone()
+        step()                                              # warm-up; what it stored is stored again by the first replay
+        table.copy_(keep)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(steps):
+        for x in (nk, nv, q):
+            x.copy_(torch.randn(x.shape, generator=g, device=DEV).bfloat16())
+        graph.replay()
+        at = [n + i for n in lens]
+        assert pos[0].tolist() == at + [0, 0] and slot[B:].tolist() == [-1, -1]
+        for b in range(B):
+            dense_k[:, b, at[b]], dense_v[:, b, at[b]] = rk[:, b], nv[:, b]
+        for layer in range(L):
+            want, tol = ref.attention(rq[0], dense_k[layer], dense_v[layer], torch.arange(B, device=DEV)[:, None], cu.tolist(), total.tolist(), d ** -0.5)
+            assert ((out[layer, :B].double() - want[:B]).abs() <= tol[:B]).all()
+            assert (out[layer, B:] == 5).all()
+        free.copy_(free.roll(-int(used[0])))
+        cached.copy_(total)
+    cb.cb_last_device_status()
+
+
 def test_mapped_cache_into_pages_and_attention_over_it():
     """A fitted map's target cache is stored into pages, a chunk of new rows and then single tokens join it, and attention
     over the pages agrees with attention over the dense tensors."""
