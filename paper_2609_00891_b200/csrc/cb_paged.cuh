@@ -172,14 +172,16 @@ struct PaShare {
     int even;                // > 0: every pair takes this many places on the line, and no pair is split
 };
 
+struct alignas(16) PaSum { long long tiles; int units, most; };
+
 // All threads of the block.  `staged`: shared memory for the lengths (cap ints), free until the first tile is copied.
-// `sums`: [3 x warps].  Each thread counts the tiles of a run of consecutive units; one scan gives the line, one thread
+// `sums`: one per warp.  Each thread counts the tiles of a run of consecutive units; one scan gives the line, one thread
 // finds the block's start.
 // Where there are no more pairs than blocks and the longest one is at most EVEN tiles above an equal share, every pair goes
 // to a block of its own: joining two parts costs about that much (32 requests with a window of 1,024 keys, 256 pairs of 17
 // or 18 tiles of 64 keys: 38 us split, see k_paged_attn_few).
 template <int ROWS, int KT, int THREADS>
-__device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int cap, PaShare *share, long long *sums)
+__device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int cap, PaShare *share, PaSum *sums)
 {
     constexpr int EVEN = 4;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -228,19 +230,18 @@ __device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int
         if (lane >= o) { incl += up; incl_units += upu; }
         most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
     }
-    if (lane == 31) { sums[warp] = incl; sums[NWARP + warp] = incl_units; sums[2 * NWARP + warp] = most; }
+    if (lane == 31) sums[warp] = PaSum{incl, incl_units, most};
     __syncthreads();
     long long before = 0, all = 0;
     int before_units = 0, all_units = 0;
     most = 0;
 #pragma unroll
     for (int w = 0; w < NWARP; ++w) {
-        const long long s = sums[w];
-        const int su = (int)sums[NWARP + w];
-        if (w < warp) { before += s; before_units += su; }
-        all += s;
-        all_units += su;
-        most = max(most, (int)sums[2 * NWARP + w]);
+        const PaSum s = sums[w];
+        if (w < warp) { before += s.tiles; before_units += s.units; }
+        all += s.tiles;
+        all_units += s.units;
+        most = max(most, s.most);
     }
     long long line = all * a.Hkv;
     long long q = pa_div(line + gridDim.x - 1, gridDim.x);
@@ -256,21 +257,28 @@ __device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int
     }
     const long long begin = (long long)blockIdx.x * q;
     if (begin < line && begin >= pre && begin < pre + mine * a.Hkv) {
-        int b = b0;
-        for (int u = u0; u < u1; ++u) {
-            while (b + 1 < B && first_unit(b + 1) <= u) ++b;
-            if (!pa_unit<ROWS, KT>(a, cu, total, b, u - first_unit(b), un)) continue;
-            const long long len = (long long)(even ? even : un.n) * a.Hkv;
-            if (begin < pre + len) {
-                share->u = un;
-                share->unit_begin = pre;
-                share->q = q;
-                share->begin = begin;
-                share->end = begin + q < line ? begin + q : line;
-                share->even = even;
-                break;
+        auto found = [&]() {
+            share->u = un;
+            share->unit_begin = pre;
+            share->q = q;
+            share->begin = begin;
+            share->end = begin + q < line ? begin + q : line;
+            share->even = even;
+        };
+        if (per == 1) {                          // the thread's one unit is still at hand
+            found();
+        } else {
+            int b = b0;
+            for (int u = u0; u < u1; ++u) {
+                while (b + 1 < B && first_unit(b + 1) <= u) ++b;
+                if (!pa_unit<ROWS, KT>(a, cu, total, b, u - first_unit(b), un)) continue;
+                const long long len = (long long)(even ? even : un.n) * a.Hkv;
+                if (begin < pre + len) {
+                    found();
+                    break;
+                }
+                pre += len;
             }
-            pre += len;
         }
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the staged lengths' memory goes to the copies next

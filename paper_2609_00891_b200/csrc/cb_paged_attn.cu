@@ -74,14 +74,14 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
     float *stat_l = stat_m + 64;
     uint64_t *full = reinterpret_cast<uint64_t *>(stat_l + 64);
     uint64_t *empty = full + C::NS;
-    long long *warp_sums = reinterpret_cast<long long *>(empty + C::NS);
-    PaShare *share = reinterpret_cast<PaShare *>(warp_sums + 16);
+    PaSum *warp_sums = reinterpret_cast<PaSum *>(empty + C::NS);
+    PaShare *share = reinterpret_cast<PaShare *>(warp_sums + 5);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(share + 1);
     volatile int *last_flag = abort_flag + 2;
 
     const PagedArgs &a = P.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (tid == 0) {
+    if (tid == 128) {
         for (int i = 0; i < C::NS; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 4); }
         abort_flag[0] = 0;
         abort_flag[1] = (int)a.poll_limit;

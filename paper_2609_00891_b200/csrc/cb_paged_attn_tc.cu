@@ -86,8 +86,8 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
     uint64_t *o_full = p_ready + 4;        // [2] last product with V of a piece complete
     uint64_t *landed = o_full + 2;         // [NS] a V tile that has rows to clear: copied
     uint64_t *drain = landed + C::NS;
-    long long *warp_sums = reinterpret_cast<long long *>(drain + 1);
-    PaShare *share = reinterpret_cast<PaShare *>(warp_sums + 36);
+    PaSum *warp_sums = reinterpret_cast<PaSum *>(((uintptr_t)(drain + 1) + 15) & ~(uintptr_t)15);
+    PaShare *share = reinterpret_cast<PaShare *>(warp_sums + 12);
     using Walk = PaWalk<C::ROWS, C::KT>;
     TcPiece *info = reinterpret_cast<TcPiece *>(((uintptr_t)(share + 1) + 15) & ~(uintptr_t)15);   // [2]
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(info + 2);
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
 
     const PagedArgs &a = P.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (tid == 0) {
+    if (tid == 256) {
         for (int i = 0; i < C::NS; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&landed[i], 1); }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&q_full[i], 1);
