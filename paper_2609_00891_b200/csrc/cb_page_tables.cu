@@ -27,11 +27,28 @@ struct TablesArgs {
     int vector;               // positions and slot_map allow 16-byte stores
 };
 
+// The last i with at[i] <= e, for lanes whose e ascend (all 32 lanes): the first and last lane's by two votes each, on every
+// 32nd entry and on the 32 behind it, the others' by a search between those two, which are mostly the same request.
+__device__ __forceinline__ int locate(const unsigned *every32, const unsigned *at, unsigned e, int lane)
+{
+    auto vote = [&](unsigned x) {
+        const int g = __popc(__ballot_sync(0xffffffffu, every32[lane] <= x)) - 1;
+        return g * 32 + __popc(__ballot_sync(0xffffffffu, at[g * 32 + lane] <= x)) - 1;
+    };
+    int lo = vote(__shfl_sync(0xffffffffu, e, 0)), hi = vote(__shfl_sync(0xffffffffu, e, 31));
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (at[mid] <= e) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
 __global__ void __launch_bounds__(PT_THREADS) k_page_tables(const TablesArgs a)
 {
     __shared__ unsigned long long warp_sums[32];
     __shared__ unsigned row_at[PT_THREADS + 1], page_at[PT_THREADS + 1];   // within the group of requests
     __shared__ int s_cached[PT_THREADS], s_held[PT_THREADS];
+    __shared__ unsigned row_of_warp[32], page_of_warp[32];                // row_at and page_at of every 32nd request
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int ps1 = (1 << a.page_log2) - 1;
     const long long stride = (long long)gridDim.x * PT_THREADS, mine = (long long)blockIdx.x * PT_THREADS + tid;
@@ -58,6 +75,7 @@ __global__ void __launch_bounds__(PT_THREADS) k_page_tables(const TablesArgs a)
         const unsigned long long excl = before + incl - own;
         row_at[tid] = (unsigned)excl;
         page_at[tid] = (unsigned)(excl >> 32);
+        if (lane == 0) { row_of_warp[warp] = (unsigned)excl; page_of_warp[warp] = (unsigned)(excl >> 32); }
         s_cached[tid] = cached;
         s_held[tid] = held;
         if (tid == PT_THREADS - 1) { row_at[PT_THREADS] = (unsigned)(excl + own); page_at[PT_THREADS] = (unsigned)((excl + own) >> 32); }
@@ -68,27 +86,29 @@ __global__ void __launch_bounds__(PT_THREADS) k_page_tables(const TablesArgs a)
         __syncthreads();
         const unsigned n_rows = row_at[PT_THREADS], n_pages = page_at[PT_THREADS];
         // new pages: the e-th of the group belongs to the last request whose pages start at or before e
-        for (long long e = mine; e < n_pages; e += stride) {
-            int lo = 0, hi = PT_THREADS - 1;
-            while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (page_at[mid] <= e) lo = mid; else hi = mid - 1; }
-            const int col = s_held[lo] + (int)(e - page_at[lo]);
-            const long long f = pages0 + e;
-            if ((unsigned)col < (unsigned)a.cols) a.table[(long long)(b0 + lo) * a.table_stride + col] = f < a.n_free ? a.free_pages[f] : -1;
+        for (long long w0 = mine - lane; w0 < n_pages; w0 += stride) {
+            const unsigned e = min((unsigned)w0 + lane, n_pages - 1);
+            const int lo = locate(page_of_warp, page_at, e, lane);
+            if (w0 + lane < n_pages) {
+                const int col = s_held[lo] + (int)(e - page_at[lo]);
+                const long long f = pages0 + e;
+                if ((unsigned)col < (unsigned)a.cols) a.table[(long long)(b0 + lo) * a.table_stride + col] = f < a.n_free ? a.free_pages[f] : -1;
+            }
         }
         // rows, four neighbours a thread: one search for the four
         const long long end = min(rows0 + (long long)n_rows, a.n_rows);
-        for (long long t0 = rows0 / 4 * 4 + mine * 4; t0 < end; t0 += stride * 4) {
-            const long long first = max(t0, rows0);
-            unsigned e = (unsigned)(first - rows0);
-            int lo = 0, hi = PT_THREADS - 1;
-            while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (row_at[mid] <= e) lo = mid; else hi = mid - 1; }
+        for (long long w0 = rows0 / 4 * 4 + (mine - lane) * 4; w0 < end && rows0 < end; w0 += stride * 4) {
+            const long long t0 = w0 + lane * 4;
+            unsigned e = (unsigned)(min(max(t0, rows0), end - 1) - rows0);
+            int lo = locate(row_of_warp, row_at, e, lane);
+            if (t0 >= end) continue;
             int pos[4], page[4];
             const int *from[4];                       // where the row's page id stands
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 pos[k] = 0;
                 from[k] = nullptr;
-                if (t0 + k < first || t0 + k >= end) continue;
+                if (t0 + k < rows0 || t0 + k >= end) continue;
                 while (lo < PT_THREADS - 1 && row_at[lo + 1] <= e) ++lo;
                 pos[k] = s_cached[lo] + (int)(e - row_at[lo]);
                 const int col = pos[k] >> a.page_log2;
@@ -111,7 +131,7 @@ __global__ void __launch_bounds__(PT_THREADS) k_page_tables(const TablesArgs a)
             } else {
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    if (t0 + k >= first && t0 + k < end) {
+                    if (t0 + k >= rows0 && t0 + k < end) {
                         a.positions[t0 + k] = pos[k];
                         a.slot_map[t0 + k] = slot[k];
                     }
