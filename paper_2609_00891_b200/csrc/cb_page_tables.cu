@@ -103,25 +103,40 @@ __global__ void __launch_bounds__(PT_THREADS) k_page_tables(const TablesArgs a)
             int lo = locate(row_of_warp, row_at, e, lane);
             if (t0 >= end) continue;
             int pos[4], page[4];
-            const int *from[4];                       // where the row's page id stands
+            // where the page id of a request's position stands: its table for the pages it held, else the free list
+            auto source = [&](int request, int p) -> const int * {
+                const int col = p >> a.page_log2;
+                if ((unsigned)col >= (unsigned)a.cols) return nullptr;
+                if (col < s_held[request]) return a.table + (long long)(b0 + request) * a.table_stride + col;
+                const long long f = pages0 + page_at[request] + (col - s_held[request]);
+                return f < a.n_free ? a.free_pages + f : nullptr;
+            };
+            if (t0 >= rows0 && t0 + 4 <= end && row_at[lo + 1] - e >= 4) {
+                // four rows of one request: on one page or on two neighbours (a page has 8 rows or more)
+                const int p = s_cached[lo] + (int)(e - row_at[lo]);
+                const int *one = source(lo, p), *two = source(lo, p + 3);
+                const int id1 = one ? *one : -1, id2 = two ? *two : -1;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                pos[k] = 0;
-                from[k] = nullptr;
-                if (t0 + k < rows0 || t0 + k >= end) continue;
-                while (lo < PT_THREADS - 1 && row_at[lo + 1] <= e) ++lo;
-                pos[k] = s_cached[lo] + (int)(e - row_at[lo]);
-                const int col = pos[k] >> a.page_log2;
-                if ((unsigned)col < (unsigned)a.cols) {
-                    const long long f = pages0 + page_at[lo] + (col - s_held[lo]);
-                    if (col < s_held[lo]) from[k] = a.table + (long long)(b0 + lo) * a.table_stride + col;
-                    else if (f < a.n_free) from[k] = a.free_pages + f;
+                for (int k = 0; k < 4; ++k) {
+                    pos[k] = p + k;
+                    page[k] = ((p + k) >> a.page_log2) == (p >> a.page_log2) ? id1 : id2;
                 }
-                ++e;
+            } else {
+                const int *from[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    pos[k] = 0;
+                    from[k] = nullptr;
+                    if (t0 + k < rows0 || t0 + k >= end) continue;
+                    while (lo < PT_THREADS - 1 && row_at[lo + 1] <= e) ++lo;
+                    pos[k] = s_cached[lo] + (int)(e - row_at[lo]);
+                    from[k] = source(lo, pos[k]);
+                    ++e;
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) page[k] = from[k] ? *from[k] : -1;
             }
             long long slot[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) page[k] = from[k] ? *from[k] : -1;
 #pragma unroll
             for (int k = 0; k < 4; ++k) slot[k] = page[k] < 0 ? -1ll : ((long long)page[k] << a.page_log2) + (pos[k] & ps1);
             if (a.vector && t0 >= rows0 && t0 + 4 <= end) {
