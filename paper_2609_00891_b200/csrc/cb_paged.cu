@@ -63,6 +63,9 @@ cb_status cb_page_tables(const int32_t *cached_len, const int32_t *new_len, int3
     if ((((uintptr_t)cached_len | (uintptr_t)new_len | (uintptr_t)free_pages | (uintptr_t)block_table | (uintptr_t)cu_new |
           (uintptr_t)total_len | (uintptr_t)positions | (uintptr_t)pages_used) & 3) || ((uintptr_t)slot_map & 7))
         return CB_ERR_INVALID_ARG;
+    // every block reads the lengths while the first one writes its results
+    if (n_requests > 0 && (total_len == cached_len || total_len == new_len || cu_new == cached_len || cu_new == new_len || cu_new == total_len))
+        return CB_ERR_INVALID_ARG;
     const int lg = page_log2_of(page_size);
     if (lg < 0 || n_rows >= (1ll << 31)) return CB_ERR_UNSUPPORTED;
     if (const cudaError_t e = launch_page_tables(cached_len, new_len, n_requests, lg, free_pages, n_free, block_table, table_stride, max_pages,

@@ -41,7 +41,7 @@ def _tables(cached=0x100, new=0x200, B=3, ps=16, free=0x300, n_free=5, table=0x4
     (dict(B=0, cached=0, new=0, table=0, total=0), CUDA), (dict(B=-1), BAD), (dict(cached=0), BAD), (dict(new=0), BAD), (dict(table=0), BAD),
     (dict(total=0), BAD), (dict(cu=0), BAD), (dict(free=0), BAD), (dict(pos=0), BAD), (dict(slot=0), BAD), (dict(slot=0x804), BAD), (dict(pos=0x702), BAD),
     (dict(n_free=-1), BAD), (dict(rows=-1), BAD), (dict(cols=0), BAD), (dict(stride=7), BAD), (dict(ps=24), UNS), (dict(ps=0), UNS),
-    (dict(rows=1 << 31), UNS)])
+    (dict(rows=1 << 31), UNS), (dict(total=0x100), BAD), (dict(total=0x200), BAD), (dict(cu=0x100), BAD), (dict(cu=0x600), BAD)])
 def test_page_tables(change, want):
     assert _tables(**change) == want
 
