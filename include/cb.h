@@ -430,7 +430,8 @@ cb_status cb_rank_layers(const float *scores, int32_t Lt, int32_t Ls, int32_t k,
  *     cb_rope_axes        rotary embedding with several position axes (queries, new keys)
  *     cb_paged_store      rows of a mapped cache (cb_apply*'s output) or of a step's new keys and values into their pages
  *     cb_paged_attention  attention of the new rows of every request over its pages
- * All lengths are read from device memory, so a step can be captured into a CUDA graph once and replayed as requests grow.
+ * All lengths are read from device memory, so a step can be captured into a CUDA graph once and replayed as requests grow
+ * (make the first call of each on a device outside any capture: it loads the kernel).
  * Every tensor of a call lives on the current device.
  *
  * cb_page_pool: K and V of all layers in pages of page_size rows.  Element (layer, page, slot, head, c) is at
@@ -500,7 +501,7 @@ cb_status cb_rope_axes(const void *x, void *out, int32_t n_layers, int32_t n_hea
  * Attention of new rows over one layer of a paged cache.  Request b owns rows [cu_new[b], cu_new[b+1]) of q and out
  * (bf16, row t of query head h at t*stride_token + h*stride_head, multiples of 8, a stride of 0 only on a dimension of
  * size 1, 16-byte aligned; q and out must not overlap); they are the LAST
- * rows of its total_len[b] rows in the cache (their own keys and values are stored already), so row i of the request has
+ * rows of its total_len[b] (below 2^31 - 256) rows in the cache (their own keys and values are stored already), so row i of the request has
  * position p = total_len - new + i, and
  *     out = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale q . k_j)   over the keys j <= p with
  *     window == 0  or  p - j < window  or  j < n_sink

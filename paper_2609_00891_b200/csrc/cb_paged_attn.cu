@@ -126,10 +126,8 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
                 more = !dead && w.next(a);
             }
             // after a time-out the copies in flight land before the block ends
-            for (int i = dead ? min(issued, C::NS) : 0; i > 0; --i) {
-                mbar_wait_suspended_warp(&full[st.idx], st.phase ^ 1, abort_flag);
-                st.next();
-            }
+            for (int k = 0; dead && k < min(issued, C::NS); ++k)
+                mbar_wait_suspended_warp(&full[k], ((issued - k - 1) / C::NS) & 1, abort_flag);
         }
     } else if (any) {
         // ================================ consumers ================================

@@ -168,10 +168,8 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                 more = !dead && w.next(a);
             }
             // after a time-out the copies in flight land before the block ends
-            for (int k = dead ? min(issued, C::NS) : 0; k > 0; --k) {
-                mbar_wait_suspended_warp(&full[st.idx], st.phase ^ 1, abort_flag);
-                st.next();
-            }
+            for (int k = 0; dead && k < min(issued, C::NS); ++k)
+                mbar_wait_suspended_warp(&full[k], ((issued - k - 1) / C::NS) & 1, abort_flag);
         }
     } else if (warp == 10) {
         // ================================ clears rows of V tiles ================================
