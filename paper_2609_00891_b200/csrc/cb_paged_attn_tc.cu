@@ -1,19 +1,24 @@
 // Attention of chunks of new rows over a paged cache on the tensor cores (tcgen05): the same sum as cb_paged_attn.cu for
-// more than 64 flattened rows per request and KV head, where the products bound the time.
+// more than 16 flattened rows per request and KV head.
 //
-// A unit is 256 flattened rows (new rows x the query heads of a KV head) as two tiles of 128, which share every key tile
+// A unit is two tiles of up to 128 flattened rows (whole tokens x the query heads of a KV head), which share every key tile
 // of 128 keys.  Per thread block:
 //   producer warp    TMA, one box per page and 64-channel half, ring of K and V tiles (a page id outside the pool reads as
 //                    zeros).
 //   clearing warp    rows of a V tile that no row of the unit sees may hold anything and 0 * NaN is NaN: a tile that has
 //                    such rows lands on a barrier of its own, and this warp sets them to zero before it hands it on.
-//   MMA thread       S_i = Q_i K^T into tensor memory, then O_i += P_i V with P_i read from tensor memory, i = 0, 1 in
+//   piece warp       describes the next piece to the softmax warps and copies its query tiles, one piece ahead.
+//   MMA warp         S_i = Q_i K^T into tensor memory, then O_i += P_i V with P_i read from tensor memory, i = 0, 1 in
 //                    turn: while the softmax warps work on one tile the tensor cores work on the other.
 //   2 x 4 softmax warps   one thread per row: scores to registers, running maximum, exp2, weights as bf16 back over the
 //                    scores in tensor memory.  The output is rescaled only when a maximum grows by more than 2^8 (weights
 //                    stay below 2^8, sums and outputs are fp32), which after the first tiles is hardly ever.
-// The tensor pipe runs a thread's products in order, so that S_i of the next tile may overwrite P_i, and its completion
-// also says that P_i V of the tile before is complete.
+// The tensor pipe runs a warp's products in order, so that S_i of the next tile may overwrite P_i, and its completion also
+// says that P_i V of the tile before is complete.
+// Bound by the two tiles taking turns: ~3,100 cycles for 128 keys of both, of which the products run 2,048 and the
+// special-function unit 2,048; on long runs by the board's power limit.  Measured, 64 query heads of 128 on 8 KV heads:
+// 4,096 rows over 16,384 keys 1.6 - 1.75 ms = 1.1 - 1.2 PFLOP/s; 8,192 rows of a prompt 1.3 ms; 16 requests of 16 rows over
+// 8,192 keys 115 us (4.7 TB/s).
 #include "cb_paged.cuh"
 #include "cb_ptx.cuh"
 #include "cb_math.cuh"
@@ -31,6 +36,10 @@ struct TcAttnCfg {
     static constexpr int NS = D == 128 ? 5 : 10;           // K and V tiles in flight
     static constexpr int THREADS = 384;
     static constexpr int TMEM_COLS = 512;                  // S0, S1: 128 columns each, then O0, O1: D columns each
+    // Quarters of a tile's weights that are handed on first, so that their product runs while the rest is computed.  Prefill of
+    // 8,192 rows, three quarters against two: 64 channels 1,048 / 1,087 us, 128 channels 1,295 / 1,299 us alone and 1,700 /
+    // 1,610 us for the chunk of 4,096 rows over 16,384 keys under the power limit.
+    static constexpr int FIRST = D == 64 ? 3 : 2;
     static constexpr size_t SMEM = 1024 + 2 * (size_t)TILE + (size_t)NS * TILE + 1280;
     static constexpr int REC = 256 * (D + 2);              // floats of a partial record: [D / 4][256 rows][4], maxima, sums
 };
@@ -82,7 +91,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
     uint64_t *info_empty = info_full + 2;  // [2] read by the 8 softmax warps
     uint64_t *joined = info_empty + 2;     // [2] barrier among a tile's 4 softmax warps
     uint64_t *s_full = joined + 2;         // [2] scores complete
-    uint64_t *p_ready = s_full + 2;        // [2][2] weights of the first and second 64 keys written (4 warps)
+    uint64_t *p_ready = s_full + 2;        // [2][2] weights of the first keys and of the rest written (4 warps)
     uint64_t *o_full = p_ready + 4;        // [2] last product with V of a piece complete
     uint64_t *landed = o_full + 2;         // [NS] a V tile that has rows to clear: copied
     uint64_t *drain = landed + C::NS;
@@ -271,12 +280,12 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                 }
                 __syncwarp();
             };
-            // 64 keys of the tile; `first`: nothing is in the output yet
+            // the part of the tile's keys that is handed on first, or the rest; `first`: nothing is in the output yet
             auto values = [&](int i, uint32_t stage, int half, uint32_t first) {
                 const uint64_t vd = proto_v | (uint64_t)(kv_addr + __shfl_sync(0xffffffffu, stage, 0) * (C::TILE >> 4));
                 if (leader) {
 #pragma unroll
-                    for (int k = 4 * half; k < 4 * half + 4; ++k)
+                    for (int k = half ? 2 * C::FIRST : 0; k < (half ? 8 : 2 * C::FIRST); ++k)
                         umma_bf16_ts(tm + 256 + i * D, tm + i * 128 + k * 8, vd + k * 128, idesc_o, k == 0 ? 1u - first : 1u);
                 }
                 __syncwarp();
@@ -421,7 +430,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
 #pragma unroll
-                        for (int x = 2 * half; x < 2 * half + 2; ++x) {
+                        for (int x = half ? C::FIRST : 0; x < (half ? 4 : C::FIRST); ++x) {
                             uint32_t p[16];
 #pragma unroll
                             for (int y = 0; y < 16; ++y) {
