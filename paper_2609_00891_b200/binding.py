@@ -663,10 +663,11 @@ class PagePool:
     __slots__ = ("k", "v", "n_layers", "n_heads", "head_dim", "page_size", "n_pages", "c")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
-        sl, sp, ss, sh, sc = k.stride()
-        L, N, S, H, d = k.shape
-        assert k.dtype == v.dtype == torch.bfloat16 and k.shape == v.shape and v.stride() == (sl, sp, ss, sh, sc) and sc == 1
-        assert k.device == v.device
+        strides, shape, bf16 = k.stride(), k.shape, torch.bfloat16
+        sl, sp, ss, sh, sc = strides
+        L, N, S, H, d = shape
+        assert k.dtype is bf16 and v.dtype is bf16 and v.shape == shape and v.stride() == strides and sc == 1
+        assert k.get_device() == v.get_device()
         self.k, self.v = k, v
         self.n_layers, self.n_pages, self.page_size, self.n_heads, self.head_dim = L, N, S, H, d
         self.c = _PAGE_POOL.pack(k.data_ptr(), v.data_ptr(), L, H, d, S, N, sl, sp, ss, sh)
@@ -699,12 +700,13 @@ def cb_page_tables(cached_len: torch.Tensor, new_len: torch.Tensor, page_size: i
     block_table [B][max_pages] is completed in place, cu_new [B + 1], total_len [B], positions and slot_map [rows]."""
     B, rows = cached_len.numel(), positions.numel()
     used = free_pages if pages_used is None else pages_used
+    i32 = torch.int32
     for t in (cached_len, new_len, free_pages, cu_new, total_len, positions, used):
-        assert t.dtype == torch.int32 and t.is_contiguous()
-    assert slot_map.dtype == torch.int64 and slot_map.is_contiguous() and slot_map.numel() == rows
+        assert t.dtype is i32 and t.is_contiguous()
+    assert slot_map.dtype is torch.int64 and slot_map.is_contiguous() and slot_map.numel() == rows
     assert new_len.numel() == B and total_len.numel() == B and cu_new.numel() == B + 1 and (pages_used is None or used.numel() >= 1)
     n, cols = block_table.shape
-    assert block_table.dtype == torch.int32 and n == B and (cols <= 1 or block_table.stride(1) == 1)
+    assert block_table.dtype is i32 and n == B and (cols <= 1 or block_table.stride(1) == 1)
     st = _on_one_device(stream, cu_new, cached_len, new_len, free_pages, block_table, total_len, positions, slot_map, used)
     _check(lib().cb_page_tables(cached_len.data_ptr(), new_len.data_ptr(), B, page_size, free_pages.data_ptr(), free_pages.numel(),
                                 block_table.data_ptr(), block_table.stride(0), cols, cu_new.data_ptr(), total_len.data_ptr(),

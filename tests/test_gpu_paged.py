@@ -426,6 +426,28 @@ def test_attention_on_another_stream_and_in_a_graph_whose_lengths_grow():
         assert ((out.double() - want).abs() <= tol).all()
 
 
+def test_attention_two_calls_at_once():
+    """Two streams with a workspace each, both kernels in flight together, against the same calls one after the other."""
+    one = _batch([1, 1, 1], [9000, 700, 50], 2, 8, 128, 16, seed=1)
+    two = _batch([200, 90], [5000, 90], 2, 4, 128, 32, seed=2)
+    calls = []
+    for q, k, v, table, cu, total in (one, two):
+        ws = torch.zeros(cb.cb_paged_attention_workspace_bytes(128), dtype=torch.uint8, device=DEV)
+        args = (cb.PagePool(k, v), 0, table, _i32(cu), _i32(total), 128 ** -0.5, ws)
+        want = torch.empty(q.shape, dtype=torch.bfloat16, device=DEV)
+        cb.cb_paged_attention(q, want, *args, max_new=cu[1])
+        calls.append((q, args, want, cu[1], torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    outs = [[torch.empty_like(c[2]) for _ in range(20)] for c in calls]
+    for i in range(20):
+        for c, out in zip(calls, outs):
+            cb.cb_paged_attention(c[0], out[i], *c[1], max_new=c[3], stream=c[4])
+    torch.cuda.synchronize()
+    for c, out in zip(calls, outs):
+        assert all(torch.equal(o, c[2]) for o in out)
+    cb.cb_last_device_status()
+
+
 def test_attention_time_out_is_reported_and_leaves_the_workspace_usable():
     b = _batch([1, 1, 70], [3000, 100, 70], 1, 4, 128, 16)
     want = _compare(*b)
