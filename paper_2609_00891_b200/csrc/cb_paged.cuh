@@ -338,6 +338,14 @@ struct PaWalk {
     __device__ __forceinline__ int record(int c) const { return 2 * c + (pair_begin <= (long long)c * q ? 0 : 1); }
 };
 
+// One more part of a pair is in memory (the writes of the threads that met this one before count as its own); how many
+// there were before, whose writes are visible from here on.
+__device__ __forceinline__ int pa_arrive(int *counter)
+{
+    int n;
+    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(n) : "l"(counter) : "memory");
+    return n;
+}
 __device__ __forceinline__ float pa_exp2(float x)
 {
     float r;

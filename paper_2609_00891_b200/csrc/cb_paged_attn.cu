@@ -10,8 +10,8 @@
 //                   entry can make the copy fault.
 //   4 consumer warps   a warp owns 16 rows and 64 MT / 4 keys of a tile and carries its own running maximum, sum and
 //                   output, so that the main loop has no barrier between warps; they are joined at the end of a piece.
-// Measured: 64 requests of 512 to 8,192 keys, 8 KV heads x 8 query heads x 128: 213 us for 1.30 GB = 6.1 TB/s; one request
-// of 1,024 keys 13 us, of which the launch and the schedule take 4, the copies 2, the tiles 1.5, the joins 3.
+// Measured: 64 requests of 512 to 8,192 keys, 8 KV heads x 8 query heads x 128: 205 us for 1.30 GB = 6.3 TB/s; one request
+// of 1,024 keys 9.5 us in a graph, of which the schedule takes 2, the copies 1.3, the tiles 1.5, the joins 3.
 // A wait that runs out is not followed by another one: the block runs through to its end, so that every barrier and join
 // counter is served as in a good run, and sets the status word; its rows are then not valid.
 // Scores, maxima, sums and outputs are fp32; the weights exp2(s - m) are rounded to bf16 for the product with V, which is
@@ -57,7 +57,7 @@ __device__ __forceinline__ void ldsm_x4(uint32_t addr, uint32_t (&r)[4])
 }
 __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -183,12 +183,18 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
                     const int pg = key >> box_log2, rr = key & ((1 << box_log2) - 1);
                     const uint32_t row = kb + ((uint32_t)(pg * C::NB) << (box_log2 + 7)) + rr * 128;
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        uint32_t b[4];
-                        const int ch = (k & 3) * 2 + k_ch;
-                        ldsm_x4(row + ((uint32_t)(k >> 2) << (box_log2 + 7)) + (uint32_t)((ch ^ (rr & 7)) << 4), b);
-                        mma_16816(s[2 * n], qf[k], b[0], b[1]);
-                        mma_16816(s[2 * n + 1], qf[k], b[2], b[3]);
+                    for (int k0 = 0; k0 < D / 16; k0 += 4) {
+                        uint32_t b[4][4];                  // four loads in flight before the products that need them
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int ch = k * 2 + k_ch;
+                            ldsm_x4(row + ((uint32_t)(k0 >> 2) << (box_log2 + 7)) + (uint32_t)((ch ^ (rr & 7)) << 4), b[k]);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            mma_16816(s[2 * n], qf[k0 + k], b[k][0], b[k][1]);
+                            mma_16816(s[2 * n + 1], qf[k0 + k], b[k][2], b[k][3]);
+                        }
                     }
                 }
                 const int j0 = pa_tile(u, t) * C::KT + ks * C::WK;
@@ -250,12 +256,18 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
                         }
                     }
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        uint32_t b[4];
-                        const int ch = (k & 3) * 2 + v_ch;
-                        ldmatrix_x4_trans(row + ((uint32_t)(k >> 2) << (box_log2 + 7)) + (uint32_t)((ch ^ (rr & 7)) << 4), b);
-                        mma_16816(o[2 * k], pf[n], b[0] & keep[0], b[1] & keep[1]);
-                        mma_16816(o[2 * k + 1], pf[n], b[2] & keep[0], b[3] & keep[1]);
+                    for (int k0 = 0; k0 < D / 16; k0 += 4) {
+                        uint32_t b[4][4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int ch = k * 2 + v_ch;
+                            ldmatrix_x4_trans(row + ((uint32_t)(k0 >> 2) << (box_log2 + 7)) + (uint32_t)((ch ^ (rr & 7)) << 4), b[k]);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            mma_16816(o[2 * (k0 + k)], pf[n], b[k][0] & keep[0], b[k][1] & keep[1]);
+                            mma_16816(o[2 * (k0 + k) + 1], pf[n], b[k][2] & keep[0], b[k][3] & keep[1]);
+                        }
                     }
                 }
                 __syncwarp();
@@ -346,11 +358,8 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
                 const int b0 = w.first_block(), b1 = w.last_block();
                 bar_consumers();
                 if (tid == 0) {
-                    __threadfence();
-                    const int n = atomicAdd(&a.counters[b0], 1);
-                    const int last = n == b1 - b0;
+                    const int last = pa_arrive(&a.counters[b0]) == b1 - b0;
                     if (last) a.counters[b0] = 0;
-                    __threadfence();
                     *last_flag = last;
                 }
                 bar_consumers();

@@ -514,11 +514,8 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                         rec[256 * D + 256 + rr] = l;
                         meet();
                         if (r == 0) {
-                            __threadfence();
-                            const int k = atomicAdd(counter, 1);
-                            const int last = k == p.b1 - p.b0;
+                            const int last = pa_arrive(counter) == p.b1 - p.b0;
                             if (last) *counter = 0;
-                            __threadfence();
                             last_flag[i] = last;
                         }
                         meet();
