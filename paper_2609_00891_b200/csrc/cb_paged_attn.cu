@@ -15,7 +15,7 @@
 // A wait that runs out is not followed by another one: the block runs through to its end, so that every barrier and join
 // counter is served as in a good run, and sets the status word; its rows are then not valid.
 // Scores, maxima, sums and outputs are fp32; the weights exp2(s - m) are rounded to bf16 for the product with V, which is
-// bf16 as well (relative 2^-9 per weight, of the size of the output's own rounding).
+// bf16 as well (at most 2^-8 of each weight, as the output's own rounding).
 #include "cb_paged.cuh"
 #include "cb_ptx.cuh"
 #include "cb_math.cuh"
