@@ -676,14 +676,14 @@ class PagePool:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
-def _on_one_device(stream, *tensors) -> int:
+def _on_one_device(stream, first, *others) -> int:
     """All tensors on one CUDA device, and that the current one (a launch goes to the current device); the stream handle."""
-    dev = tensors[0].get_device()
-    for t in tensors:
+    dev = first.get_device()
+    for t in others:
         if t.get_device() != dev:
-            dev = -1
+            raise ValueError("all tensors of a call must be on one CUDA device")
     if dev < 0:
-        raise ValueError("all tensors of a call must be on one CUDA device")
+        raise ValueError("the tensors of a call must be on a CUDA device")
     if dev != torch.cuda.current_device():
         raise ValueError("the tensors' device must be the current device")
     if stream is None:
@@ -700,13 +700,12 @@ def cb_page_tables(cached_len: torch.Tensor, new_len: torch.Tensor, page_size: i
     block_table [B][max_pages] is completed in place, cu_new [B + 1], total_len [B], positions and slot_map [rows]."""
     B, rows = cached_len.numel(), positions.numel()
     used = free_pages if pages_used is None else pages_used
-    i32 = torch.int32
-    for t in (cached_len, new_len, free_pages, cu_new, total_len, positions, used):
-        assert t.dtype is i32 and t.is_contiguous()
-    assert slot_map.dtype is torch.int64 and slot_map.is_contiguous() and slot_map.numel() == rows
-    assert new_len.numel() == B and total_len.numel() == B and cu_new.numel() == B + 1 and (pages_used is None or used.numel() >= 1)
     n, cols = block_table.shape
-    assert block_table.dtype is i32 and n == B and (cols <= 1 or block_table.stride(1) == 1)
+    for t in (cached_len, new_len, free_pages, cu_new, total_len, positions, used):
+        assert t.dtype is torch.int32 and t.is_contiguous()
+    assert slot_map.dtype is torch.int64 and slot_map.is_contiguous() and slot_map.numel() == rows
+    assert new_len.numel() == B and total_len.numel() == B and cu_new.numel() == B + 1 and used.numel() >= (pages_used is not None)
+    assert block_table.dtype is torch.int32 and n == B and (cols <= 1 or block_table.stride(1) == 1)
     st = _on_one_device(stream, cu_new, cached_len, new_len, free_pages, block_table, total_len, positions, slot_map, used)
     _check(lib().cb_page_tables(cached_len.data_ptr(), new_len.data_ptr(), B, page_size, free_pages.data_ptr(), free_pages.numel(),
                                 block_table.data_ptr(), block_table.stride(0), cols, cu_new.data_ptr(), total_len.data_ptr(),

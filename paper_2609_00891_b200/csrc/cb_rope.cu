@@ -75,7 +75,7 @@ cudaError_t launch_rope_rotate(void *k, int L, int H, int d, long long T, long l
 // heads of 128 channels in 47 us (5.7 TB/s); 51 us when every thread held the angles of eight pairs in registers and
 // streamed eight heads, 53 us with eight pieces in flight and fewer blocks.
 // Angles are turns in 0.64 fixed point: pos * f modulo 2^64 is exact for every 32-bit position, so the angle is off by
-// at most pos * 2^-56 turns (the frequency's own rounding from double) plus the 2^-24 turns of the sine's argument.
+// at most pos * 2^-56 turns (the frequency's own rounding) plus the 2^-24 turns of the sine's argument.
 struct RopeAxesArgs {
     const __nv_bfloat16 *x;
     __nv_bfloat16 *out;
@@ -157,10 +157,13 @@ cudaError_t launch_rope_axes(const void *x, void *out, int L, int H, int d, long
     a.x_sl = xs[0]; a.x_st = xs[1]; a.x_sh = xs[2];
     a.o_sl = os[0]; a.o_st = os[1]; a.o_sh = os[2];
     a.H = H; a.LH = L * H; a.T = T; a.pos = positions; a.axis_stride = axis_stride; a.inverse = inverse;
+    // one power and then products in extended precision (64 powers took 3 us a call, as long as the launch)
+    const long double ratio = powl((long double)base, -2.0L / (long double)d);
+    long double turns = 1.0L / 6.283185307179586476925286766559L;
     for (int i = 0; i < ROPE_MAX_FREQ; ++i) {
         a.axis[i] = i < d / 2 ? axis_of_pair[i] : 0;
-        const double turns = i < d / 2 ? pow(base, -2.0 * (double)i / (double)d) / 6.283185307179586476925286766559 : 0.0;
-        a.f[i] = (unsigned long long)ldexp(turns, 64);          // turns < 0.16: no wrap
+        a.f[i] = i < d / 2 ? (unsigned long long)(turns * 18446744073709551616.0L) : 0ull;   // turns < 0.16: no wrap
+        turns *= ratio;
     }
     const long long rows = 512 / d, blocks = (T + rows - 1) / rows;
     // at most 64 (layer, head) pairs a block (one round of loads), fewer where that leaves SMs without a block
