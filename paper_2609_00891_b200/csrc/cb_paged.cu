@@ -198,6 +198,7 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
     a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + PA_COUNTER_BYTES);
     s = launch_state(a);
     if (s != CB_OK) return s;
+    if (device_sm_count() * 8 > PA_COUNTERS) return CB_ERR_UNSUPPORTED;
     if (max_new == 0 || max_new > n_rows) max_new = (int32_t)n_rows;
     const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(pool->k) + layer * pool->stride_layer;
     const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(pool->v) + layer * pool->stride_layer;

@@ -11,8 +11,8 @@
 
 namespace cb {
 
-constexpr int PA_MAX_GRID = 1024;            // blocks of an attention launch (counters in the workspace)
-constexpr size_t PA_COUNTER_BYTES = PA_MAX_GRID * sizeof(int);
+constexpr int PA_COUNTERS = 2048;            // one per block (warp-level kernel), eight per block (two tiles of four warps)
+constexpr size_t PA_COUNTER_BYTES = PA_COUNTERS * sizeof(int);
 
 struct PagedArgs {
     const __nv_bfloat16 *q;
@@ -34,7 +34,7 @@ struct PagedArgs {
     float scale_log2;                        // softmax scale times log2(e)
     int q_min;                               // least tiles a block takes
     float *part;                             // partial results of split pairs, two records per block
-    int *counters;                           // [PA_MAX_GRID], zero between calls
+    int *counters;                           // [PA_COUNTERS], zero between calls
     int *status;
     unsigned poll_limit;
     int starve;

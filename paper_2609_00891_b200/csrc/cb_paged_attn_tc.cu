@@ -89,8 +89,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
     uint64_t *q_empty = q_full + 2;        // [2] its last scores of a piece complete
     uint64_t *info_full = q_empty + 2;     // [2] a piece's description written
     uint64_t *info_empty = info_full + 2;  // [2] read by the 8 softmax warps
-    uint64_t *joined = info_empty + 2;     // [2] barrier among a tile's 4 softmax warps
-    uint64_t *s_full = joined + 2;         // [2] scores complete
+    uint64_t *s_full = info_empty + 2;         // [2] scores complete
     uint64_t *p_ready = s_full + 2;        // [2][2] weights of the first keys and of the rest written (4 warps)
     uint64_t *o_full = p_ready + 4;        // [2] last product with V of a piece complete
     uint64_t *landed = o_full + 2;         // [NS] a V tile that has rows to clear: copied
@@ -101,7 +100,6 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
     TcPiece *info = reinterpret_cast<TcPiece *>(((uintptr_t)(share + 1) + 15) & ~(uintptr_t)15);   // [2]
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(info + 2);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    volatile int *last_flag = abort_flag + 2;               // [2]
 
     const PagedArgs &a = P.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -112,7 +110,6 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
             mbar_init(&q_empty[i], 1);
             mbar_init(&info_full[i], 1);
             mbar_init(&info_empty[i], 8);
-            mbar_init(&joined[i], 4);
             mbar_init(&s_full[i], 1);
             mbar_init(&p_ready[2 * i], 4);
             mbar_init(&p_ready[2 * i + 1], 4);
@@ -353,20 +350,20 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
         const uint32_t s_tm = tmem + i * 128 + lanes, o_tm = tmem + 256 + i * D + lanes;
         const float c = a.scale_log2;
         const uint64_t cc = f2_pack(c, c);
-        uint32_t ns = 0, no = 0, nj = 0;
+        uint32_t ns = 0, no = 0;
         auto settle = [&](int tile, uint32_t from) {
             Walk w;
             bool more = w.open(a, *share);
             for (uint32_t k = 0; more; ++k, more = w.next(a))
                 if (k >= from && !w.whole() && tile * RT < w.u.rows) {
-                    int *counter = &a.counters[2 * w.first_block() + tile];
-                    if (atomicAdd(counter, 1) == w.last_block() - w.first_block()) *counter = 0;
+                    int *counter = &a.counters[(2 * w.first_block() + tile) * 4 + (warp & 3)];
+                    if (pa_arrive(counter) == w.last_block() - w.first_block()) *counter = 0;
                 }
         };
         for (uint32_t n = 0; any; ++n) {
             if (!mbar_wait_suspended_warp(&info_full[n & 1], (n >> 1) & 1, abort_flag)) {
                 // time-out: the parts that this block will not write still count, or the next call would wait for them
-                if (r == 0) settle(i, n);
+                if (lane == 0) settle(i, n);
                 break;
             }
             const TcPiece p = info[n & 1];
@@ -480,23 +477,13 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                     }
                     tc_fence_before();
                 } else {
-                    auto meet = [&]() {                    // the tile's four warps
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&joined[i]);
-                        if (!dead && !mbar_wait_suspended_warp(&joined[i], nj & 1, abort_flag)) dead = true;
-                        ++nj;
-                    };
-                    int *counter = &a.counters[2 * p.b0 + i];
-                    // The block that has the last part of the pair joins all of them, in block order.  A block's first piece
-                    // ends a pair that the block before it finishes last, so that the other parts are mostly there already:
-                    // then this part stays in tensor memory and is joined from there.
-                    if (r == 0) {
-                        const int k = ld_acquire(counter);
-                        if (k == p.b1 - p.b0) *counter = 0;
-                        last_flag[i] = k == p.b1 - p.b0;
-                    }
-                    meet();
-                    bool join = last_flag[i];
+                    // Rows of a warp are joined by the warp that has their last part, of any block, in block order: no warp waits
+                    // for another.  A block's first piece ends a pair that the block before it finishes last, so that the
+                    // other parts are mostly there already: then this part stays in tensor memory and is joined from there.
+                    int *counter = &a.counters[(2 * p.b0 + i) * 4 + (warp & 3)];
+                    int there_are = 0;
+                    if (lane == 0) there_are = ld_acquire(counter);
+                    bool join = __shfl_sync(0xffffffffu, there_are, 0) == p.b1 - p.b0;
                     const bool fresh = join;               // this block's part is not in memory
                     if (!fresh) {
                         float *rec = a.part + (size_t)p.rec * C::REC;
@@ -512,16 +499,13 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                         }
                         rec[256 * D + rr] = m * c;         // c > 0: -inf stays -inf
                         rec[256 * D + 256 + rr] = l;
-                        meet();
-                        if (r == 0) {
-                            const int last = pa_arrive(counter) == p.b1 - p.b0;
-                            if (last) *counter = 0;
-                            last_flag[i] = last;
-                        }
-                        meet();
-                        join = last_flag[i];
+                        __syncwarp();
+                        if (lane == 0) there_are = pa_arrive(counter);
+                        join = __shfl_sync(0xffffffffu, there_are, 0) == p.b1 - p.b0;
                     }
                     if (join) {
+                        __syncwarp();                      // what lane 0 acquired is every lane's
+                        if (lane == 0) *counter = 0;
                         const int me = (int)blockIdx.x;
                         const float *mine = a.part + 256 * D + rr;
                         auto at = [&](int b) { return (size_t)(b == p.b0 ? p.rec0 : 2 * b) * C::REC; };
@@ -587,7 +571,6 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                         }
                     }
                     tc_fence_before();
-                    meet();                                // last_flag is read before the next piece writes it
                 }
             }
         }

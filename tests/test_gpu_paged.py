@@ -268,7 +268,7 @@ def _compare(q, k, v, table, cu, total, window=0, n_sink=0, max_new=None, layer=
     assert not bad.any(), (int(bad.sum()), err.max().item(), bad.nonzero()[:4].tolist())
     assert (out[n:] == 5).all()
     cb.cb_last_device_status()
-    assert int(_workspace(q.shape[2])[:4096].sum()) == 0            # the join counters are ready for the next call
+    assert int(_workspace(q.shape[2])[:8192].sum()) == 0            # the join counters are ready for the next call
     return out
 
 
