@@ -550,9 +550,11 @@ int32_t cb_last_cuda_error(const char **text);
 /*
  * TEST HOOK, not for production use (the paper has no counterpart).  Affects every later launch of this process:
  * poll_limit > 0 shortens the number of polls after which a bounded device-side wait gives up (0 restores the
- * default of 2^22); starve_producer != 0 makes the source-tile producer of the statistics kernel (d = 128) and of
- * the apply kernel issue no copies at all, so that every consumer's bounded wait runs out, the blocks tear down by
- * themselves and the status word reads CB_ERR_TIMEOUT.  Nothing faults, traps or spins without a limit.
+ * default of 2^22); starve_producer == 1 makes the tile producer of the statistics kernel (d = 128), of the apply
+ * kernel and of the paged attention issue no copies at all, so that every consumer's bounded wait runs out, the blocks
+ * tear down by themselves and the status word reads CB_ERR_TIMEOUT; 2 starves nobody, but some consumers of the paged
+ * attention take their first wait as run out while the copies go on (other kernels run as ever).  Nothing faults, traps
+ * or spins without a limit.
  */
 cb_status cb_test_hooks(uint32_t poll_limit, int32_t starve_producer);
 

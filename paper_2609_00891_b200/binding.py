@@ -771,8 +771,9 @@ def cb_last_device_status(stream=None) -> None:
     _check(lib().cb_last_device_status(_stream_ptr(stream)), "cb_last_device_status")
 
 
-def cb_test_hooks(poll_limit: int = 0, starve_producer: bool = False) -> None:
-    _check(lib().cb_test_hooks(ctypes.c_uint32(poll_limit), ctypes.c_int32(1 if starve_producer else 0)), "cb_test_hooks")
+def cb_test_hooks(poll_limit: int = 0, starve_producer: bool = False, consumers_give_up: bool = False) -> None:
+    mode = 1 if starve_producer else 2 if consumers_give_up else 0
+    _check(lib().cb_test_hooks(ctypes.c_uint32(poll_limit), ctypes.c_int32(mode)), "cb_test_hooks")
 
 
 def cb_launch_count() -> int:

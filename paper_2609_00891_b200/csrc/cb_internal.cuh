@@ -161,8 +161,9 @@ int *library_status_word();
 // the caller has none), clears the runtime's last-error state and returns CB_ERR_CUDA.
 cb_status cuda_failed(cudaError_t e = cudaSuccess);
 
-// Test hooks (cb_test_hooks): poll limit of the bounded waits and the starved-producer switch for later launches.
-struct TestHooks { unsigned poll_limit; int starve; };
+// Test hooks (cb_test_hooks): poll limit of the bounded waits, the starved-producer switch and the switch of
+// consumers that give up, for later launches.
+struct TestHooks { unsigned poll_limit; int starve, give_up; };
 TestHooks test_hooks();
 // Opt a kernel in to more than 48 KB of dynamic shared memory, once per device.
 template <class K>

@@ -44,6 +44,7 @@ cb_status launch_state(Args &a)
     const TestHooks h = test_hooks();
     a.poll_limit = h.poll_limit;
     a.starve = h.starve;
+    a.give_up = h.give_up;
     return CB_OK;
 }
 

@@ -37,7 +37,7 @@ struct PagedArgs {
     int *counters;                           // [PA_COUNTERS], zero between calls
     int *status;
     unsigned poll_limit;
-    int starve;
+    int starve, give_up;
 };
 
 cudaError_t launch_paged_attn_few(const PagedArgs &a, int d, const void *k, const void *v, int page_size, long long s_page,

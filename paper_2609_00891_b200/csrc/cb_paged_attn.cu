@@ -13,7 +13,8 @@
 // Measured: 64 requests of 512 to 8,192 keys, 8 KV heads x 8 query heads x 128: 205 us for 1.30 GB = 6.3 TB/s; one request
 // of 1,024 keys 9.5 us in a graph, of which the schedule takes 2, the copies 1.3, the tiles 1.5, the joins 3.
 // A wait that runs out is not followed by another one: the block runs through to its end, so that every barrier and join
-// counter is served as in a good run, and sets the status word; its rows are then not valid.
+// counter is served as in a good run, and sets the status word; its rows are then not valid.  No copy is issued after it,
+// and the block ends only when those in flight have landed.
 // Scores, maxima, sums and outputs are fp32; the weights exp2(s - m) are rounded to bf16 for the product with V, which is
 // bf16 as well (at most 2^-8 of each weight, as the output's own rounding).
 #include "cb_paged.cuh"
@@ -78,6 +79,7 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
     PaShare *share = reinterpret_cast<PaShare *>(warp_sums + 5);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(share + 1);
     volatile int *last_flag = abort_flag + 2;
+    volatile int *filled = abort_flag + 3;                  // stages that the producer filled
 
     const PagedArgs &a = P.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -85,6 +87,7 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
         for (int i = 0; i < C::NS; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 4); }
         abort_flag[0] = 0;
         abort_flag[1] = (int)a.poll_limit;
+        *filled = 0;
         mbar_fence_init();
         tma_prefetch_desc(&P.k);
         tma_prefetch_desc(&P.v);
@@ -114,7 +117,7 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
                         const int col = key >> a.page_log2;
                         if (col < a.table_cols) page = __ldg(row + col);
                     }
-                    if (!mbar_wait_suspended_warp(&empty[st.idx], st.phase ^ 1, abort_flag)) { dead = true; break; }
+                    if (!mbar_wait_to_issue_warp(&empty[st.idx], st.phase ^ 1, abort_flag)) { dead = true; break; }
                     if (lane == 0) mbar_arrive_expect_tx(&full[st.idx], C::STAGE);
                     __syncwarp();
                     if (lane < n_box)
@@ -125,9 +128,7 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
                 }
                 more = !dead && w.next(a);
             }
-            // after a time-out the copies in flight land before the block ends
-            for (int k = 0; dead && k < min(issued, C::NS); ++k)
-                mbar_wait_suspended_warp(&full[k], ((issued - k - 1) / C::NS) & 1, abort_flag);
+            if (lane == 0) *filled = issued;
         }
     } else if (any) {
         // ================================ consumers ================================
@@ -137,6 +138,10 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
         // ldmatrix rows of this lane: K (keys x channels) and V (keys x channels, transposed on the way)
         const int k_key = ((lane >> 4) << 3) + (lane & 7), k_ch = (lane >> 3) & 1;
         const int v_key = (((lane >> 3) & 1) << 3) + (lane & 7), v_ch = lane >> 4;
+        if (a.give_up && warp == 0) {                    // test hook: as if a wait had run out
+            abort_flag[0] = 1;
+            dead = true;
+        }
         Ring<C::NS> st;
         bool more = true;
         while (more) {
@@ -411,7 +416,11 @@ __global__ void __launch_bounds__(160, 2) k_paged_attn_few(const __grid_constant
         }
     }
     __syncthreads();
-    if (tid == 0 && abort_flag[0]) atomicExch(a.status, DEV_TIMEOUT);
+    if (abort_flag[0]) {                                 // the same in every thread: nobody writes it after the barrier
+        if (tid == 0) atomicExch(a.status, DEV_TIMEOUT);
+        const int issued = *filled;
+        for (int k = 0; k < min(issued, C::NS); ++k) mbar_drain(&full[k], ((issued - k - 1) / C::NS) & 1);
+    }
 }
 
 size_t paged_attn_few_workspace(int d) { return (size_t)2 * 2 * device_sm_count() * 64 * (d + 2) * sizeof(float); }

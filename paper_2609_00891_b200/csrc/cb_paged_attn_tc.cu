@@ -100,6 +100,10 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
     TcPiece *info = reinterpret_cast<TcPiece *>(((uintptr_t)(share + 1) + 15) & ~(uintptr_t)15);   // [2]
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(info + 2);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+    // What is to land before the block may end after a time-out: stages that the producer filled; per stage (bits) whether its
+    // last copy went to `landed`, and the parity of its next phase there; copies of each query tile.
+    struct Flight { int issued; uint32_t on_landed, landings, n_query[2]; };
+    Flight *flight = reinterpret_cast<Flight *>(tmem_slot + 3);
 
     const PagedArgs &a = P.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -118,6 +122,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
         mbar_init(drain, 1);
         abort_flag[0] = 0;
         abort_flag[1] = (int)a.poll_limit;
+        *flight = Flight{};
         mbar_fence_init();
         tma_prefetch_desc(&P.q);
         tma_prefetch_desc(&P.k);
@@ -144,6 +149,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
         if (any && !a.starve) {
             Ring<C::NS> st;
             int issued = 0;
+            uint32_t on_landed = 0, landings = 0;
             const int n_page = 1 << (7 - box_log2);
             const int cb = lane / n_page, i = lane - cb * n_page;        // 64-channel block and box of this lane
             bool more = true;
@@ -160,8 +166,11 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                     const int slot = key & ((1 << a.page_log2) - 1);
                     const bool clear = pa_clears<C::KT>(a, w.u, j0);
                     for (int comp = 0; comp < 2; ++comp) {
-                        if (!mbar_wait_suspended_warp(&empty[st.idx], st.phase ^ 1, abort_flag)) { dead = true; break; }
-                        uint64_t *bar = comp && clear ? &landed[st.idx] : &full[st.idx];
+                        if (!mbar_wait_to_issue_warp(&empty[st.idx], st.phase ^ 1, abort_flag)) { dead = true; break; }
+                        const bool cleared = comp && clear;
+                        uint64_t *bar = cleared ? &landed[st.idx] : &full[st.idx];
+                        on_landed = (on_landed & ~(1u << st.idx)) | ((uint32_t)cleared << st.idx);
+                        landings ^= (uint32_t)cleared << st.idx;
                         uint8_t *dst = kv + (size_t)st.idx * C::TILE;
                         if (lane == 0) mbar_arrive_expect_tx(bar, C::TILE);
                         __syncwarp();
@@ -173,9 +182,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                 }
                 more = !dead && w.next(a);
             }
-            // after a time-out the copies in flight land before the block ends
-            for (int k = 0; dead && k < min(issued, C::NS); ++k)
-                mbar_wait_suspended_warp(&full[k], ((issued - k - 1) / C::NS) & 1, abort_flag);
+            if (lane == 0) { flight->issued = issued; flight->on_landed = on_landed; flight->landings = landings; }
         }
     } else if (warp == 10) {
         // ================================ clears rows of V tiles ================================
@@ -214,7 +221,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
         // ================================ pieces and their Q tiles ================================
         // Runs ahead of the softmax warps: the next piece's rows are loaded while the last tile of this one is worked on.
         if (any) {
-            uint32_t n = 0, nq[2] = {0, 0};
+            uint32_t n = 0, n_query[2] = {0, 0};
             bool more = true;
             while (more && !dead) {
                 if (!mbar_wait_suspended_warp(&info_empty[n & 1], ((n >> 1) & 1) ^ 1, abort_flag)) { dead = true; break; }
@@ -231,8 +238,11 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                 __syncwarp();
                 ++n;
                 const int tiles = w.u.rows > RT ? 2 : 1;
-                for (int i = 0; i < tiles; ++i) {
-                    if (!mbar_wait_suspended_warp(&q_empty[i], (nq[i]++ & 1) ^ 1, abort_flag)) { dead = true; break; }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (i >= tiles) break;
+                    if (!mbar_wait_to_issue_warp(&q_empty[i], (n_query[i] & 1) ^ 1, abort_flag)) { dead = true; break; }
+                    ++n_query[i];
                     // rows behind the request's are another one's, or zeros, or an earlier tile's: nobody reads their results
                     if (lane == 0) {
                         mbar_arrive_expect_tx(&q_full[i], C::NB * P.q_bytes);
@@ -244,6 +254,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                 }
                 more = w.next(a);
             }
+            if (lane == 0) { flight->n_query[0] = n_query[0]; flight->n_query[1] = n_query[1]; }
             if (!dead && mbar_wait_suspended_warp(&info_empty[n & 1], ((n >> 1) & 1) ^ 1, abort_flag) && lane == 0) {
                 info[n & 1].t0 = -1;
                 mbar_arrive(&info_full[n & 1]);
@@ -335,10 +346,8 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                 }
                 more = !dead && w.next(a);
             }
-            if (dead) {                                    // products in flight end before tensor memory is freed
-                commit(drain);
-                mbar_wait_suspended_warp(drain, 0, abort_flag);
-            }
+            commit(drain);                                 // every product has ended before tensor memory is freed
+            mbar_drain(drain, 0);
         }
     }
     } else {
@@ -351,6 +360,10 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
         const float c = a.scale_log2;
         const uint64_t cc = f2_pack(c, c);
         uint32_t ns = 0, no = 0;
+        if (a.give_up && any && i == 0) {                  // test hook: as if a wait had run out
+            abort_flag[0] = 1;
+            dead = true;
+        }
         auto settle = [&](int tile, uint32_t from) {
             Walk w;
             bool more = w.open(a, *share);
@@ -579,7 +592,20 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (tid == 0 && abort_flag[0]) atomicExch(a.status, DEV_TIMEOUT);
+    if (abort_flag[0]) {                                   // the same in every thread: nobody writes it after the barrier
+        if (tid == 0) atomicExch(a.status, DEV_TIMEOUT);
+        // copies in flight land before the block ends
+        if (warp == 9) {
+            const Flight f = *flight;
+            for (int k = 0; k < min(f.issued, C::NS); ++k) {
+                if (f.on_landed >> k & 1) mbar_drain(&landed[k], (f.landings >> k & 1) ^ 1);
+                else mbar_drain(&full[k], ((f.issued - k - 1) / C::NS) & 1);
+            }
+            for (int i = 0; i < 2; ++i)
+                if (f.n_query[i]) mbar_drain(&q_full[i], (f.n_query[i] - 1) & 1);
+        }
+        __syncwarp();
+    }
     if (warp == 9) tmem_dealloc(tmem, C::TMEM_COLS);
 }
 

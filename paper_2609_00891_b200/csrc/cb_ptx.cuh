@@ -120,6 +120,20 @@ __device__ __forceinline__ bool mbar_wait_suspended_warp(uint64_t *bar, uint32_t
     return __all_sync(0xffffffffu, mbar_wait_suspended(bar, parity, abort_flag)) != 0;
 }
 
+// For a warp that issues copies, before it fills a stage again: the same wait, and false as well once any warp of the block
+// has given up.  A warp that gave up releases stages whose copy it has not seen land; it sets the flag before that arrival,
+// so the flag is seen here and no copy goes to such a stage.
+__device__ __forceinline__ bool mbar_wait_to_issue_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
+{
+    return __all_sync(0xffffffffu, mbar_wait_suspended(bar, parity, abort_flag) && abort_flag[0] == 0) != 0;
+}
+// After a time-out: waits for a copy or a product in flight whatever the abort flag says (2^20 polls, a quarter of a second
+// or more; those take microseconds).
+__device__ __forceinline__ void mbar_drain(uint64_t *bar, uint32_t parity)
+{
+    for (uint32_t i = 0; i < (1u << 20) && !mbar_try_wait(bar, parity); ++i) __nanosleep(256);
+}
+
 // Make this thread's generic-proxy writes to shared memory visible to the async proxy (TMA, tensor cores).
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 

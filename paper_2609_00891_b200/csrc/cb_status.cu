@@ -51,7 +51,11 @@ int *library_status_word()
     return g_status_ptr[dev];
 }
 
-TestHooks test_hooks() { return TestHooks{g_poll_limit.load(), g_starve.load()}; }
+TestHooks test_hooks()
+{
+    const int mode = g_starve.load();
+    return TestHooks{g_poll_limit.load(), mode == 1, mode == 2};
+}
 
 static std::atomic<int> g_last_cuda_error{0};
 
@@ -86,7 +90,7 @@ extern "C" cb_status cb_last_device_status(void *stream)
 extern "C" cb_status cb_test_hooks(uint32_t poll_limit, int32_t starve_producer)
 {
     g_poll_limit.store(poll_limit ? poll_limit : (1u << 22));
-    g_starve.store(starve_producer ? 1 : 0);
+    g_starve.store(starve_producer == 2 ? 2 : starve_producer ? 1 : 0);
     return CB_OK;
 }
 

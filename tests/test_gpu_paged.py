@@ -465,6 +465,26 @@ def test_attention_time_out_is_reported_and_leaves_the_workspace_usable():
         cb.cb_test_hooks()
 
 
+@pytest.mark.parametrize("new,total,d,page,window", [
+    ([1, 1, 70], [3000, 100, 70], 128, 16, 0), ([300, 1], [9000, 700], 128, 64, 0), ([300, 7], [20000, 40], 64, 8, 1000), ([1] * 9, [5000] * 9, 64, 16, 70)])
+def test_attention_consumers_that_give_up_while_copies_are_in_flight(new, total, d, page, window):
+    """Some warps take their first wait as run out while the copies go on: the block issues no more of them, lets those in
+    flight land, reports, and leaves the workspace as a good run does."""
+    b = _batch(new, total, 2, 4, d, page)
+    want = _compare(*b, window=window, n_sink=2)
+    try:
+        for max_new in (1, 0, 1, 0):
+            cb.cb_test_hooks(poll_limit=2000, consumers_give_up=True)
+            _attend(*b, window=window, n_sink=2, max_new=max_new)
+            with pytest.raises(cb.CbError) as e:
+                cb.cb_last_device_status()
+            assert e.value.status == cb.CB_ERR_TIMEOUT
+            cb.cb_test_hooks()
+            assert torch.equal(_compare(*b, window=window, n_sink=2), want)
+    finally:
+        cb.cb_test_hooks()
+
+
 # ---------------------------------------------------------------------------------------------------- together
 def test_a_decode_step_captured_once_and_replayed_as_requests_grow():
     """Tables, rotation, store and attention in one graph; the host only rotates the free list between replays."""
