@@ -432,7 +432,7 @@ cb_status cb_rank_layers(const float *scores, int32_t Lt, int32_t Ls, int32_t k,
  *     cb_paged_attention  attention of the new rows of every request over its pages
  * All lengths are read from device memory, so a step can be captured into a CUDA graph once and replayed as requests grow
  * (make the first call of each on a device outside any capture: it loads the kernel).
- * Every tensor of a call lives on the current device.
+ * Every tensor of a call lives on the current device.  n_requests is below 2^28 (CB_ERR_UNSUPPORTED otherwise).
  *
  * cb_page_pool: K and V of all layers in pages of page_size rows.  Element (layer, page, slot, head, c) is at
  *     (bf16*)k + layer*stride_layer + page*stride_page + slot*stride_slot + head*stride_head + c

@@ -11,6 +11,8 @@ using namespace cb;
 
 namespace {
 
+constexpr int32_t MAX_REQUESTS = 1 << 28;      // the kernels count requests, and twice as many, in 32 bits
+
 // log2 of a page size the kernels take (8 .. 256), or -1
 int page_log2_of(int32_t ps)
 {
@@ -68,7 +70,7 @@ cb_status cb_page_tables(const int32_t *cached_len, const int32_t *new_len, int3
     if (n_requests > 0 && (total_len == cached_len || total_len == new_len || cu_new == cached_len || cu_new == new_len || cu_new == total_len))
         return CB_ERR_INVALID_ARG;
     const int lg = page_log2_of(page_size);
-    if (lg < 0 || n_rows >= (1ll << 31)) return CB_ERR_UNSUPPORTED;
+    if (lg < 0 || n_rows >= (1ll << 31) || n_requests >= MAX_REQUESTS) return CB_ERR_UNSUPPORTED;
     if (const cudaError_t e = launch_page_tables(cached_len, new_len, n_requests, lg, free_pages, n_free, block_table, table_stride, max_pages,
                                                  cu_new, total_len, positions, reinterpret_cast<long long *>(slot_map), n_rows,
                                                  pages_used, static_cast<cudaStream_t>(stream)); e != cudaSuccess) return cuda_failed(e);
@@ -166,7 +168,7 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
     if ((n_rows > 1 && (o_stride_token == 0 || q_stride_token == 0)) || (n_q_heads > 1 && (o_stride_head == 0 || q_stride_head == 0))) return CB_ERR_UNSUPPORTED;
     if (q_stride_token >= (1ll << 39) || q_stride_head >= (1ll << 39)) return CB_ERR_UNSUPPORTED;
     // flattened rows and units are counted in 32 bits
-    if (n_rows >= (1ll << 31) || n_rows * n_q_heads + n_requests >= (1ll << 31)) return CB_ERR_UNSUPPORTED;
+    if (n_rows >= (1ll << 31) || n_rows * n_q_heads + n_requests >= (1ll << 31) || n_requests >= MAX_REQUESTS) return CB_ERR_UNSUPPORTED;
     if (n_requests > 1 && table_stride < max_pages) return CB_ERR_INVALID_ARG;
     if (n_rows == 0 || n_requests == 0) return CB_OK;
     if (!q || !out || !block_table || !cu_new || !total_len) return CB_ERR_INVALID_ARG;

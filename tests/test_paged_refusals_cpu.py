@@ -110,3 +110,10 @@ def test_workspace_and_tensors_of_the_wrong_place():
     with pytest.raises(ValueError):                                   # tensors of the host
         cb.cb_paged_store(cb.PagePool(pool, pool), rows, rows, torch.zeros(3, dtype=torch.int64))
     assert cb.cb_launch_count() == 0
+
+
+@pytest.mark.parametrize("B,want", [((1 << 28) - 1, CUDA), (1 << 28, UNS), ((1 << 31) - 1, UNS)])
+def test_request_counts(B, want):
+    """Requests and what is counted from them stay far inside 32 bits."""
+    assert _tables(B=B) == want
+    assert _attention(B=B, rows=1) == want
