@@ -506,7 +506,8 @@ cb_status cb_rope_axes(const void *x, void *out, int32_t n_layers, int32_t n_hea
  *     out = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale q . k_j)   over the keys j <= p with
  *     window == 0  or  p - j < window  or  j < n_sink
  * (a sliding window of the row's own and the window - 1 keys before it, and n_sink first keys that stay visible).  A row
- * that sees no key (p < 0) gets zeros; rows of q behind cu_new[n_requests] are neither read nor written.  Query head h
+ * that sees no key (p < 0) gets zeros; rows of q behind cu_new[n_requests] are neither read nor written, and rows of a
+ * request past n_rows (a batch larger than a captured step's room) are dropped.  Query head h
  * reads KV head h / (n_q_heads / n_heads).  Key j is at slot j mod page_size of page block_table[b][j / page_size]; only
  * entries of pages that hold a visible key are read, and a page id outside the pool reads as zeros.  Rows of a page that
  * no row of the request sees may hold anything; keys and values that some row of the request sees must be finite.

@@ -91,7 +91,7 @@ __device__ __forceinline__ int pa_unit_of(const PagedArgs &a, int n)
 // One unit's place in the batch and its key tiles of KT keys.
 struct PaUnit {
     int b, qt, nq;          // request, row block, row blocks of the request
-    int row0, rows;         // first flattened row, rows in the block
+    int row0, rows;         // first flattened row, rows in the block (those that q has)
     int tok0;               // first row of the request in q
     int base;               // position of the request's first new row (negative if the cache is shorter than the chunk)
     int p0, p1;             // positions of the block's first and last row
@@ -104,11 +104,12 @@ template <int ROWS, int KT>
 __device__ __forceinline__ bool pa_unit(const PagedArgs &a, const int *cu, const int *total, int b, int qt, PaUnit &u)
 {
     const int c0 = cu[b], fresh = cu[b + 1] - c0;
-    const int all = fresh * a.group;
+    const int here = max(0, min(cu[b + 1], a.n_rows) - c0);       // rows past the room of q are dropped
+    const int all = here * a.group;
     u.b = b;
     u.qt = qt;
     const int per = ROWS ? ROWS : a.unit_rows;
-    u.nq = ROWS ? (all + ROWS - 1) / (ROWS ? ROWS : 1) : pa_unit_of<0>(a, max(fresh, 0) + a.unit_tokens - 1);
+    u.nq = ROWS ? (all + ROWS - 1) / (ROWS ? ROWS : 1) : pa_unit_of<0>(a, here + a.unit_tokens - 1);
     if (qt >= u.nq) { u.n = 0; return false; }
     u.tok0 = c0;
     u.row0 = qt * per;
@@ -198,7 +199,7 @@ __device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int
     __syncthreads();
     // unit index u: the last request b with floor(cu[b] group / ROWS) + b <= u (some indices are no unit); 32 bits hold
     // rows * query heads, checked by the host
-    auto first_unit = [&](int b) { return pa_unit_of<ROWS>(a, max(cu[b], 0)) + b; };
+    auto first_unit = [&](int b) { return pa_unit_of<ROWS>(a, min(max(cu[b], 0), a.n_rows)) + b; };
     const int n_units = pa_unit_of<ROWS>(a, a.n_rows) + B;
     const int per = (n_units + THREADS - 1) / THREADS;
     const int u0 = min(n_units, tid * per), u1 = min(n_units, u0 + per);
@@ -322,7 +323,7 @@ struct PaWalk {
             int b = u.b, qt = u.qt + 1;
             if (qt >= u.nq) {
                 qt = 0;
-                do { ++b; } while (b < a.n_requests && a.cu[b + 1] <= a.cu[b]);
+                do { ++b; } while (b < a.n_requests && min(a.cu[b + 1], a.n_rows) <= a.cu[b]);
                 if (b >= a.n_requests) return false;
             }
             pa_unit<ROWS, KT>(a, a.cu, a.total, b, qt, u);

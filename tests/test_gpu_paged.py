@@ -389,6 +389,22 @@ def test_attention_many_requests():
     _compare(*b)
 
 
+@pytest.mark.parametrize("new", [[3, 9, 4], [2, 300, 1], [3, 1 << 28, 1 << 28]])
+@pytest.mark.parametrize("H,group,d", [(2, 8, 128), (1, 16, 64), (2, 5, 64)])
+def test_attention_rows_past_the_room_are_dropped(new, H, group, d):
+    """A batch with more rows than q has room for, as the tables of a captured step describe it."""
+    room, before = 7, [10, 20, 30]                          # rows of q; keys in the cache before the step
+    kept = [min(n, room - at) for n, at in zip(new, (0, new[0], room))]
+    q, k, v, table, cu, total = _batch(kept[:2] + [0], [b + n for b, n in zip(before, kept)], H, group, d, 16)
+    assert cu[-1] == room
+    want, tol = ref.attention(q, k[0], v[0], table, cu, total, d ** -0.5)
+    all_cu = np.concatenate([[0], np.cumsum(new)]).tolist()
+    for max_new in (1, 0, 1 << 30):
+        out = _attend(q, k, v, table, all_cu, [b + n for b, n in zip(before, new)], max_new=max_new)
+        assert ((out.double() - want).abs() <= tol).all()
+        assert int(_workspace(d)[:8192].sum()) == 0
+
+
 def test_attention_large_scores_and_layers():
     q, k, v, table, cu, total = _batch([1, 3], [200, 100], 2, 4, 128, 16, layers=3, layer=2)
     _compare(q * 30, k, v, table, cu, total, layer=2)
