@@ -513,7 +513,7 @@ cb_status cb_rope_axes(const void *x, void *out, int32_t n_layers, int32_t n_hea
  * no row of the request sees may hold anything; keys and values that some row of the request sees must be finite.
  * max_new: the largest number of new rows of a request, or 0 if unknown.  It chooses between kernels and never changes
  * which rows are computed.
- * scale > 0.  workspace: device, 256-byte aligned, cb_paged_attention_workspace_bytes() bytes (it depends on
+ * scale > 0, and scale * log2(e) finite in 32 bits.  workspace: device, 256-byte aligned, cb_paged_attention_workspace_bytes() bytes (it depends on
  * the current device's SM count), ZERO-FILLED once by the
  * caller before its first use (calls leave it ready for the next one); calls that share a workspace must be ordered on
  * the device (one stream, or graphs that never run at the same time).  Results are bitwise reproducible.  A device-side

@@ -162,7 +162,8 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
     if (layer < 0 || layer >= pool->n_layers || n_rows < 0 || n_q_heads <= 0 || n_requests < 0 || max_pages <= 0 || max_new < 0 ||
         table_stride < 0 || window < 0 || n_sink < 0)
         return CB_ERR_INVALID_ARG;
-    if (n_q_heads % pool->n_heads || !(scale > 0.f) || !std::isfinite(scale)) return CB_ERR_INVALID_ARG;
+    const float scale_log2 = (float)(scale * 1.4426950408889634074);
+    if (n_q_heads % pool->n_heads || !(scale > 0.f) || !std::isfinite(scale_log2)) return CB_ERR_INVALID_ARG;
     if (q_stride_token < 0 || q_stride_head < 0 || o_stride_token < 0 || o_stride_head < 0) return CB_ERR_INVALID_ARG;
     if ((q_stride_token | q_stride_head | o_stride_token | o_stride_head) & 7) return CB_ERR_INVALID_ARG;
     if ((n_rows > 1 && (o_stride_token == 0 || q_stride_token == 0)) || (n_q_heads > 1 && (o_stride_head == 0 || q_stride_head == 0))) return CB_ERR_UNSUPPORTED;
@@ -195,7 +196,7 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
     a.page_log2 = page_log2_of(pool->page_size);
     a.n_pages = (int)pool->n_pages;
     a.window = window; a.n_sink = window > 0 ? n_sink : 0;
-    a.scale_log2 = (float)(scale * 1.4426950408889634074);
+    a.scale_log2 = scale_log2;
     a.q_min = 2;
     a.counters = static_cast<int *>(workspace);
     a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + PA_COUNTER_BYTES);

@@ -117,3 +117,9 @@ def test_request_counts(B, want):
     """Requests and what is counted from them stay far inside 32 bits."""
     assert _tables(B=B) == want
     assert _attention(B=B, rows=1) == want
+
+
+@pytest.mark.parametrize("scale,want", [(2.3e38, CUDA), (2.4e38, BAD), (3.4e38, BAD), (1e-45, CUDA)])
+def test_scales(scale, want):
+    """The kernels scale scores by scale * log2(e): that product is finite too."""
+    assert _attention(scale=scale) == want
