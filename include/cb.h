@@ -463,7 +463,7 @@ typedef struct cb_page_pool {
  *   pages_used    [1] or NULL       pages taken from the free list; more than n_free if it was too short
  * n_rows is the room in positions and slot_map (a captured step keeps it fixed); rows past it are dropped.  One launch,
  * deterministic; calling again with the same inputs writes the same values.  No output may overlap an input or another
- * output, block_table apart (total_len in the place of cached_len is CB_ERR_INVALID_ARG: copy it between steps).
+ * output (CB_ERR_INVALID_ARG: total_len in the place of cached_len, for one, is copied between steps).
  */
 cb_status cb_page_tables(const int32_t *cached_len, const int32_t *new_len, int32_t n_requests, int32_t page_size,
                          const int32_t *free_pages, int64_t n_free, int32_t *block_table, int64_t table_stride, int32_t max_pages,

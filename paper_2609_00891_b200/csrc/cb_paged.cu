@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <iterator>
 
 #include "cb_paged.cuh"
 #include "cb_rope.cuh"
@@ -38,6 +39,13 @@ cb_status check_pool(const cb_page_pool *p)
     return CB_OK;
 }
 
+struct Range { const void *p; int64_t bytes; };
+bool overlap(const Range &a, const Range &b)
+{
+    const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+    return a.bytes > 0 && b.bytes > 0 && x < y + (uintptr_t)b.bytes && y < x + (uintptr_t)a.bytes;
+}
+
 template <class Args>
 cb_status launch_state(Args &a)
 {
@@ -66,11 +74,21 @@ cb_status cb_page_tables(const int32_t *cached_len, const int32_t *new_len, int3
     if ((((uintptr_t)cached_len | (uintptr_t)new_len | (uintptr_t)free_pages | (uintptr_t)block_table | (uintptr_t)cu_new |
           (uintptr_t)total_len | (uintptr_t)positions | (uintptr_t)pages_used) & 3) || ((uintptr_t)slot_map & 7))
         return CB_ERR_INVALID_ARG;
-    // every block reads the lengths while the first one writes its results
-    if (n_requests > 0 && (total_len == cached_len || total_len == new_len || cu_new == cached_len || cu_new == new_len || cu_new == total_len))
-        return CB_ERR_INVALID_ARG;
     const int lg = page_log2_of(page_size);
     if (lg < 0 || n_rows >= (1ll << 31) || n_requests >= MAX_REQUESTS) return CB_ERR_UNSUPPORTED;
+    // Every block reads the inputs while others write their results.  (A table whose rows have room behind them may have
+    // something else there, so its rows are not looked at then.)
+    const int64_t B = n_requests;
+    const bool dense = B <= 1 || table_stride == max_pages;
+    const Range in[] = {{cached_len, B * 4}, {new_len, B * 4}, {free_pages, n_free * 4}},
+                out[] = {{cu_new, (B + 1) * 4}, {total_len, B * 4}, {positions, n_rows * 4}, {slot_map, n_rows * 8},
+                         {pages_used, pages_used ? 4 : 0}, {block_table, dense ? B * max_pages * 4 : 0}};
+    for (size_t i = 0; i < std::size(out); ++i) {
+        for (const Range &r : in)
+            if (overlap(out[i], r)) return CB_ERR_INVALID_ARG;
+        for (size_t j = 0; j < i; ++j)
+            if (overlap(out[i], out[j])) return CB_ERR_INVALID_ARG;
+    }
     if (const cudaError_t e = launch_page_tables(cached_len, new_len, n_requests, lg, free_pages, n_free, block_table, table_stride, max_pages,
                                                  cu_new, total_len, positions, reinterpret_cast<long long *>(slot_map), n_rows,
                                                  pages_used, static_cast<cudaStream_t>(stream)); e != cudaSuccess) return cuda_failed(e);
@@ -172,6 +190,7 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
     if (n_rows >= (1ll << 31) || n_rows * n_q_heads + n_requests >= (1ll << 31) || n_requests >= MAX_REQUESTS) return CB_ERR_UNSUPPORTED;
     if (n_requests > 1 && table_stride < max_pages) return CB_ERR_INVALID_ARG;
     if (n_rows == 0 || n_requests == 0) return CB_OK;
+    if (q == out) return CB_ERR_INVALID_ARG;         // rows are written while other blocks still read theirs
     if (!q || !out || !block_table || !cu_new || !total_len) return CB_ERR_INVALID_ARG;
     if ((((uintptr_t)q | (uintptr_t)out) & 15) || (((uintptr_t)block_table | (uintptr_t)cu_new | (uintptr_t)total_len) & 3)) return CB_ERR_INVALID_ARG;
     size_t need = 0;

@@ -115,7 +115,7 @@ def test_workspace_and_tensors_of_the_wrong_place():
 @pytest.mark.parametrize("B,want", [((1 << 28) - 1, CUDA), (1 << 28, UNS), ((1 << 31) - 1, UNS)])
 def test_request_counts(B, want):
     """Requests and what is counted from them stay far inside 32 bits."""
-    assert _tables(B=B) == want
+    assert _tables(B=B, cached=1 << 40, new=2 << 40, table=3 << 40, cu=4 << 40, total=5 << 40) == want
     assert _attention(B=B, rows=1) == want
 
 
@@ -123,3 +123,15 @@ def test_request_counts(B, want):
 def test_scales(scale, want):
     """The kernels scale scores by scale * log2(e): that product is finite too."""
     assert _attention(scale=scale) == want
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(pos=0x500), BAD), (dict(pos=0x104), BAD), (dict(pos=0x10c), CUDA), (dict(slot=0x700), BAD), (dict(used=0x508), BAD), (dict(used=0x510), CUDA),
+    (dict(total=0x310), BAD), (dict(total=0x314), CUDA), (dict(cu=0x45c), BAD), (dict(cu=0x460), CUDA), (dict(total=0x20, stride=9, table=0x24), CUDA),
+    (dict(free=0x400, n_free=1), BAD), (dict(pos=0x100, slot=0x200, rows=0), CUDA)])
+def test_page_tables_outputs_in_the_place_of_other_arrays(change, want):
+    assert _tables(**change) == want
+
+
+def test_attention_in_place():
+    assert _attention(out=0x1000) == BAD
