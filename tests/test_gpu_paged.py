@@ -389,6 +389,17 @@ def test_attention_many_requests():
     _compare(*b)
 
 
+@pytest.mark.parametrize("new,total", [([1, 0, 33, 64, 65, 130], [1, 0, 40, 64, 300, 131]), ([700], [1500]), ([1, 2, 1], [255, 257, 900])])
+@pytest.mark.parametrize("window,n_sink", [(0, 0), (100, 3), (1, 0), (300, 130)])
+@pytest.mark.parametrize("d,page,hnd", [(128, 8, False), (128, 256, True), (64, 8, True), (64, 256, False)])
+def test_attention_smallest_and_largest_pages(d, page, hnd, window, n_sink, new, total):
+    """Both kernels with sixteen boxes a tile and with boxes that start inside a page, windows and sinks over 64-channel heads."""
+    b = _batch(new, total, 2, 8, d, page, hnd, pad_rows=1)
+    one = _compare(*b, window=window, n_sink=n_sink, max_new=0)
+    assert torch.equal(one, _attend(*b, window=window, n_sink=n_sink, max_new=0))
+    _compare(*b, window=window, n_sink=n_sink, max_new=2)
+
+
 @pytest.mark.parametrize("new", [[3, 9, 4], [2, 300, 1], [3, 1 << 28, 1 << 28]])
 @pytest.mark.parametrize("H,group,d", [(2, 8, 128), (1, 16, 64), (2, 5, 64)])
 def test_attention_rows_past_the_room_are_dropped(new, H, group, d):
