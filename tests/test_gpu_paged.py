@@ -578,6 +578,92 @@ def test_a_decode_step_captured_once_and_replayed_as_requests_grow():
     cb.cb_last_device_status()
 
 
+def test_a_step_layer_by_layer_through_views_of_one_layer():
+    """A layer's queries, keys and values follow from the attention of the layer before it, so that its rows are stored just
+    before its attention reads them; the whole step is captured and replayed as requests grow."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(31)
+    B, H, group, d, page, L, base = 3, 2, 4, 64, 16, 3, 1e4
+    pages, cols, Hq = 40, 6, 8
+    k, v = _pool(L, pages, page, H, d, True, fill=float("nan"))
+    pools = [cb.PagePool(k[l:l + 1], v[l:l + 1]) for l in range(L)]
+    lens = [3, 16, 40]
+    ids = torch.randperm(pages, generator=g, device=DEV).int()
+    table, at = torch.full((B, cols), -1, dtype=torch.int32, device=DEV), 0
+    old = []                                                # [request][layer] -> keys, values so far, as stored
+    for b, n in enumerate(lens):
+        held = -(-n // page)
+        table[b, :held], at = ids[at:at + held], at + held
+        j, rows = torch.arange(n, device=DEV), [torch.randn(L, n, H, d, generator=g, device=DEV).bfloat16() for _ in range(2)]
+        k[:, table[b, j // page].long(), j % page], v[:, table[b, j // page].long(), j % page] = rows
+        old.append(rows)
+    free = ids[at:].clone()
+    wq, wk, wv = (torch.randn(L, Hq * d, n * d, generator=g, device=DEV) * (Hq * d) ** -0.5 for n in (Hq, H, H))
+    x0, cached, new = torch.randn(B, Hq * d, generator=g, device=DEV), _i32(lens), _i32([1] * B)
+    cu, total, used, pos = _i32([0] * (B + 1)), _i32([0] * B), _i32([0]), torch.zeros(1, B, dtype=torch.int32, device=DEV)
+    slot, o = torch.zeros(B, dtype=torch.int64, device=DEV), torch.zeros(L, B, Hq, d, dtype=torch.bfloat16, device=DEV)
+    got = [[torch.zeros(B, n, d, dtype=torch.bfloat16, device=DEV) for n in (Hq, H, H)] for _ in range(L)]
+    ws = _workspace(d)
+
+    def step():
+        x = x0
+        cb.cb_page_tables(cached, new, page, free, table, cu, total, pos[0], slot, used)
+        for l in range(L):
+            q, kn, vn = ((x @ w[l]).bfloat16().view(1, B, -1, d) for w in (wq, wk, wv))
+            cb.cb_rope_axes(q, q, pos, [d // 2], base)
+            cb.cb_rope_axes(kn, kn, pos, [d // 2], base)
+            cb.cb_paged_store(pools[l], kn, vn, slot)
+            cb.cb_paged_attention(q[0], o[l], pools[l], 0, table, cu, total, d ** -0.5, ws, max_new=1)
+            for t, s in zip(got[l], (q, kn, vn)):
+                t.copy_(s[0])
+            x = x + o[l].reshape(B, Hq * d).float()
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        keep = table.clone()
+        step()
+        table.copy_(keep)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(20):
+        x0.copy_(torch.randn(B, Hq * d, generator=g, device=DEV))
+        graph.replay()
+        assert pos[0].tolist() == [n + i for n in lens]
+        x = x0
+        for l in range(L):
+            q, kn, vn = got[l]
+            # The layer's rows follow from the attention of the layer before.  The fp32 product over 512 terms is off by up to
+            # 2 * 512 * 2^-24 of the sum of sizes, a rounding to bf16 by 2^-8 of the value; queries and keys are then turned
+            # (each part of the pair carries its error into both, the angle and polynomials add 2^-20 of the pair's length)
+            # and rounded once more.
+            for have, w, turn in ((q, wq, True), (kn, wk, True), (vn, wv, False)):
+                row = (x.double() @ w[l].double()).view(B, -1, d)
+                off = row.abs() * 2.0 ** -8 + 2 * 512 * 2.0 ** -24 * (x.abs().double() @ w[l].abs().double()).view(B, -1, d)
+                if turn:
+                    off = (off[..., :d // 2] + off[..., d // 2:] + 2.0 ** -20 * torch.sqrt(row[..., :d // 2] ** 2 + row[..., d // 2:] ** 2)).repeat(1, 1, 2)
+                    row = ref.rope(row[None], pos, [d // 2], base, False, False)[0]
+                    off = off + (row.abs() + off) * 2.0 ** -8
+                assert ((have.double() - row).abs() <= off).all()
+            n = max(lens) + i + 1
+            kd, vd = (torch.zeros(B, n, H, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+            for b in range(B):
+                have = old[b][0].shape[1]
+                kd[b, :have], vd[b, :have] = old[b][0][l], old[b][1][l]
+                kd[b, have], vd[b, have] = kn[b], vn[b]
+            want, tol = ref.attention(q, kd, vd, torch.arange(B, device=DEV)[:, None], list(range(B + 1)), total.tolist(), d ** -0.5)
+            assert ((o[l].double() - want).abs() <= tol).all()
+            x = x + o[l].reshape(B, Hq * d).float()
+        for b in range(B):
+            for c in range(2):
+                old[b][c] = torch.cat([old[b][c], torch.stack([got[l][1 + c][b] for l in range(L)])[:, None]], 1)
+        free.copy_(free.roll(-int(used[0])))
+        cached.copy_(total)
+    cb.cb_last_device_status()
+
+
 def test_mapped_cache_into_pages_and_attention_over_it():
     """A fitted map's target cache is stored into pages, a chunk of new rows and then single tokens join it, and attention
     over the pages agrees with attention over the dense tensors."""
