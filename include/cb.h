@@ -472,10 +472,12 @@ cb_status cb_page_tables(const int32_t *cached_len, const int32_t *new_len, int3
 
 /*
  * Stores row t of every layer and head to slot slot_map[t] (device int64 [n_rows]; negative or past the pool: the row is
- * skipped).  src_k / src_v: device, element (layer, row, head, c) at layer*stride_layer + row*stride_token +
- * head*stride_head + c elements of src_dtype (CB_DTYPE_BF16: copied; CB_DTYPE_F32: rounded to nearest even), 16-byte
- * aligned, strides multiples of 8; the pool's layers, heads and head_dim.  Slots must differ (those of cb_page_tables do):
- * of two rows with one slot either may end there, piece by piece.  n_rows == 0 is a no-op.
+ * skipped).  All layers at once is the mapped cache's case; a model's step stores one layer at a time, through a pool
+ * that describes that layer alone (k and v at the layer's first element, n_layers 1).  src_k / src_v: device, element
+ * (layer, row, head, c) at layer*stride_layer + row*stride_token + head*stride_head + c elements of src_dtype
+ * (CB_DTYPE_BF16: copied; CB_DTYPE_F32: rounded to nearest even), 16-byte aligned, strides multiples of 8; the pool's
+ * layers, heads and head_dim.  Slots must differ (those of cb_page_tables do): of two rows with one slot either may end
+ * there, piece by piece.  n_rows == 0 is a no-op.
  */
 cb_status cb_paged_store(const cb_page_pool *pool, const void *src_k, const void *src_v, int32_t src_dtype, int64_t n_rows,
                          int64_t stride_layer, int64_t stride_token, int64_t stride_head, const int64_t *slot_map, void *stream);
@@ -486,10 +488,14 @@ cb_status cb_paged_store(const cb_page_pool *pool, const void *src_k, const void
  *     positions[axis(i)][token] * rope_base^(-2 i / head_dim).
  * positions: device int32, axis a at positions + a*axis_stride, any 32-bit value.  sections: HOST [n_axes] (<= 8), pairs
  * per axis, summing to head_dim/2; axis(i) takes the sections one after the other, or with interleaved != 0 axis
- * a = i mod n_axes while i < n_axes*sections[a], and axis 0 after that.  One axis is the ordinary embedding.  inverse != 0
- * turns the other way (the adjoint, and the removal of the embedding).  x, out: bf16 [layer][token][head][channel] by
- * strides (multiples of 8, 16-byte aligned; output strides of 0 only on dimensions of size 1); out may be x itself with
- * the same strides, but not overlap it otherwise.  Angles are exact to 2^-22 turns at every 32-bit position.
+ * a = i mod n_axes while i < n_axes*sections[a], and axis 0 after that (so an axis gets the pairs that `sections` names
+ * only if that rule has room for them below head_dim/2: of {2, 60, 2} at head_dim 128 axis 1 gets 21, and axis 0 the rest).
+ * One axis is the ordinary embedding: as cb_rope_rotate, which takes positions below 2^20 and carries angles in 32 bits
+ * where this call carries 64; use this one for far positions, out of place, or with strides of 0.  Rows
+ * are bf16 only: mapped fp32 keys are rotated by cb_apply_rope, or rounded first.  inverse != 0 turns the other way
+ * (the adjoint, and the removal of the embedding).  x, out: bf16 [layer][token][head][channel] by strides (multiples of
+ * 8, 16-byte aligned; output strides of 0 only on dimensions of size 1); out may be x itself with the same strides, but
+ * not overlap it otherwise.  Angles are exact to 2^-22 turns at every 32-bit position.
  */
 cb_status cb_rope_axes(const void *x, void *out, int32_t n_layers, int32_t n_heads, int32_t head_dim, int64_t n_tokens,
                        int64_t x_stride_layer, int64_t x_stride_token, int64_t x_stride_head,
@@ -500,24 +506,27 @@ cb_status cb_rope_axes(const void *x, void *out, int32_t n_layers, int32_t n_hea
 /*
  * Attention of new rows over one layer of a paged cache.  Request b owns rows [cu_new[b], cu_new[b+1]) of q and out
  * (bf16, row t of query head h at t*stride_token + h*stride_head, multiples of 8, a stride of 0 only on a dimension of
- * size 1, 16-byte aligned; q and out must not overlap); they are the LAST
- * rows of its total_len[b] (below 2^31 - 256) rows in the cache (their own keys and values are stored already), so row i of the request has
- * position p = total_len - new + i, and
+ * size 1, 16-byte aligned; q and out must not overlap, and q == out is CB_ERR_INVALID_ARG); they are the LAST rows of
+ * its total_len[b] (below 2^31 - 256) rows in the cache (their own keys and values are stored already), so row i of the
+ * request has position p = total_len - new + i, and
  *     out = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale q . k_j)   over the keys j <= p with
  *     window == 0  or  p - j < window  or  j < n_sink
  * (a sliding window of the row's own and the window - 1 keys before it, and n_sink first keys that stay visible).  A row
  * that sees no key (p < 0) gets zeros; rows of q behind cu_new[n_requests] are neither read nor written, and rows of a
- * request past n_rows (a batch larger than a captured step's room) are dropped.  Query head h
- * reads KV head h / (n_q_heads / n_heads).  Key j is at slot j mod page_size of page block_table[b][j / page_size]; only
- * entries of pages that hold a visible key are read, and a page id outside the pool reads as zeros.  Rows of a page that
- * no row of the request sees may hold anything; keys and values that some row of the request sees must be finite.
+ * request past n_rows (a batch larger than a captured step's room) are dropped.  Query head h reads KV head h /
+ * (n_q_heads / n_heads).  Scores, softmax statistics and sums are fp32; the weights w are rounded to bf16 for the
+ * product with V (2^-8 of each at most), and the output to bf16.  Key j is at slot j mod page_size of page
+ * block_table[b][j / page_size]; only entries of pages that hold a visible key are read, and a page id outside the pool
+ * reads as zeros.  Rows of a page that no row of the request sees may hold anything; keys and values that some row of
+ * the request sees must be finite.
  * max_new: the largest number of new rows of a request, or 0 if unknown.  It chooses between kernels and never changes
  * which rows are computed.
- * scale > 0, and scale * log2(e) finite in 32 bits.  workspace: device, 256-byte aligned, cb_paged_attention_workspace_bytes() bytes (it depends on
- * the current device's SM count), ZERO-FILLED once by the
- * caller before its first use (calls leave it ready for the next one); calls that share a workspace must be ordered on
- * the device (one stream, or graphs that never run at the same time).  Results are bitwise reproducible.  A device-side
- * time-out shows in cb_last_device_status.  n_rows * n_q_heads + n_requests < 2^31.
+ * scale > 0, and scale * log2(e) finite in 32 bits.  workspace: device, 256-byte aligned,
+ * cb_paged_attention_workspace_bytes() bytes (it depends on the current device's SM count), ZERO-FILLED once by the caller
+ * before its first use (calls leave it ready for the next one); calls that share a workspace must be ordered on the device
+ * (one stream, or graphs that never run at the same time).  The same call on the same kind of device gives the same bits;
+ * where a request's keys are split, and so its last bits, depends on the other requests' lengths, on the number of SMs and
+ * on max_new.  A device-side time-out shows in cb_last_device_status.  n_rows * n_q_heads + n_requests < 2^31.
  */
 cb_status cb_paged_attention_workspace_bytes(int32_t head_dim, size_t *bytes);
 cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void *q, int64_t q_stride_token, int64_t q_stride_head,
