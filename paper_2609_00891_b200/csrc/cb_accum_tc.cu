@@ -533,9 +533,7 @@ static PFN_cuTensorMapEncodeTiled_v12000 encode_fn()
     return fn;
 }
 
-// 5-D map over (64 channels, token, 64-channel block, head, layer).  One box = box_tokens tokens of one head of
-// one layer, laid out in shared memory as [channel block][token][64 channels] with the 128-byte swizzle.
-// box_cblocks: 64-channel blocks per box (0: all d / 64 of them; 1: one block, selected by the copy's third coordinate).
+// 4-D map over (64 channels, head, token, 64-channel block): one box = 64 channels of box_heads heads of box_tokens tokens.
 bool make_q_tensor_map(CUtensorMap *map, const void *base, int d, int H, long long T, long long sh, long long st, int box_heads,
                        int box_tokens)
 {
@@ -551,6 +549,9 @@ bool make_q_tensor_map(CUtensorMap *map, const void *base, int d, int H, long lo
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// 5-D map over (64 channels, token, 64-channel block, head, layer).  One box = box_tokens tokens of one head of
+// one layer, laid out in shared memory as [channel block][token][64 channels] with the 128-byte swizzle.
+// box_cblocks: 64-channel blocks per box (0: all d / 64 of them; 1: one block, selected by the copy's third coordinate).
 bool make_kv_tensor_map(CUtensorMap *map, const void *base, int d, int H, long long T, int L,
                         long long sh, long long st, long long sl, int box_tokens, int box_cblocks)
 {
