@@ -75,7 +75,8 @@ cudaError_t launch_rope_rotate(void *k, int L, int H, int d, long long T, long l
 // heads of 128 channels in 47 us (5.7 TB/s); 51 us when every thread held the angles of eight pairs in registers and
 // streamed eight heads, 53 us with eight pieces in flight and fewer blocks.
 // Angles are turns in 0.64 fixed point: pos * f modulo 2^64 is exact for every 32-bit position, so the angle is off by
-// at most pos * 2^-56 turns (the frequency's own rounding) plus the 2^-24 turns of the sine's argument.
+// at most pos * 2^-56 turns (the frequency's own rounding) plus just under 2^-23 turns (the sine's argument is cut to 23
+// bits, always downwards).
 struct RopeAxesArgs {
     const __nv_bfloat16 *x;
     __nv_bfloat16 *out;
