@@ -197,9 +197,10 @@ __device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int
     }
     if (tid == 0) { share->begin = 0; share->end = 0; }
     __syncthreads();
-    // unit index u: the last request b with floor(cu[b] group / ROWS) + b <= u (some indices are no unit); 32 bits hold
-    // rows * query heads, checked by the host
-    auto first_unit = [&](int b) { return pa_unit_of<ROWS>(a, min(max(cu[b], 0), a.n_rows)) + b; };
+    // unit index u: the last request b with floor((cu[b] - cu[0]) group / ROWS) + b <= u (some indices are no unit); 32 bits
+    // hold rows * query heads, checked by the host
+    const int cu0 = cu[0];                       // not 0 for the later requests of a batch, called by themselves
+    auto first_unit = [&](int b) { return pa_unit_of<ROWS>(a, min(max(cu[b] - cu0, 0), a.n_rows)) + b; };
     const int n_units = pa_unit_of<ROWS>(a, a.n_rows) + B;
     const int per = (n_units + THREADS - 1) / THREADS;
     const int u0 = min(n_units, tid * per), u1 = min(n_units, u0 + per);

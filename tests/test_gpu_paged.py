@@ -416,6 +416,22 @@ def test_attention_rows_past_the_room_are_dropped(new, H, group, d):
         assert int(_workspace(d)[:8192].sum()) == 0
 
 
+@pytest.mark.parametrize("new", [[5, 70, 1, 1, 33], [1, 1, 1, 1, 1, 1], [600, 3, 0, 2], [0, 0, 20, 300]])
+@pytest.mark.parametrize("H,group,d", [(2, 1, 128), (1, 5, 64), (2, 8, 128), (1, 130, 64)])
+def test_attention_later_requests_of_a_batch_by_themselves(H, group, d, new):
+    """Slices of the tables of a batch, with all of its queries: the first row is not row 0, and rows before it stay as they are."""
+    q, k, v, table, cu, total = _batch(new, [n + 40 * b for b, n in enumerate(new)], H, group, d, 16)
+    whole, tol = ref.attention(q, k[0], v[0], table, cu, total, d ** -0.5)
+    for first, last in ((1, len(new)), (2, len(new)), (len(new) - 1, len(new)), (1, 3)):
+        for max_new in (1, 0):
+            out = torch.full(q.shape, 5.0, dtype=torch.bfloat16, device=DEV)
+            _attend(q, k, v, table[first:last], cu[first:last + 1], total[first:last], max_new=max_new, out=out)
+            a, b = cu[first], cu[last]
+            assert ((out[a:b].double() - whole[a:b]).abs() <= tol[a:b]).all()
+            assert (out[:a] == 5).all() and (out[b:] == 5).all()
+            assert int(_workspace(d)[:8192].sum()) == 0
+
+
 def test_attention_large_scores_and_layers():
     q, k, v, table, cu, total = _batch([1, 3], [200, 100], 2, 4, 128, 16, layers=3, layer=2)
     _compare(q * 30, k, v, table, cu, total, layer=2)
