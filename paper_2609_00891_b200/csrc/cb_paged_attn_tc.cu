@@ -104,6 +104,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
     // last copy went to `landed`, and the parity of its next phase there; copies of each query tile.
     struct Flight { int issued; uint32_t on_landed, landings, n_query[2]; };
     Flight *flight = reinterpret_cast<Flight *>(tmem_slot + 3);
+    volatile int *moves = &flight->issued;                  // counted up per stage, for the waits that outlast many tiles
 
     const PagedArgs &a = P.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -178,11 +179,12 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                             tma_load_5d(dst + cb * C::BLK + ((size_t)i << (box_log2 + 7)), comp ? &P.v : &P.k, bar, 0, slot, cb, w.h, page);
                         st.next();
                         ++issued;
+                        if (lane == 0) *moves = issued;
                     }
                 }
                 more = !dead && w.next(a);
             }
-            if (lane == 0) { flight->issued = issued; flight->on_landed = on_landed; flight->landings = landings; }
+            if (lane == 0) { flight->on_landed = on_landed; flight->landings = landings; }
         }
     } else if (warp == 10) {
         // ================================ clears rows of V tiles ================================
@@ -194,7 +196,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                     const int j0 = pa_tile(w.u, t) * C::KT;
                     stage = (stage + 1) % C::NS;           // past the K tile
                     if (pa_clears<C::KT>(a, w.u, j0)) {
-                        if (!mbar_wait_suspended_warp(&landed[stage], (uses >> stage) & 1, abort_flag)) { dead = true; break; }
+                        if (!mbar_wait_while_moving_warp(&landed[stage], (uses >> stage) & 1, abort_flag, moves)) { dead = true; break; }
                         uses ^= 1u << stage;
                         uint8_t *dst = kv + (size_t)stage * C::TILE;
                         // keys outside [lo_key, hi_key) and behind the sinks: nobody sees them
@@ -224,7 +226,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
             uint32_t n = 0, n_query[2] = {0, 0};
             bool more = true;
             while (more && !dead) {
-                if (!mbar_wait_suspended_warp(&info_empty[n & 1], ((n >> 1) & 1) ^ 1, abort_flag)) { dead = true; break; }
+                if (!mbar_wait_while_moving_warp(&info_empty[n & 1], ((n >> 1) & 1) ^ 1, abort_flag, moves)) { dead = true; break; }
                 if (lane == 0) {
                     TcPiece &p = info[n & 1];
                     p.t0 = w.t; p.t1 = w.t1;
@@ -241,7 +243,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     if (i >= tiles) break;
-                    if (!mbar_wait_to_issue_warp(&q_empty[i], (n_query[i] & 1) ^ 1, abort_flag)) { dead = true; break; }
+                    if (!mbar_wait_while_moving_warp(&q_empty[i], (n_query[i] & 1) ^ 1, abort_flag, moves)) { dead = true; break; }
                     ++n_query[i];
                     // rows behind the request's are another one's, or zeros, or an earlier tile's: nobody reads their results
                     if (lane == 0) {
@@ -255,7 +257,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                 more = w.next(a);
             }
             if (lane == 0) { flight->n_query[0] = n_query[0]; flight->n_query[1] = n_query[1]; }
-            if (!dead && mbar_wait_suspended_warp(&info_empty[n & 1], ((n >> 1) & 1) ^ 1, abort_flag) && lane == 0) {
+            if (!dead && mbar_wait_while_moving_warp(&info_empty[n & 1], ((n >> 1) & 1) ^ 1, abort_flag, moves) && lane == 0) {
                 info[n & 1].t0 = -1;
                 mbar_arrive(&info_full[n & 1]);
             }
@@ -374,7 +376,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
                 }
         };
         for (uint32_t n = 0; any; ++n) {
-            if (!mbar_wait_suspended_warp(&info_full[n & 1], (n >> 1) & 1, abort_flag)) {
+            if (!mbar_wait_while_moving_warp(&info_full[n & 1], (n >> 1) & 1, abort_flag, moves)) {
                 // time-out: the parts that this block will not write still count, or the next call would wait for them
                 if (lane == 0) settle(i, n);
                 break;

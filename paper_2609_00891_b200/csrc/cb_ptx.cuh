@@ -90,13 +90,12 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t *bar, uint32_t parity, v
 }
 
 // The same bounded wait for kernels whose waiting warps share a scheduler with warps that compute: the thread is suspended
-// in the barrier unit for up to ~1 ms per poll instead of polling (a spinning warp takes issue slots: measured, the
-// exponentials of an attention tile took 1,300 cycles beside a spinning warp and 600 without one).  abort_flag as above;
-// the limit counts in units of 1,024 polls, so that it stays a few seconds.
-__device__ __forceinline__ bool mbar_wait_suspended(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
+// in the barrier unit, for 4 us a poll as measured (whatever longer time the hint names), instead of polling (a spinning
+// warp takes issue slots: measured, the exponentials of an attention tile took 1,300 cycles beside a spinning warp and 600
+// without one).  abort_flag as above; the limit counts in units of four polls: 2^20 of them, four seconds.
+__device__ __forceinline__ bool mbar_poll_suspended(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
 {
-    if (mbar_try_wait(bar, parity)) return true;
-    const uint32_t limit = 1u + ((uint32_t)abort_flag[1] >> 10);
+    const uint32_t limit = 1u + ((uint32_t)abort_flag[1] >> 2);
     for (uint32_t i = 0; i < limit; ++i) {
         uint32_t ok;
         asm volatile(
@@ -111,8 +110,31 @@ __device__ __forceinline__ bool mbar_wait_suspended(uint64_t *bar, uint32_t pari
         if (ok) return true;
         if (abort_flag[0]) return false;
     }
+    return false;
+}
+__device__ __forceinline__ bool mbar_wait_suspended(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
+{
+    if (mbar_try_wait(bar, parity) || mbar_poll_suspended(bar, parity, abort_flag)) return true;
     abort_flag[0] = 1;
     return false;
+}
+// For a wait that lasts as long as others' work on many tiles: it runs out only when `moves`, which a warp of the block
+// counts up with that work, has stood still for as long as the limit.
+__device__ __forceinline__ bool mbar_wait_while_moving(uint64_t *bar, uint32_t parity, volatile int *abort_flag, volatile int *moves)
+{
+    if (mbar_try_wait(bar, parity)) return true;
+    int seen, now = *moves;
+    do {
+        seen = now;
+        if (mbar_poll_suspended(bar, parity, abort_flag)) return true;
+        now = *moves;
+    } while (now != seen && abort_flag[0] == 0);
+    abort_flag[0] = 1;
+    return false;
+}
+__device__ __forceinline__ bool mbar_wait_while_moving_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag, volatile int *moves)
+{
+    return __all_sync(0xffffffffu, mbar_wait_while_moving(bar, parity, abort_flag, moves)) != 0;
 }
 // Warp-wide, with a warp-uniform outcome; all 32 lanes must call it.
 __device__ __forceinline__ bool mbar_wait_suspended_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag)

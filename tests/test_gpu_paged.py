@@ -416,6 +416,35 @@ def test_attention_rows_past_the_room_are_dropped(new, H, group, d):
         assert int(_workspace(d)[:8192].sum()) == 0
 
 
+@pytest.mark.parametrize("heads,group,new,total", [(1, 1, 150 * 256, 2_000_003), (2, 1, 40_100, 2_000_003), (1, 8, 12_000, 1_500_001)])
+def test_attention_pieces_longer_than_any_wait_within_a_tile(heads, group, new, total):
+    """Blocks with one or several pieces of 20 ms and more: the warps that wait from piece to piece outlast them."""
+    d, page = 64, 256
+    pages = -(-total // page)
+    k, v = _pool(1, pages, page, heads, d, False, seed=2)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    q = torch.randn(new, heads * group, d, generator=g, device=DEV).bfloat16()
+    table = torch.randperm(pages, generator=g, device=DEV).int()[None]
+    out = _attend(q, k, v, table, [0, new], [total], max_new=0)
+    cb.cb_last_device_status()
+    assert int(_workspace(d)[:8192].sum()) == 0
+    rows = torch.tensor([0, 1, 255, 256, new // 2, new - 1], device=DEV)
+    for h in range(heads):
+        kd, vd = (x[0][table[0].long()].flatten(0, 1)[:total, h].double() for x in (k, v))
+        for r in rows.tolist():
+            n = total - new + r + 1
+            qr = q[r, h * group:(h + 1) * group].double()
+            s = qr @ kd[:n].T * d ** -0.5
+            w = torch.softmax(s, -1)
+            want, size = w @ vd[:n], w @ vd[:n].abs()
+            # as in the plain form's tolerance, and the fp32 sums of n weights and products (in tiles of 128, then one tile after
+            # the other): n / 128 + 128 roundings of 2^-24, of the sum and of the weighted values
+            worst = float((qr.abs() @ kd[:n].abs().T).max()) * d ** -0.5
+            tol = want.abs() * 2.0 ** -8 + size * (2.0 ** -8 + 2 * (2 * d * 2.0 ** -24 * worst + 2.0 ** -20) + 2 * (n / 128 + 128) * 2.0 ** -24)
+            assert ((out[r, h * group:(h + 1) * group].double() - want).abs() <= tol).all()
+
+
 @pytest.mark.parametrize("new", [[5, 70, 1, 1, 33], [1, 1, 1, 1, 1, 1], [600, 3, 0, 2], [0, 0, 20, 300]])
 @pytest.mark.parametrize("H,group,d", [(2, 1, 128), (1, 5, 64), (2, 8, 128), (1, 130, 64)])
 def test_attention_later_requests_of_a_batch_by_themselves(H, group, d, new):
