@@ -226,9 +226,9 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
     const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(pool->k) + layer * pool->stride_layer;
     const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(pool->v) + layer * pool->stride_layer;
     // Up to 16 flattened rows per request and KV head: the warp-level kernel, which has no rows to pad.  Measured on 16
-    // requests of 8,192 keys, 8 KV heads (537 MB), warp-level against tensor-memory kernel: 8 rows 98 / 113 us, 16 rows
-    // 103 / 114 us, 32 rows 138 / 115 us, 64 rows 282 / 115 us.  (And more than 128 query heads per KV head, which do not
-    // fit a tile.)
+    // requests of 8,192 keys, 8 KV heads (537 MB), pages of 16 and 64, warp-level against tensor-memory kernel: 8 rows 94 - 97
+    // / 109 - 125 us, 16 rows 98 - 102 / 109 - 121 us, 32 rows 176 / 117 - 125 us, 64 rows 335 / 125 - 135 us.  (And more than
+    // 128 query heads per KV head, which do not fit a tile.)
     const bool few = (long long)max_new * a.group <= 16 || a.group > 128;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const cudaError_t e = few ? launch_paged_attn_few(a, pool->head_dim, k, v, pool->page_size, pool->stride_page, pool->stride_slot, pool->stride_head, max_new, st)

@@ -180,7 +180,8 @@ struct alignas(16) PaSum { long long tiles; int units, most; };
 // finds the block's start.
 // Where there are no more pairs than blocks and the longest one is at most EVEN tiles above an equal share, every pair goes
 // to a block of its own: joining two parts costs about that much (32 requests with a window of 1,024 keys, 256 pairs of 17
-// or 18 tiles of 64 keys: 38 us split, see k_paged_attn_few).
+// or 18 tiles of 64 keys: 38 us split, see k_paged_attn_few; for the tensor-memory kernel the number was taken over, not
+// measured).
 template <int ROWS, int KT, int THREADS>
 __device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int cap, PaShare *share, PaSum *sums)
 {

@@ -10,8 +10,8 @@
 //                   entry can make the copy fault.
 //   4 consumer warps   a warp owns 16 rows and 64 MT / 4 keys of a tile and carries its own running maximum, sum and
 //                   output, so that the main loop has no barrier between warps; they are joined at the end of a piece.
-// Measured: 64 requests of 512 to 8,192 keys, 8 KV heads x 8 query heads x 128: 205 us for 1.30 GB = 6.3 TB/s; one request
-// of 1,024 keys 9.5 us in a graph, of which the schedule takes 2, the copies 1.3, the tiles 1.5, the joins 3.
+// Measured: 64 requests of 512 to 8,192 keys, 8 KV heads x 8 query heads x 128: 205 - 214 us for 1.30 GB = 6.05 - 6.3 TB/s
+// (box to box), of 64 channels 154 us for 0.62 GB; one request of 1,024 keys 9.6 - 11 us in a graph, of which the schedule takes 2, the copies 1.3, the tiles 1.5, the joins 3.
 // A wait that runs out is not followed by another one: the block runs through to its end, so that every barrier and join
 // counter is served as in a good run, and sets the status word; its rows are then not valid.  No copy is issued after it,
 // and the block ends only when those in flight have landed.

@@ -13,12 +13,17 @@
 //   2 x 4 softmax warps   one thread per row: scores to registers, running maximum, exp2, weights as bf16 back over the
 //                    scores in tensor memory.  The output is rescaled only when a maximum grows by more than 2^8 (weights
 //                    stay below 2^8, sums and outputs are fp32), which after the first tiles is hardly ever.
-// The tensor pipe runs a warp's products in order, so that S_i of the next tile may overwrite P_i, and its completion also
-// says that P_i V of the tile before is complete.
+// S_i of the next tile overwrites P_i, issued right after the P_i V that reads it and without a wait: this relies on the
+// tensor pipe running one thread's products in the order of issue, which holds on this machine (every test, repeated runs
+// bitwise) but which PTX promises only for products with one accumulator and shape.  A commit and a wait between the two
+// would make it independent of that: measured, the long chunk below 1,726 -> 1,815 us.  A commit covers everything issued
+// before it, so that the scores' completion also says that P_i V of the tile before is complete.
 // Bound by the two tiles taking turns: ~3,100 cycles for 128 keys of both, of which the products run 2,048 and the
 // special-function unit 2,048; on long runs by the board's power limit.  Measured, 64 query heads of 128 on 8 KV heads:
-// 4,096 rows over 16,384 keys 1.6 - 1.75 ms = 1.1 - 1.2 PFLOP/s; 8,192 rows of a prompt 1.3 ms; 16 requests of 16 rows over
-// 8,192 keys 115 us (4.7 TB/s).
+// 4,096 rows over 16,384 keys 1.7 - 1.75 ms = 1.1 PFLOP/s; a prompt of 8,192 rows (one request, nothing before it) 1.33 ms =
+// 0.83 PFLOP/s: the line gives every block 450 tiles, but those at its begin are of one to five tiles a piece, and the first
+// block walks 154 pieces where the others walk 14; a piece costs 7,600 cycles beside its tiles, the same number for every
+// prompt measured.  16 requests of 2 to 16 rows over 8,192 keys 109 - 144 us (4.9 - 3.7 TB/s), by rows and page size.
 #include "cb_paged.cuh"
 #include "cb_ptx.cuh"
 #include "cb_math.cuh"
