@@ -92,6 +92,18 @@ def test_tables_room_for_fewer_rows_and_no_requests():
     _check_tables(want, out, bt)
 
 
+@pytest.mark.parametrize("at", [1, 2, 3])
+def test_tables_into_rows_that_are_not_16_byte_aligned(at):
+    want, out, bt, _, args = _tables([5, 0, 1000, 30], [2049, 7, 1, 600], 16, pad=9)
+    n = out["pos"].numel()
+    pos, slot = torch.full((n + at + 2,), -9, dtype=torch.int32, device=DEV), torch.full((n + at + 2,), -9, dtype=torch.int64, device=DEV)
+    out["pos"], out["slot"] = pos[at:at + n], slot[at:at + n]
+    cb.cb_page_tables(*args[:7], out["pos"], out["slot"], out["used"])
+    _check_tables(want, out, bt)
+    for x in (pos, slot):
+        assert (x[:at] == -9).all() and (x[at + n:] == -9).all()
+
+
 # ---------------------------------------------------------------------------------------------------- store
 def _pool(L, pages, page, H, d, hnd, fill=None, seed=0):
     g = torch.Generator(device=DEV)
