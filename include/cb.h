@@ -535,6 +535,79 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
                              const int32_t *cu_new, const int32_t *total_len, int32_t n_requests, int32_t max_new,
                              float scale, int32_t window, int32_t n_sink, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * The paged cache held in 8 bits (no counterpart in the paper): half the bytes of a bf16 cache, which are a decode step's
+ * time, and twice the contexts in the same memory.  Three calls beside cb_page_tables:
+ *     cb_paged_store8       rows quantised as they are written into their pages
+ *     cb_paged_load8        rows read back (to be mapped to another model, or handed to an engine with a bf16 cache)
+ *     cb_paged_attention8   attention of the new rows of every request over its pages
+ * Capture, devices and request counts as for the calls above.
+ *
+ * cb_page_pool8: codes of K and V of all layers, e4m3 (largest 448) or int8 (largest 127; -128 is not used), and a power of
+ * two for each block of `block` rows of a page and KV head:
+ *     value(layer, page, slot, head, c) = code * 2^exp
+ *     code at (uint8*)k + layer*stride_layer + page*stride_page + slot*stride_slot + head*stride_head + c
+ *     exp  at k_exp + layer*exp_stride_layer + page*exp_stride_page + (slot / block)*exp_stride_block + head*exp_stride_head
+ * Channels are contiguous, k and v 16-byte aligned, code strides (bytes) multiples of 16, exponents anywhere; strides below
+ * 2^40, 0 only on a dimension of size 1 (CB_ERR_UNSUPPORTED otherwise).  head_dim 64 or 128; page_size 8, 16, 32, 64, 128 or
+ * 256; block one of these too, at most page_size; n_pages < 2^31.  Exponents lie in -100 .. 119 (e4m3) or .. 121 (int8), and
+ * one outside counts as the nearest of these.  A cache needs no initialisation.
+ */
+enum { CB_CACHE_E4M3 = 0, CB_CACHE_INT8 = 1 };
+typedef struct cb_page_pool8 {
+    void *k;
+    void *v;
+    int8_t *k_exp;
+    int8_t *v_exp;
+    int32_t n_layers, n_heads, head_dim, page_size;
+    int32_t format, block;
+    int64_t n_pages;
+    int64_t stride_layer, stride_page, stride_slot, stride_head;
+    int64_t exp_stride_layer, exp_stride_page, exp_stride_block, exp_stride_head;
+} cb_page_pool8;
+
+/*
+ * Quantises row t of every layer and head into slot slot_map[t] (as cb_paged_store: device int64 [n_rows]; negative or past
+ * the pool: the row is skipped; all layers at once, or one through a pool that describes that layer alone).  For each block
+ * that rows fall into, head, and K or V, with a the largest magnitude of those rows:
+ *     need = the least exponent with a * 2^-need <= 448 (e4m3) or 127 (int8)
+ *     exp' = need                    if one of the rows is the block's first (the block begins anew: nothing in it counts)
+ *            max(exp, need)          otherwise; where that is larger, the codes of the block become round(code * 2^(exp - exp'))
+ *     code = round(x * 2^-exp')      to the nearest code, ties to even
+ * So a request's rows are written in order of their positions, in any number of calls; a row may be written again (the
+ * exponent then stays at least what it was).  The scaling is exact and the result does not depend on the order of work.
+ * The rows of one block stand together in slot_map, with at most 31 skipped rows between two of them, as cb_page_tables
+ * leaves them (where they do not, the block's contents are unspecified); of two rows with one slot either may end there,
+ * piece by piece.  Rows must be finite: an infinity becomes the largest code of a block whose other rows vanish beside it,
+ * NaN becomes e4m3's NaN or int8's 0.  (Of int8 codes, magnitudes of 2^127 and more become 127 * 2^121.)
+ * src_k / src_v: as for cb_paged_store (bf16 or fp32, 16-byte aligned, strides in elements, multiples of 8), not in the pool.
+ */
+cb_status cb_paged_store8(const cb_page_pool8 *pool, const void *src_k, const void *src_v, int32_t src_dtype, int64_t n_rows,
+                          int64_t stride_layer, int64_t stride_token, int64_t stride_head, const int64_t *slot_map, void *stream);
+
+/*
+ * Reads the row at slot slot_map[t] of every layer and head into row t of dst_k and dst_v (device, CB_DTYPE_BF16 or
+ * CB_DTYPE_F32, both exact; 16-byte aligned, strides in elements, multiples of 8, 0 only on a dimension of size 1; the two
+ * must not overlap each other or the pool).  A slot that is negative or past the pool: the row is left as it is.  A slot may
+ * occur any number of times, in any order.
+ */
+cb_status cb_paged_load8(const cb_page_pool8 *pool, void *dst_k, void *dst_v, int32_t dst_dtype, int64_t n_rows,
+                         int64_t stride_layer, int64_t stride_token, int64_t stride_head, const int64_t *slot_map, void *stream);
+
+/*
+ * cb_paged_attention over a pool of 8 bits: the same arguments, rows, masks, splits, and promises (and the same test hooks
+ * and device status), with its own workspace size.  Codes become 16-bit numbers exactly.  Weights are rounded to fp16
+ * (2^-11 of each that is above 2^-20 of the largest) or bf16 (2^-8), as max_new chooses between kernels.  Rows of a page
+ * that no row of the request sees may hold anything, and so may the exponents of blocks without a seen row; values that
+ * some row sees must be finite and below 2^90.
+ */
+cb_status cb_paged_attention8_workspace_bytes(int32_t head_dim, size_t *bytes);
+cb_status cb_paged_attention8(const cb_page_pool8 *pool, int32_t layer, const void *q, int64_t q_stride_token, int64_t q_stride_head,
+                              void *out, int64_t o_stride_token, int64_t o_stride_head, int64_t n_rows, int32_t n_q_heads,
+                              const int32_t *block_table, int64_t table_stride, int32_t max_pages,
+                              const int32_t *cu_new, const int32_t *total_len, int32_t n_requests, int32_t max_new,
+                              float scale, int32_t window, int32_t n_sink, void *workspace, size_t workspace_bytes, void *stream);
+
 /*
  * Synchronises the stream and reads the context's device status word: CB_OK, or CB_ERR_TIMEOUT if a bounded
  * wait inside a kernel ran out (the statistics are then invalid; reset before reuse).

@@ -22,6 +22,7 @@ CB_ERR_INVALID_ARG, CB_ERR_UNSUPPORTED, CB_ERR_STATE, CB_ERR_WORKSPACE = 1, 2, 3
 CB_ERR_CUDA, CB_ERR_NOT_PD, CB_ERR_TIMEOUT, CB_ERR_STATIC_LIMIT = 5, 6, 7, 8
 CB_FLAG_COMPENSATED, CB_FLAG_RAW_LAMBDA, CB_FLAG_SIMT, CB_FLAG_ONE_ROW_HEAD = 1, 2, 4, 8
 CB_DTYPE_BF16, CB_DTYPE_F32 = 0, 1
+CB_CACHE_E4M3, CB_CACHE_INT8 = 0, 1
 
 EXPORTS = ("cb_status_string", "cb_head_map_nearest", "cb_work_list", "cb_workspace_bytes", "cb_token_splits", "cb_create",
            "cb_destroy", "cb_stats_reset", "cb_stats_accumulate", "cb_staging_bytes", "cb_stats_accumulate_host",
@@ -36,7 +37,8 @@ EXPORTS = ("cb_status_string", "cb_head_map_nearest", "cb_work_list", "cb_worksp
            "cb_means_energy", "cb_probe_r2", "cb_probe_scores", "cb_rank_layers",
            "cb_last_device_status", "cb_test_hooks", "cb_stats_state_bytes", "cb_stats_export", "cb_stats_import",
            "cb_last_cuda_error", "cb_launch_count",
-           "cb_page_tables", "cb_paged_store", "cb_rope_axes", "cb_paged_attention_workspace_bytes", "cb_paged_attention")
+           "cb_page_tables", "cb_paged_store", "cb_rope_axes", "cb_paged_attention_workspace_bytes", "cb_paged_attention",
+           "cb_paged_store8", "cb_paged_load8", "cb_paged_attention8_workspace_bytes", "cb_paged_attention8")
 
 
 class CbError(RuntimeError):
@@ -87,6 +89,8 @@ def lib() -> ctypes.CDLL:
         L.cb_rope_axes.argtypes = [p, p, i32, i32, i32, i64, i64, i64, i64, i64, i64, i64, p, i64, i32, p, i32, ctypes.c_double, i32, p]
         L.cb_paged_attention.argtypes = [p, i32, p, i64, i64, p, i64, i64, i64, i32, p, i64, i32, p, p, i32, i32, ctypes.c_float, i32, i32,
                                          p, ctypes.c_size_t, p]
+        L.cb_paged_store8.argtypes = L.cb_paged_load8.argtypes = L.cb_paged_store.argtypes
+        L.cb_paged_attention8.argtypes = L.cb_paged_attention.argtypes
         _lib = L
     return _lib
 
@@ -745,11 +749,7 @@ def cb_paged_attention_workspace_bytes(head_dim: int) -> int:
     return n.value
 
 
-def cb_paged_attention(q: torch.Tensor, out: torch.Tensor, pool: PagePool, layer: int, block_table: torch.Tensor,
-                       cu_new: torch.Tensor, total_len: torch.Tensor, scale: float, workspace: torch.Tensor,
-                       max_new: int = 0, window: int = 0, n_sink: int = 0, stream=None) -> None:
-    """Attention of new rows q [T][Hq][d] (bf16) over layer `layer` of the pool; block_table [B][max_pages], cu_new [B + 1],
-    total_len [B] as cb_page_tables leaves them; workspace: uint8, zero-filled once (torch.zeros)."""
+def _attention_call(q, out, pool, layer, block_table, cu_new, total_len, scale, workspace, max_new, window, n_sink, stream) -> tuple:
     T, Hq, d = q.shape
     qs, os_ = q.stride(), out.stride()
     assert q.dtype == torch.bfloat16 and out.dtype == torch.bfloat16 and q.shape == out.shape and qs[2] == 1 and os_[2] == 1
@@ -758,9 +758,87 @@ def cb_paged_attention(q: torch.Tensor, out: torch.Tensor, pool: PagePool, layer
     assert (cols <= 1 or block_table.stride(1) == 1) and cu_new.is_contiguous() and total_len.is_contiguous()
     assert cu_new.numel() == B + 1 and total_len.numel() == B and workspace.dtype == torch.uint8 and workspace.is_contiguous()
     st = _on_one_device(stream, q, out, pool.k, block_table, cu_new, total_len, workspace)
-    _check(lib().cb_paged_attention(pool.c, layer, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1], T, Hq, block_table.data_ptr(),
-                                    block_table.stride(0), cols, cu_new.data_ptr(), total_len.data_ptr(), B, max_new, scale, window, n_sink,
-                                    workspace.data_ptr(), workspace.numel(), st), "cb_paged_attention")
+    return (pool.c, layer, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1], T, Hq, block_table.data_ptr(), block_table.stride(0), cols,
+            cu_new.data_ptr(), total_len.data_ptr(), B, max_new, scale, window, n_sink, workspace.data_ptr(), workspace.numel(), st)
+
+
+def cb_paged_attention(q: torch.Tensor, out: torch.Tensor, pool: PagePool, layer: int, block_table: torch.Tensor,
+                       cu_new: torch.Tensor, total_len: torch.Tensor, scale: float, workspace: torch.Tensor,
+                       max_new: int = 0, window: int = 0, n_sink: int = 0, stream=None) -> None:
+    """Attention of new rows q [T][Hq][d] (bf16) over layer `layer` of the pool; block_table [B][max_pages], cu_new [B + 1],
+    total_len [B] as cb_page_tables leaves them; workspace: uint8, zero-filled once (torch.zeros)."""
+    _check(lib().cb_paged_attention(*_attention_call(q, out, pool, layer, block_table, cu_new, total_len, scale, workspace, max_new, window,
+                                                     n_sink, stream)), "cb_paged_attention")
+
+
+class _PagePool8(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("n_layers", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("format", ctypes.c_int32), ("block", ctypes.c_int32), ("n_pages", ctypes.c_int64),
+                ("stride_layer", ctypes.c_int64), ("stride_page", ctypes.c_int64), ("stride_slot", ctypes.c_int64),
+                ("stride_head", ctypes.c_int64),
+                ("exp_stride_layer", ctypes.c_int64), ("exp_stride_page", ctypes.c_int64), ("exp_stride_block", ctypes.c_int64),
+                ("exp_stride_head", ctypes.c_int64)]
+
+
+_PAGE_POOL8 = struct.Struct("PPPPiiiiiiqqqqqqqqq")
+
+
+class PagePool8:
+    """A cache held in 8 bits: codes of K and V (torch.float8_e4m3fn or torch.int8, which is the format) indexed
+    [layer][page][slot][head][channel], any strides, channels contiguous; exponents (int8) [layer][page][block of rows][head]."""
+
+    __slots__ = ("k", "v", "k_exp", "v_exp", "n_layers", "n_heads", "head_dim", "page_size", "n_pages", "block", "c")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor):
+        strides, shape, exps, code = k.stride(), k.shape, k_exp.stride(), k.dtype
+        sl, sp, ss, sh, sc = strides
+        L, N, S, H, d = shape
+        n = k_exp.shape[2]
+        assert (code is torch.float8_e4m3fn or code is torch.int8) and v.dtype is code and v.shape == shape and v.stride() == strides and sc == 1
+        assert k_exp.dtype is torch.int8 and v_exp.dtype is torch.int8 and k_exp.shape == (L, N, n, H) == v_exp.shape and exps == v_exp.stride()
+        assert n > 0 and S % n == 0
+        dev = k.get_device()
+        assert dev == v.get_device() == k_exp.get_device() == v_exp.get_device()
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.n_layers, self.n_pages, self.page_size, self.n_heads, self.head_dim, self.block = L, N, S, H, d, S // n
+        self.c = _PAGE_POOL8.pack(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), L, H, d, S,
+                                  CB_CACHE_INT8 if code is torch.int8 else CB_CACHE_E4M3, S // n, N, sl, sp, ss, sh, *exps)
+
+
+def _rows8(pool: PagePool8, k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, stream) -> tuple:
+    L, T, H, d = k.shape
+    ss = k.stride()
+    assert k.dtype == v.dtype and k.shape == v.shape and ss == v.stride() and ss[3] == 1
+    assert L == pool.n_layers and H == pool.n_heads and d == pool.head_dim
+    assert slot_map.dtype == torch.int64 and slot_map.is_contiguous() and slot_map.numel() == T
+    dt = CB_DTYPE_BF16 if k.dtype == torch.bfloat16 else {torch.float32: CB_DTYPE_F32}[k.dtype]
+    st = _on_one_device(stream, pool.k, k, v, slot_map)
+    return pool.c, k.data_ptr(), v.data_ptr(), dt, T, ss[0], ss[1], ss[2], slot_map.data_ptr(), st
+
+
+def cb_paged_store8(pool: PagePool8, src_k: torch.Tensor, src_v: torch.Tensor, slot_map: torch.Tensor, stream=None) -> None:
+    """Rows [L][T][H][d] (bf16 or fp32) of all layers, quantised into the slots slot_map [T] (int64, -1: skipped)."""
+    _check(lib().cb_paged_store8(*_rows8(pool, src_k, src_v, slot_map, stream)), "cb_paged_store8")
+
+
+def cb_paged_load8(pool: PagePool8, dst_k: torch.Tensor, dst_v: torch.Tensor, slot_map: torch.Tensor, stream=None) -> None:
+    """The rows at slots slot_map [T] (int64, -1: the row is left as it is) of all layers into dst [L][T][H][d] (bf16 or fp32)."""
+    _check(lib().cb_paged_load8(*_rows8(pool, dst_k, dst_v, slot_map, stream)), "cb_paged_load8")
+
+
+def cb_paged_attention8_workspace_bytes(head_dim: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().cb_paged_attention8_workspace_bytes(head_dim, ctypes.byref(n)), "cb_paged_attention8_workspace_bytes")
+    return n.value
+
+
+def cb_paged_attention8(q: torch.Tensor, out: torch.Tensor, pool: PagePool8, layer: int, block_table: torch.Tensor,
+                        cu_new: torch.Tensor, total_len: torch.Tensor, scale: float, workspace: torch.Tensor,
+                        max_new: int = 0, window: int = 0, n_sink: int = 0, stream=None) -> None:
+    """As cb_paged_attention, over layer `layer` of a pool of 8 bits."""
+    _check(lib().cb_paged_attention8(*_attention_call(q, out, pool, layer, block_table, cu_new, total_len, scale, workspace, max_new, window,
+                                                      n_sink, stream)), "cb_paged_attention8")
 
 
 def cb_device_status(ctx: Context, stream=None) -> None:

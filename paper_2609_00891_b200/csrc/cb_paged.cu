@@ -1,11 +1,12 @@
 // Host side of the paged target cache: argument checks and launches (page tables, store, rotary positions with several
-// axes, attention).
+// axes, attention; store, read-back and attention of a cache held in 8 bits).
 #include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <iterator>
 
 #include "cb_paged.cuh"
+#include "cb_paged8.cuh"
 #include "cb_rope.cuh"
 
 using namespace cb;
@@ -55,6 +56,125 @@ cb_status launch_state(Args &a)
     a.poll_limit = h.poll_limit;
     a.starve = h.starve;
     a.give_up = h.give_up;
+    return CB_OK;
+}
+
+// The checks and the kernels' arguments that both kinds of cache share.  `nothing`: no rows, no requests: no launch.
+struct AttnCall {
+    const void *q;
+    int64_t q_stride_token, q_stride_head;
+    void *out;
+    int64_t o_stride_token, o_stride_head, n_rows;
+    int32_t n_q_heads;
+    const int32_t *block_table;
+    int64_t table_stride;
+    int32_t max_pages;
+    const int32_t *cu_new, *total_len;
+    int32_t n_requests, max_new;
+    float scale;
+    int32_t window, n_sink;
+    void *workspace;
+    size_t workspace_bytes;
+};
+cb_status attention_args(const AttnCall &c, int32_t layer, int32_t n_layers, int32_t n_heads, int page_log2, int64_t n_pages, size_t need,
+                         PagedArgs &a, int32_t &max_new, bool &nothing)
+{
+    nothing = false;
+    if (layer < 0 || layer >= n_layers || c.n_rows < 0 || c.n_q_heads <= 0 || c.n_requests < 0 || c.max_pages <= 0 || c.max_new < 0 ||
+        c.table_stride < 0 || c.window < 0 || c.n_sink < 0)
+        return CB_ERR_INVALID_ARG;
+    const float scale_log2 = (float)(c.scale * 1.4426950408889634074);
+    if (c.n_q_heads % n_heads || !(c.scale > 0.f) || !std::isfinite(scale_log2)) return CB_ERR_INVALID_ARG;
+    if (c.q_stride_token < 0 || c.q_stride_head < 0 || c.o_stride_token < 0 || c.o_stride_head < 0) return CB_ERR_INVALID_ARG;
+    if ((c.q_stride_token | c.q_stride_head | c.o_stride_token | c.o_stride_head) & 7) return CB_ERR_INVALID_ARG;
+    if ((c.n_rows > 1 && (c.o_stride_token == 0 || c.q_stride_token == 0)) || (c.n_q_heads > 1 && (c.o_stride_head == 0 || c.q_stride_head == 0))) return CB_ERR_UNSUPPORTED;
+    if (c.q_stride_token >= (1ll << 39) || c.q_stride_head >= (1ll << 39)) return CB_ERR_UNSUPPORTED;
+    // flattened rows and units are counted in 32 bits
+    if (c.n_rows >= (1ll << 31) || c.n_rows * c.n_q_heads + c.n_requests >= (1ll << 31) || c.n_requests >= MAX_REQUESTS) return CB_ERR_UNSUPPORTED;
+    if (c.n_requests > 1 && c.table_stride < c.max_pages) return CB_ERR_INVALID_ARG;
+    if (c.n_rows == 0 || c.n_requests == 0) { nothing = true; return CB_OK; }
+    if (c.q == c.out) return CB_ERR_INVALID_ARG;         // rows are written while other blocks still read theirs
+    if (!c.q || !c.out || !c.block_table || !c.cu_new || !c.total_len) return CB_ERR_INVALID_ARG;
+    if ((((uintptr_t)c.q | (uintptr_t)c.out) & 15) || (((uintptr_t)c.block_table | (uintptr_t)c.cu_new | (uintptr_t)c.total_len) & 3)) return CB_ERR_INVALID_ARG;
+    if (!c.workspace || ((uintptr_t)c.workspace & 255) || c.workspace_bytes < need) return CB_ERR_WORKSPACE;
+    a.q = static_cast<const __nv_bfloat16 *>(c.q);
+    a.out = static_cast<__nv_bfloat16 *>(c.out);
+    a.q_st = c.q_stride_token; a.q_sh = c.q_stride_head; a.o_st = c.o_stride_token; a.o_sh = c.o_stride_head;
+    a.table = c.block_table; a.table_stride = c.table_stride; a.table_cols = c.max_pages;
+    a.cu = c.cu_new; a.total = c.total_len; a.n_requests = c.n_requests; a.n_rows = (int)c.n_rows;
+    a.Hkv = n_heads; a.group = c.n_q_heads / n_heads;
+    // n / d == mulhi(n, ceil(2^32 / d)) as long as n (d - 1) < 2^32
+    auto reciprocal = [](int64_t d, int64_t most) {
+        return d > 1 && (unsigned __int128)most * d < ((unsigned __int128)1 << 32) ? (unsigned)(((1ull << 32) + d - 1) / d) : 0u;
+    };
+    a.group_mul = reciprocal(a.group, c.n_rows * a.group);
+    // tensor-core kernel: a tile of 128 rows holds whole tokens, so that one copy brings it
+    a.unit_tokens = a.group <= 128 ? 2 * (128 / a.group) : 1;
+    a.unit_rows = a.unit_tokens * a.group;
+    a.unit_mul = reciprocal(a.unit_tokens, c.n_rows + a.unit_tokens);
+    a.page_log2 = page_log2;
+    a.n_pages = (int)n_pages;
+    a.window = c.window; a.n_sink = c.window > 0 ? c.n_sink : 0;
+    a.scale_log2 = scale_log2;
+    a.q_min = 2;
+    a.counters = static_cast<int *>(c.workspace);
+    a.part = reinterpret_cast<float *>(static_cast<char *>(c.workspace) + PA_COUNTER_BYTES);
+    const cb_status s = launch_state(a);
+    if (s != CB_OK) return s;
+    if (device_sm_count() * 8 > PA_COUNTERS) return CB_ERR_UNSUPPORTED;
+    max_new = c.max_new == 0 || c.max_new > c.n_rows ? (int32_t)c.n_rows : c.max_new;
+    return CB_OK;
+}
+
+cb_status check_pool8(const cb_page_pool8 *p)
+{
+    if (!p || p->n_layers <= 0 || p->n_heads <= 0 || p->head_dim <= 0 || p->page_size <= 0 || p->n_pages <= 0 || p->block <= 0) return CB_ERR_INVALID_ARG;
+    if (!p->k || !p->v || (((uintptr_t)p->k | (uintptr_t)p->v) & 15) || !p->k_exp || !p->v_exp) return CB_ERR_INVALID_ARG;
+    if (p->format != CB_CACHE_E4M3 && p->format != CB_CACHE_INT8) return CB_ERR_INVALID_ARG;
+    const int64_t all[] = {p->stride_layer, p->stride_page, p->stride_slot, p->stride_head};
+    const int64_t exps[] = {p->exp_stride_layer, p->exp_stride_page, p->exp_stride_block, p->exp_stride_head};
+    for (const int64_t x : all)
+        if (x < 0 || (x & 15)) return CB_ERR_INVALID_ARG;
+    for (const int64_t x : exps)
+        if (x < 0) return CB_ERR_INVALID_ARG;
+    if (p->head_dim != 64 && p->head_dim != 128) return CB_ERR_UNSUPPORTED;
+    if (page_log2_of(p->page_size) < 0 || page_log2_of(p->block) < 0 || p->block > p->page_size || p->n_pages >= (1ll << 31)) return CB_ERR_UNSUPPORTED;
+    // a broadcast over more than one layer, page, row or head: pieces of the cache, or exponents, would share memory
+    const bool more[] = {p->n_layers > 1, p->n_pages > 1, true, p->n_heads > 1}, more_exp[] = {p->n_layers > 1, p->n_pages > 1, p->page_size > p->block, p->n_heads > 1};
+    for (int i = 0; i < 4; ++i)
+        if ((more[i] && all[i] == 0) || (more_exp[i] && exps[i] == 0) || all[i] >= (1ll << 40) || exps[i] >= (1ll << 40)) return CB_ERR_UNSUPPORTED;
+    return CB_OK;
+}
+
+// As the kernels take it; first layer `layer`.
+Pool8 pool8_of(const cb_page_pool8 *p, int64_t layer)
+{
+    Pool8 q;
+    q.k = static_cast<uint8_t *>(p->k) + layer * p->stride_layer; q.v = static_cast<uint8_t *>(p->v) + layer * p->stride_layer;
+    q.ke = p->k_exp + layer * p->exp_stride_layer; q.ve = p->v_exp + layer * p->exp_stride_layer;
+    q.sl = p->stride_layer; q.sp = p->stride_page; q.ss = p->stride_slot; q.sh = p->stride_head;
+    q.el = p->exp_stride_layer; q.ep = p->exp_stride_page; q.eb = p->exp_stride_block; q.eh = p->exp_stride_head;
+    q.page_log2 = page_log2_of(p->page_size);
+    q.block_log2 = page_log2_of(p->block);
+    q.n_pages = (int)p->n_pages;
+    q.n_slots = p->n_pages << q.page_log2;
+    q.L = p->n_layers; q.H = p->n_heads; q.d = p->head_dim; q.format = p->format;
+    return q;
+}
+
+// Rows beside an 8-bit pool: what store and load check alike.
+cb_status check_rows8(const cb_page_pool8 *pool, const void *k, const void *v, int32_t dtype, int64_t n_rows, int64_t stride_layer,
+                      int64_t stride_token, int64_t stride_head, const int64_t *slot_map)
+{
+    const cb_status s = check_pool8(pool);
+    if (s != CB_OK) return s;
+    if (dtype != CB_DTYPE_BF16 && dtype != CB_DTYPE_F32) return CB_ERR_INVALID_ARG;
+    if (n_rows < 0 || stride_layer < 0 || stride_token < 0 || stride_head < 0) return CB_ERR_INVALID_ARG;
+    if ((stride_layer | stride_token | stride_head) & 7) return CB_ERR_INVALID_ARG;
+    if (n_rows >= (1ll << 31) || pool->n_layers > 65535 || pool->n_heads > 65535) return CB_ERR_UNSUPPORTED;
+    if (n_rows * pool->n_heads >= (1ll << 35)) return CB_ERR_UNSUPPORTED;      // blocks of one launch
+    if (n_rows == 0) return CB_OK;
+    if (!k || !v || !slot_map || (((uintptr_t)k | (uintptr_t)v) & 15) || ((uintptr_t)slot_map & 7)) return CB_ERR_INVALID_ARG;
     return CB_OK;
 }
 
@@ -177,52 +297,14 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
 {
     cb_status s = check_pool(pool);
     if (s != CB_OK) return s;
-    if (layer < 0 || layer >= pool->n_layers || n_rows < 0 || n_q_heads <= 0 || n_requests < 0 || max_pages <= 0 || max_new < 0 ||
-        table_stride < 0 || window < 0 || n_sink < 0)
-        return CB_ERR_INVALID_ARG;
-    const float scale_log2 = (float)(scale * 1.4426950408889634074);
-    if (n_q_heads % pool->n_heads || !(scale > 0.f) || !std::isfinite(scale_log2)) return CB_ERR_INVALID_ARG;
-    if (q_stride_token < 0 || q_stride_head < 0 || o_stride_token < 0 || o_stride_head < 0) return CB_ERR_INVALID_ARG;
-    if ((q_stride_token | q_stride_head | o_stride_token | o_stride_head) & 7) return CB_ERR_INVALID_ARG;
-    if ((n_rows > 1 && (o_stride_token == 0 || q_stride_token == 0)) || (n_q_heads > 1 && (o_stride_head == 0 || q_stride_head == 0))) return CB_ERR_UNSUPPORTED;
-    if (q_stride_token >= (1ll << 39) || q_stride_head >= (1ll << 39)) return CB_ERR_UNSUPPORTED;
-    // flattened rows and units are counted in 32 bits
-    if (n_rows >= (1ll << 31) || n_rows * n_q_heads + n_requests >= (1ll << 31) || n_requests >= MAX_REQUESTS) return CB_ERR_UNSUPPORTED;
-    if (n_requests > 1 && table_stride < max_pages) return CB_ERR_INVALID_ARG;
-    if (n_rows == 0 || n_requests == 0) return CB_OK;
-    if (q == out) return CB_ERR_INVALID_ARG;         // rows are written while other blocks still read theirs
-    if (!q || !out || !block_table || !cu_new || !total_len) return CB_ERR_INVALID_ARG;
-    if ((((uintptr_t)q | (uintptr_t)out) & 15) || (((uintptr_t)block_table | (uintptr_t)cu_new | (uintptr_t)total_len) & 3)) return CB_ERR_INVALID_ARG;
     size_t need = 0;
     cb_paged_attention_workspace_bytes(pool->head_dim, &need);
-    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return CB_ERR_WORKSPACE;
+    const AttnCall c = {q, q_stride_token, q_stride_head, out, o_stride_token, o_stride_head, n_rows, n_q_heads, block_table, table_stride, max_pages,
+                        cu_new, total_len, n_requests, max_new, scale, window, n_sink, workspace, workspace_bytes};
     PagedArgs a;
-    a.q = static_cast<const __nv_bfloat16 *>(q);
-    a.out = static_cast<__nv_bfloat16 *>(out);
-    a.q_st = q_stride_token; a.q_sh = q_stride_head; a.o_st = o_stride_token; a.o_sh = o_stride_head;
-    a.table = block_table; a.table_stride = table_stride; a.table_cols = max_pages;
-    a.cu = cu_new; a.total = total_len; a.n_requests = n_requests; a.n_rows = (int)n_rows;
-    a.Hkv = pool->n_heads; a.group = n_q_heads / pool->n_heads;
-    // n / d == mulhi(n, ceil(2^32 / d)) as long as n (d - 1) < 2^32
-    auto reciprocal = [](int64_t d, int64_t most) {
-        return d > 1 && (unsigned __int128)most * d < ((unsigned __int128)1 << 32) ? (unsigned)(((1ull << 32) + d - 1) / d) : 0u;
-    };
-    a.group_mul = reciprocal(a.group, n_rows * a.group);
-    // tensor-core kernel: a tile of 128 rows holds whole tokens, so that one copy brings it
-    a.unit_tokens = a.group <= 128 ? 2 * (128 / a.group) : 1;
-    a.unit_rows = a.unit_tokens * a.group;
-    a.unit_mul = reciprocal(a.unit_tokens, n_rows + a.unit_tokens);
-    a.page_log2 = page_log2_of(pool->page_size);
-    a.n_pages = (int)pool->n_pages;
-    a.window = window; a.n_sink = window > 0 ? n_sink : 0;
-    a.scale_log2 = scale_log2;
-    a.q_min = 2;
-    a.counters = static_cast<int *>(workspace);
-    a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + PA_COUNTER_BYTES);
-    s = launch_state(a);
-    if (s != CB_OK) return s;
-    if (device_sm_count() * 8 > PA_COUNTERS) return CB_ERR_UNSUPPORTED;
-    if (max_new == 0 || max_new > n_rows) max_new = (int32_t)n_rows;
+    bool nothing;
+    s = attention_args(c, layer, pool->n_layers, pool->n_heads, page_log2_of(pool->page_size), pool->n_pages, need, a, max_new, nothing);
+    if (s != CB_OK || nothing) return s;
     const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(pool->k) + layer * pool->stride_layer;
     const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(pool->v) + layer * pool->stride_layer;
     // Up to 16 flattened rows per request and KV head: the warp-level kernel, which has no rows to pad.  Measured on 16
@@ -234,6 +316,67 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
     const cudaError_t e = few ? launch_paged_attn_few(a, pool->head_dim, k, v, pool->page_size, pool->stride_page, pool->stride_slot, pool->stride_head, max_new, st)
                               : launch_paged_attn_tc(a, pool->head_dim, k, v, pool->page_size, pool->stride_page, pool->stride_slot, pool->stride_head, st);
     if (e != cudaSuccess) return cuda_failed(e);
+    return CB_OK;
+}
+
+cb_status cb_paged_store8(const cb_page_pool8 *pool, const void *src_k, const void *src_v, int32_t src_dtype, int64_t n_rows,
+                          int64_t stride_layer, int64_t stride_token, int64_t stride_head, const int64_t *slot_map, void *stream)
+{
+    const cb_status s = check_rows8(pool, src_k, src_v, src_dtype, n_rows, stride_layer, stride_token, stride_head, slot_map);
+    if (s != CB_OK || n_rows == 0) return s;
+    Store8Args a;
+    a.pool = pool8_of(pool, 0);
+    a.src_k = src_k; a.src_v = src_v;
+    a.s_sl = stride_layer; a.s_st = stride_token; a.s_sh = stride_head;
+    a.slot_map = reinterpret_cast<const long long *>(slot_map);
+    a.n_rows = n_rows;
+    if (const cudaError_t e = launch_paged8_store(a, src_dtype == CB_DTYPE_F32, static_cast<cudaStream_t>(stream)); e != cudaSuccess) return cuda_failed(e);
+    return CB_OK;
+}
+
+cb_status cb_paged_load8(const cb_page_pool8 *pool, void *dst_k, void *dst_v, int32_t dst_dtype, int64_t n_rows,
+                         int64_t stride_layer, int64_t stride_token, int64_t stride_head, const int64_t *slot_map, void *stream)
+{
+    const cb_status s = check_rows8(pool, dst_k, dst_v, dst_dtype, n_rows, stride_layer, stride_token, stride_head, slot_map);
+    if (s != CB_OK) return s;
+    if ((pool->n_layers > 1 && stride_layer == 0) || (n_rows > 1 && stride_token == 0) || (pool->n_heads > 1 && stride_head == 0)) return CB_ERR_UNSUPPORTED;
+    if (n_rows == 0) return CB_OK;
+    if (dst_k == dst_v) return CB_ERR_INVALID_ARG;
+    Load8Args a;
+    a.pool = pool8_of(pool, 0);
+    a.dst_k = dst_k; a.dst_v = dst_v;
+    a.d_sl = stride_layer; a.d_st = stride_token; a.d_sh = stride_head;
+    a.slot_map = reinterpret_cast<const long long *>(slot_map);
+    a.n_rows = n_rows;
+    if (const cudaError_t e = launch_paged8_load(a, dst_dtype == CB_DTYPE_F32, static_cast<cudaStream_t>(stream)); e != cudaSuccess) return cuda_failed(e);
+    return CB_OK;
+}
+
+cb_status cb_paged_attention8_workspace_bytes(int32_t head_dim, size_t *bytes)
+{
+    if (!bytes) return CB_ERR_INVALID_ARG;
+    if (head_dim != 64 && head_dim != 128) return CB_ERR_UNSUPPORTED;
+    *bytes = PA_COUNTER_BYTES + paged8_attn_few_workspace(head_dim);
+    return CB_OK;
+}
+
+cb_status cb_paged_attention8(const cb_page_pool8 *pool, int32_t layer, const void *q, int64_t q_stride_token, int64_t q_stride_head,
+                              void *out, int64_t o_stride_token, int64_t o_stride_head, int64_t n_rows, int32_t n_q_heads,
+                              const int32_t *block_table, int64_t table_stride, int32_t max_pages,
+                              const int32_t *cu_new, const int32_t *total_len, int32_t n_requests, int32_t max_new,
+                              float scale, int32_t window, int32_t n_sink, void *workspace, size_t workspace_bytes, void *stream)
+{
+    cb_status s = check_pool8(pool);
+    if (s != CB_OK) return s;
+    size_t need = 0;
+    cb_paged_attention8_workspace_bytes(pool->head_dim, &need);
+    const AttnCall c = {q, q_stride_token, q_stride_head, out, o_stride_token, o_stride_head, n_rows, n_q_heads, block_table, table_stride, max_pages,
+                        cu_new, total_len, n_requests, max_new, scale, window, n_sink, workspace, workspace_bytes};
+    PagedArgs a;
+    bool nothing;
+    s = attention_args(c, layer, pool->n_layers, pool->n_heads, page_log2_of(pool->page_size), pool->n_pages, need, a, max_new, nothing);
+    if (s != CB_OK || nothing) return s;
+    if (const cudaError_t e = launch_paged8_attn_few(a, pool8_of(pool, layer), max_new, static_cast<cudaStream_t>(stream)); e != cudaSuccess) return cuda_failed(e);
     return CB_OK;
 }
 

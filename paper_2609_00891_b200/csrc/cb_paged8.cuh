@@ -1,0 +1,112 @@
+// Paged cache held in 8 bits: declarations shared by its kernels and their host side (not part of the C ABI).
+//
+// A value is code * 2^e: codes are e4m3 (largest 448) or int8 (largest 127), e is one signed byte for each block of rows of
+// a page, KV head, layer, and K or V.  Scaling by a power of two is exact, so what the store writes does not depend on the
+// order of work.  The relative error of an e4m3 code is 2^-4 whatever the scale, and an int8 block gives up less than one bit
+// against a scale of its own maximum.
+#pragma once
+
+#include "cb_paged.cuh"
+
+namespace cb {
+
+constexpr int CACHE_E4M3 = CB_CACHE_E4M3, CACHE_INT8 = CB_CACHE_INT8;
+// Exponents of a block: with the largest ones every finite bf16 value below 2^127 fits (int8) or all do (e4m3).
+constexpr int EXP8_LEAST = -100;
+__host__ __device__ constexpr int exp8_most(int fmt) { return fmt == CACHE_E4M3 ? 119 : 121; }
+
+struct Pool8 {
+    uint8_t *k, *v;                          // codes
+    int8_t *ke, *ve;                         // exponents
+    long long sl, sp, ss, sh;                // strides of codes: layer, page, slot, head
+    long long el, ep, eb, eh;                // strides of exponents: layer, page, block, head
+    long long n_slots;                       // pages * page size
+    int n_pages, page_log2, block_log2;
+    int L, H, d, format;
+};
+
+struct Store8Args {
+    Pool8 pool;
+    const void *src_k, *src_v;
+    long long s_sl, s_st, s_sh;              // source strides (elements): layer, token, head
+    const long long *slot_map;
+    long long n_rows;
+    int tile;                                // rows of a thread block, a power of two up to 32
+    int wpr;                                 // warps that share a run of rows
+};
+cudaError_t launch_paged8_store(const Store8Args &a, bool f32, cudaStream_t st);
+
+struct Load8Args {
+    Pool8 pool;
+    void *dst_k, *dst_v;
+    long long d_sl, d_st, d_sh;
+    const long long *slot_map;
+    long long n_rows;
+};
+cudaError_t launch_paged8_load(const Load8Args &a, bool f32, cudaStream_t st);
+
+cudaError_t launch_paged8_attn_few(const PagedArgs &a, const Pool8 &pool, int max_new, cudaStream_t st);
+size_t paged8_attn_few_workspace(int d);
+
+#ifdef __CUDACC__
+// 2^e, for e in -126 .. 127.
+__device__ __forceinline__ float exp2_whole(int e) { return __int_as_float((e + 127) << 23); }
+__device__ __forceinline__ int exp8_clamp(int e, int fmt) { return min(max(e, EXP8_LEAST), exp8_most(fmt)); }
+
+// Four codes -> four fp16 values, exact, as pairs (codes 0, 1) and (codes 2, 3).
+template <int FMT>
+__device__ __forceinline__ void codes_to_f16(uint32_t y, uint32_t &lo, uint32_t &hi)
+{
+    if (FMT == CACHE_E4M3) {
+        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(y));
+    } else {
+        // 1024 + (code + 128) has the code in its low bits
+        const uint32_t t = y ^ 0x80808080u;
+        const uint32_t p = __byte_perm(t, 0x64646464u, 0x4140), q = __byte_perm(t, 0x64646464u, 0x4342);
+        asm("sub.f16x2 %0, %1, %2;" : "=r"(lo) : "r"(p), "r"(0x64806480u));
+        asm("sub.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(q), "r"(0x64806480u));
+    }
+}
+// Four codes -> four fp32 values times f.
+template <int FMT>
+__device__ __forceinline__ float4 codes_to_f32(uint32_t y, float f)
+{
+    if (FMT == CACHE_E4M3) {
+        uint32_t lo, hi;
+        codes_to_f16<FMT>(y, lo, hi);
+        float4 r;
+        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(r.x), "=f"(r.y) : "r"(lo));
+        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(r.z), "=f"(r.w) : "r"(hi));
+        return make_float4(r.x * f, r.y * f, r.z * f, r.w * f);
+    }
+    return make_float4((float)(int8_t)(y & 0xff) * f, (float)(int8_t)((y >> 8) & 0xff) * f, (float)(int8_t)((y >> 16) & 0xff) * f,
+                       (float)((int)y >> 24) * f);
+}
+// Four values, already divided by 2^e, to the nearest codes (ties to even); what lies past the largest code becomes it, NaN becomes
+// e4m3's NaN or int8's 0.
+template <int FMT>
+__device__ __forceinline__ uint32_t to_codes(float4 x)
+{
+    uint32_t r;
+    if (FMT == CACHE_E4M3) {
+        asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\n\tmov.b32 %0, {a, b};\n\t}"
+            : "=r"(r) : "f"(x.x), "f"(x.y), "f"(x.z), "f"(x.w));
+        return r;
+    }
+    const float v[4] = {x.x, x.y, x.z, x.w};
+    r = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r |= (uint32_t)(min(max(__float2int_rn(v[i]), -127), 127) & 0xff) << (8 * i);
+    return r;
+}
+// Least exponent under which `most` (the largest magnitude of a block, as the bits of an fp32 number) fits the codes: 448 is
+// 1.75 * 2^8 and 127 is (2 - 2^-6) * 2^6, so a mantissa above .75, or above 1 - 2^-6, takes one more.
+template <int FMT>
+__device__ __forceinline__ int exp8_need(uint32_t most)
+{
+    const int e = FMT == CACHE_E4M3 ? (int)((most + 0x1fffffu) >> 23) - 135 : (int)((most + 0x1ffffu) >> 23) - 133;
+    return exp8_clamp(e, FMT);
+}
+#endif
+
+}  // namespace cb
