@@ -548,8 +548,8 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
  *     value(layer, page, slot, head, c) = code * 2^exp
  *     code at (uint8*)k + layer*stride_layer + page*stride_page + slot*stride_slot + head*stride_head + c
  *     exp  at k_exp + layer*exp_stride_layer + page*exp_stride_page + (slot / block)*exp_stride_block + head*exp_stride_head
- * Channels are contiguous, k and v 16-byte aligned, code strides (bytes) multiples of 16, exponents anywhere; strides below
- * 2^40, 0 only on a dimension of size 1 (CB_ERR_UNSUPPORTED otherwise).  head_dim 64 or 128; page_size 8, 16, 32, 64, 128 or
+ * Channels are contiguous, k and v 16-byte aligned, code strides (bytes) multiples of 16, exponents anywhere; strides of
+ * pages, slots and blocks below 2^32, of layers and heads below 2^40, 0 only on a dimension of size 1 (CB_ERR_UNSUPPORTED otherwise).  head_dim 64 or 128; page_size 8, 16, 32, 64, 128 or
  * 256; block one of these too, at most page_size; n_pages < 2^31.  Exponents lie in -100 .. 119 (e4m3) or .. 121 (int8), and
  * one outside counts as the nearest of these.  A cache needs no initialisation.
  */
@@ -597,7 +597,7 @@ cb_status cb_paged_load8(const cb_page_pool8 *pool, void *dst_k, void *dst_v, in
 /*
  * cb_paged_attention over a pool of 8 bits: the same arguments, rows, masks, splits, and promises (and the same test hooks
  * and device status), with its own workspace size.  Codes become 16-bit numbers exactly.  Weights are rounded to fp16
- * (2^-11 of each that is above 2^-20 of the largest) or bf16 (2^-8), as max_new chooses between kernels.  Rows of a page
+ * (2^-11 of each that is above 2^-16 of the largest) or bf16 (2^-8), as max_new chooses between kernels.  Rows of a page
  * that no row of the request sees may hold anything, and so may the exponents of blocks without a seen row; values that
  * some row sees must be finite and below 2^90.
  */

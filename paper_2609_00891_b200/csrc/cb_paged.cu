@@ -76,7 +76,7 @@ struct AttnCall {
     void *workspace;
     size_t workspace_bytes;
 };
-cb_status attention_args(const AttnCall &c, int32_t layer, int32_t n_layers, int32_t n_heads, int page_log2, int64_t n_pages, size_t need,
+cb_status attention_args(const AttnCall &c, int32_t layer, int32_t n_layers, int32_t n_heads, int page_log2, int64_t n_pages, size_t need, int q_min,
                          PagedArgs &a, int32_t &max_new, bool &nothing)
 {
     nothing = false;
@@ -116,7 +116,7 @@ cb_status attention_args(const AttnCall &c, int32_t layer, int32_t n_layers, int
     a.n_pages = (int)n_pages;
     a.window = c.window; a.n_sink = c.window > 0 ? c.n_sink : 0;
     a.scale_log2 = scale_log2;
-    a.q_min = 2;
+    a.q_min = q_min;
     a.counters = static_cast<int *>(c.workspace);
     a.part = reinterpret_cast<float *>(static_cast<char *>(c.workspace) + PA_COUNTER_BYTES);
     const cb_status s = launch_state(a);
@@ -139,6 +139,9 @@ cb_status check_pool8(const cb_page_pool8 *p)
         if (x < 0) return CB_ERR_INVALID_ARG;
     if (p->head_dim != 64 && p->head_dim != 128) return CB_ERR_UNSUPPORTED;
     if (page_log2_of(p->page_size) < 0 || page_log2_of(p->block) < 0 || p->block > p->page_size || p->n_pages >= (1ll << 31)) return CB_ERR_UNSUPPORTED;
+    // the kernels multiply a page, a slot or a block by its stride as 32-bit numbers
+    if (p->stride_page >= (1ll << 32) || p->stride_slot >= (1ll << 32) || p->exp_stride_page >= (1ll << 32) || p->exp_stride_block >= (1ll << 32))
+        return CB_ERR_UNSUPPORTED;
     // a broadcast over more than one layer, page, row or head: pieces of the cache, or exponents, would share memory
     const bool more[] = {p->n_layers > 1, p->n_pages > 1, true, p->n_heads > 1}, more_exp[] = {p->n_layers > 1, p->n_pages > 1, p->page_size > p->block, p->n_heads > 1};
     for (int i = 0; i < 4; ++i)
@@ -303,7 +306,7 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
                         cu_new, total_len, n_requests, max_new, scale, window, n_sink, workspace, workspace_bytes};
     PagedArgs a;
     bool nothing;
-    s = attention_args(c, layer, pool->n_layers, pool->n_heads, page_log2_of(pool->page_size), pool->n_pages, need, a, max_new, nothing);
+    s = attention_args(c, layer, pool->n_layers, pool->n_heads, page_log2_of(pool->page_size), pool->n_pages, need, 2, a, max_new, nothing);
     if (s != CB_OK || nothing) return s;
     const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(pool->k) + layer * pool->stride_layer;
     const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(pool->v) + layer * pool->stride_layer;
@@ -374,7 +377,7 @@ cb_status cb_paged_attention8(const cb_page_pool8 *pool, int32_t layer, const vo
                         cu_new, total_len, n_requests, max_new, scale, window, n_sink, workspace, workspace_bytes};
     PagedArgs a;
     bool nothing;
-    s = attention_args(c, layer, pool->n_layers, pool->n_heads, page_log2_of(pool->page_size), pool->n_pages, need, a, max_new, nothing);
+    s = attention_args(c, layer, pool->n_layers, pool->n_heads, page_log2_of(pool->page_size), pool->n_pages, need, 1, a, max_new, nothing);
     if (s != CB_OK || nothing) return s;
     if (const cudaError_t e = launch_paged8_attn_few(a, pool8_of(pool, layer), max_new, static_cast<cudaStream_t>(stream)); e != cudaSuccess) return cuda_failed(e);
     return CB_OK;

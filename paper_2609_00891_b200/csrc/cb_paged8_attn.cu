@@ -1,20 +1,24 @@
 // Attention of a few new rows per request over a paged cache held in 8 bits (decode steps):
 //   out_t = sum_j softmax_j(scale q_t . k_j) v_j,   k_j = code 2^e, v_j = code 2^e, e one exponent a block of rows and head.
 //
-// Bound by the bytes of the codes, which are read once for all query heads of a KV head.  A warp takes 16 keys of every tile
-// of 64 and needs no other one until the end of a piece: it copies them into four stages of its own (cp.async; a page id
+// Bound by the bytes of the codes, which are read once for all query heads of a KV head.  A warp takes 32 keys of every tile
+// of 128 and needs no other one until the end of a piece: it copies them into two stages of its own (cp.async; a page id
 // outside the pool is filled with zeros), so that the loop has no barrier between warps, and no wait that another thread ends.
-//   scores    S^T = K Q^T: the 16 keys are the rows of the warp-level matrix instruction, 8 query rows its columns, so that
+//   scores    S^T = K Q^T: 16 keys are the rows of the warp-level matrix instruction, 8 query rows its columns, so that
 //             8 flattened rows cost one instruction where the other order would pad them to 16.
 //   channels  the sum over channels has any order: thread t of four takes D / 4 adjacent channels of a key, whose codes are one or
 //             two 16-byte loads, and q is laid out in registers the same way.
 //   outputs   O^T += V^T P^T: a pair of keys of one channel is a byte of two rows, put side by side by one permutation; the
 //             output's channels have any order too, and thread g of eight takes D / 8 adjacent ones.
-// Codes become fp16, which holds both formats exactly.  q is scaled by the power of two that brings its row's largest magnitude to
-// 2^14 .. 2^15: fp16 then holds every bf16 value down to 2^-29 of that one exactly, and the rest to 2^-40 of it.  The weights are
-// 2^6 exp2(s - m) with m at most 2^8 behind the row's maximum, so at most 2^14; they are rounded to fp16 (2^-11 of each
-// weight above 2^-20 of the largest) for the product with V, and summed unrounded.  A block's exponent multiplies its scores and its
-// part of the output, in fp32.
+//   q         becomes fp16, as the codes do (which it holds exactly): its row is scaled by the power of two that brings its largest
+//             magnitude to 2^14 .. 2^15, so that a bf16 number above 2^-29 of that one stays exact, and the rest is off by 2^-40 of it.
+//             (8-bit operands of the warp-level instruction, q in parts of 8 bits, took more instructions: 144 us for the decode
+//             batch below where conversions took 136.)
+//   weights   2^6 exp2(s - m), with m at most 13 behind the row's maximum; rounded to fp16 (2^-11 of each weight above 2^-16 of the
+//             largest) for the product with V, whose codes fp16 holds exactly, and summed unrounded.
+// A block's exponent multiplies its scores and its part of the output, in fp32.
+#include <cuda_fp16.h>
+
 #include "cb_paged8.cuh"
 #include "cb_math.cuh"
 #include "cb_ptx.cuh"
@@ -26,12 +30,12 @@ using namespace ptx;
 template <int D, int NT>
 struct Few8Cfg {
     static constexpr int ROWS = 8 * NT;
-    static constexpr int KT = 64;
-    static constexpr int NS = D == 128 ? 4 : 8;        // stages of a warp
-    static constexpr int HALF = 16 * D;                // bytes of K (or V) in a stage
+    static constexpr int KT = 128;                     // keys of a tile, 32 for each warp
+    static constexpr int HALF = 32 * D;                // bytes of a step's K (or V)
     static constexpr int STAGE = 2 * HALF;
-    static constexpr int RING = NS * STAGE;            // of a warp; holds its output at the end of a piece
+    static constexpr int RING = 2 * STAGE;             // of a warp; holds its output at the end of a piece
     static constexpr int REC = ROWS * (D + 2);         // floats of a partial record: output rows, maxima, sums
+    static constexpr int BLOCKS = D == 128 ? 4 - NT : 5 - NT;      // of an SM, by registers
     static_assert(RING >= ROWS * D * 4, "the warp's output must fit its stages");
     static constexpr size_t SMEM = 4 * RING;
 };
@@ -45,6 +49,12 @@ __device__ __forceinline__ void mma_f16_16816(float (&c)[4], const uint32_t (&a)
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// The same onto zeros.
+__device__ __forceinline__ void mma_f16_16816_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ void mma_f16_1688(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b)
 {
@@ -63,10 +73,10 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// 16 bytes to shared memory, or zeros.
-__device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src, bool there)
+// 16 bytes to shared memory, or (bytes = 0) zeros.
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src, uint32_t bytes)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16u : 0u) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -84,6 +94,27 @@ __device__ __forceinline__ uint2 lds8(uint32_t a)
     return v;
 }
 
+__device__ __forceinline__ float largest3(float x, float y, float z)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    return r;
+}
+
+// Four codes of K as fp16: e4m3 as they are, int8 as (code + 128) 2^-24, which are the subnormal numbers with that byte: the scores
+// then have 2^-24 of 128 times the row's sum of q on them, no larger than the scores themselves can be.
+template <int FMT>
+__device__ __forceinline__ void keys_to_f16(uint32_t y, uint32_t &lo, uint32_t &hi)
+{
+    if (FMT == CACHE_E4M3) {
+        codes_to_f16<FMT>(y, lo, hi);
+    } else {
+        const uint32_t t = y ^ 0x80808080u;
+        lo = __byte_perm(t, 0, 0x4140);
+        hi = __byte_perm(t, 0, 0x4342);
+    }
+}
+
 // Where the 16-byte piece c of row r of a stage stands, so that the reads below meet no bank twice.  128 channels: rows of eight
 // pieces, XORed by the row; 64: two rows a line of eight pieces, XORed by twice the line.
 template <int D>
@@ -94,10 +125,10 @@ __device__ __forceinline__ uint32_t piece_at(int r, int c)
 }
 
 template <int D, int NT, int FMT>
-__global__ void __launch_bounds__(128, 3) k_paged8_attn_few(const __grid_constant__ Few8Params P)
+__global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few(const __grid_constant__ Few8Params P)
 {
     using C = Few8Cfg<D, NT>;
-    extern __shared__ uint8_t smem_raw[];
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ PaShare share;
     __shared__ PaSum warp_sums[4];
     __shared__ float stat_m[4][C::ROWS], stat_l[4][C::ROWS];
@@ -106,8 +137,8 @@ __global__ void __launch_bounds__(128, 3) k_paged8_attn_few(const __grid_constan
     const Pool8 &p = P.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int g = lane >> 2, t4 = lane & 3;
-    constexpr int CQ = D / 4, CPT = D / 8, PIECES = D / 16;
-    constexpr int ROWS_I = 32 / PIECES;                // rows of one copy instruction of the warp
+    constexpr int CQ = D / 4, CPT = D / 8;
+    constexpr int NONE = -1000;                        // exponent of a group of keys that nobody sees, or without a page
 
     pa_schedule<C::ROWS, C::KT, 128>(a, reinterpret_cast<int *>(smem_raw), (int)(C::SMEM / 4), &share, warp_sums);
     PaWalk<C::ROWS, C::KT> w;
@@ -115,59 +146,57 @@ __global__ void __launch_bounds__(128, 3) k_paged8_attn_few(const __grid_constan
 
     uint8_t *ring = smem_raw + warp * C::RING;
     const uint32_t ring_u = smem_u32(ring);
-    const int crow = lane / PIECES, cpiece = lane % PIECES;
+    // eight lanes copy the eight keys of one group, whole rows (D = 128) or two at a time (64): a lane needs one page
+    constexpr int RI = 128 / D;                        // rows of a group that one copy of the warp brings
+    const int group8 = (lane >> 3) * 8, crow = D == 128 ? 0 : (lane >> 2) & 1, cpiece = D == 128 ? lane & 7 : lane & 3;
     const int slot_mask = (1 << a.page_log2) - 1;
     bool more = true;
     while (more) {
         const PaUnit &u = w.u;
         const int n = w.t1 - w.t;
         const int *row = a.table + (long long)u.b * a.table_stride;
-        const uint8_t *kb = p.k + (long long)w.h * p.sh, *vb = p.v + (long long)w.h * p.sh;
-        const int8_t *eb = ((lane & 2) ? p.ve : p.ke) + (long long)w.h * p.eh;    // lanes 0 .. 3: K of both halves, V of both
+        const uint8_t *kb = p.k + (long long)w.h * p.sh + crow * p.ss + cpiece * 16, *vb = p.v + (long long)w.h * p.sh + crow * p.ss + cpiece * 16;
+        const int8_t *eb = ((lane & 1) ? p.ve : p.ke) + (long long)w.h * p.eh;    // the first two lanes of eight: K's and V's exponent
 
-        // pages of the two groups of 8 keys of this warp's step s; -1 where no key is wanted
-        auto pages = [&](int s, int (&pg)[2]) {
-            const int key = pa_tile(u, w.t + s) * C::KT + warp * 16;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                pg[h] = -1;
-                if (s < n && pa_wanted(a, u, key + 8 * h, 8)) {
-                    const int col = (key + 8 * h) >> a.page_log2;
-                    if (col < a.table_cols) pg[h] = __ldg(row + col);
-                }
-            }
-        };
-        auto issue = [&](int s, int stage, const int (&pg)[2], int &ex) {
+        // first key of this lane's group in step s, and its page; outside the pool where no key is wanted
+        auto key_of = [&](int s) { return pa_tile(u, w.t + s) * C::KT + warp * 32 + group8; };
+        auto page_of = [&](int s) {
+            int page = -1;
             if (s < n) {
-                const int key = pa_tile(u, w.t + s) * C::KT + warp * 16;
-                const uint32_t to = ring_u + stage * C::STAGE;
+                const int key = key_of(s), col = key >> a.page_log2;
+                if (pa_wanted(a, u, key, 8) && col < a.table_cols) page = __ldg(row + col);
+            }
+            return page;
+        };
+        auto issue = [&](int s, int page, int &ex) {
+            const unsigned slot = (unsigned)key_of(s) & slot_mask;
+            const bool there = (unsigned)page < (unsigned)p.n_pages;
+            const uint32_t to = ring_u + (s & 1) * C::STAGE, bytes = there ? 16u : 0u;
+            const unsigned long long from = there ? (unsigned long long)(unsigned)page * (unsigned)p.sp + (unsigned long long)slot * (unsigned)p.ss : 0ull;
+            const unsigned long long step = there ? (unsigned long long)RI * p.ss : 0ull;
+            const uint8_t *ks = kb + from, *vs = vb + from;
 #pragma unroll
-                for (int i = 0; i < 16 / ROWS_I; ++i) {
-                    const int r = i * ROWS_I + crow, page = pg[(i * ROWS_I) >> 3];
-                    const bool there = (unsigned)page < (unsigned)p.n_pages;
-                    const long long from = there ? (long long)page * p.sp + (long long)((key + r) & slot_mask) * p.ss + cpiece * 16 : 0;
-                    cp_async_16(to + piece_at<D>(r, cpiece), kb + from, there);
-                    cp_async_16(to + C::HALF + piece_at<D>(r, cpiece), vb + from, there);
-                }
-                const int page = (lane & 1) ? pg[1] : pg[0];
-                ex = 0;
-                if (lane < 4 && (unsigned)page < (unsigned)p.n_pages)
-                    ex = __ldg(eb + (long long)page * p.ep + (long long)(((key + 8 * (lane & 1)) & slot_mask) >> p.block_log2) * p.eb);
+            for (int i = 0; i < 8 / RI; ++i) {
+                const uint32_t at = to + piece_at<D>(group8 + i * RI + crow, cpiece);
+                cp_async_16(at, ks, bytes);
+                cp_async_16(at + C::HALF, vs, bytes);
+                ks += step;
+                vs += step;
             }
             cp_async_commit();
+            ex = NONE;
+            if ((lane & 6) == 0 && there)
+                ex = __ldg(eb + ((unsigned long long)(unsigned)page * (unsigned)p.ep + (unsigned long long)(slot >> p.block_log2) * (unsigned)p.eb));
         };
 
-        int ex[C::NS], pg[2];
-#pragma unroll
-        for (int s = 0; s < C::NS - 1; ++s) {
-            pages(s, pg);
-            issue(s, s, pg, ex[s]);
-        }
-        pages(C::NS - 1, pg);
+        int ex_next, page = page_of(0);
+        issue(0, page, ex_next);
+        page = page_of(1);
 
         // q: row g (and g + 8), channels t4 * CQ onwards, as fp16
         uint32_t qf[NT][D / 16][2];
         float rr[NT][2];                                   // what the scores of rows 2 t4, 2 t4 + 1 are multiplied by
+        float excess[NT][2];                               // and what they are too large by (int8)
         int pos[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -178,31 +207,44 @@ __global__ void __launch_bounds__(128, 3) k_paged8_attn_few(const __grid_constan
             uint32_t top = 0;
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) {
-                const uint4 x = live ? __ldg(qp + i) : make_uint4(0, 0, 0, 0);
-                raw[4 * i] = x.x; raw[4 * i + 1] = x.y; raw[4 * i + 2] = x.z; raw[4 * i + 3] = x.w;
+                const uint4 z = live ? __ldg(qp + i) : make_uint4(0, 0, 0, 0);
+                raw[4 * i] = z.x; raw[4 * i + 1] = z.y; raw[4 * i + 2] = z.z; raw[4 * i + 3] = z.w;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) top = max(top, max(raw[4 * i + j] << 16 & 0x7fff0000u, raw[4 * i + j] & 0x7fff0000u));
             }
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const int up = min(14 - ((int)(top >> 23) - 127), 126);       // times 2^up (an all-zero row: 2^126)
-            const float f = exp2_whole(up), back = exp2_whole(-up) * a.scale_log2;
+            const float f = exp2_whole(up), back = exp2_whole(-up) * a.scale_log2 * (FMT == CACHE_INT8 ? 0x1p24f : 1.f);
+            float sum = 0.f;
 #pragma unroll
             for (int k = 0; k < D / 16; ++k)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const uint32_t x = raw[2 * k + e];
-                    qf[nt][k][e] = pack_f16x2(__uint_as_float(x << 16) * f, __uint_as_float(x & 0xffff0000u) * f);
+                    const uint32_t y = qf[nt][k][e] = pack_f16x2(__uint_as_float(raw[2 * k + e] << 16) * f, __uint_as_float(raw[2 * k + e] & 0xffff0000u) * f);
+                    if (FMT == CACHE_INT8) {
+                        const float2 z = __half22float2(*reinterpret_cast<const __half2 *>(&y));
+                        sum += z.x + z.y;
+                    }
                 }
+            if (FMT == CACHE_INT8) {
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                sum *= 0x1p-17f;
+            }
+            // a row of q that is not finite has no weights that are: NaN, as in 32 bits
+            const float whole = top < 0x7f800000u ? back : __int_as_float(0x7fc00000);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                rr[nt][e] = __shfl_sync(0xffffffffu, back, (2 * t4 + e) * 4);
+                rr[nt][e] = __shfl_sync(0xffffffffu, whole, (2 * t4 + e) * 4);
+                excess[nt][e] = FMT == CACHE_INT8 ? __shfl_sync(0xffffffffu, sum, (2 * t4 + e) * 4) : 0.f;
                 const int r2 = nt * 8 + 2 * t4 + e, tok2 = pa_token(a, u.row0 + r2);
                 pos[nt][e] = r2 < u.rows && (unsigned)(u.tok0 + tok2) < (unsigned)a.n_rows ? u.base + tok2 : -1;
             }
         }
         float o[NT][D / 16][4];
         float m[NT][2], l[NT][2];                          // 2^6 below the maximum that counts, sum of this thread's weights
+        int eo = NONE;                                     // o is in units of 2^eo
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -215,92 +257,127 @@ __global__ void __launch_bounds__(128, 3) k_paged8_attn_few(const __grid_constan
         int full0, full1;                                  // tiles [full0, full1) need no mask
         pa_full_tiles<C::KT>(a, u, full0, full1);
 
-        for (int s0 = 0; s0 < n; s0 += C::NS) {
-#pragma unroll
-            for (int js = 0; js < C::NS; ++js) {
-                const int s = s0 + js;
-                if (s >= n) break;
-                cp_async_wait<C::NS - 2>();
-                __syncwarp();                              // every lane's copies of this step have landed, and all are done with the one before
-                issue(s + C::NS - 1, (js + C::NS - 1) % C::NS, pg, ex[(js + C::NS - 1) % C::NS]);
-                pages(s + C::NS, pg);
-                const uint32_t ks = ring_u + js * C::STAGE, vs = ks + C::HALF;
-                const bool edge = w.t + s < full0 || w.t + s >= full1;
-                const int j0 = pa_tile(u, w.t + s) * C::KT + warp * 16;
-                const int ek0 = __shfl_sync(0xffffffffu, ex[js], 0), ek1 = __shfl_sync(0xffffffffu, ex[js], 1);
-                const int ev0 = __shfl_sync(0xffffffffu, ex[js], 2), ev1 = __shfl_sync(0xffffffffu, ex[js], 3);
+#pragma unroll 1
+        for (int s = 0; s < n; ++s) {
+            cp_async_wait<0>();
+            __syncwarp();                                  // every lane's copies of this step have landed, and all are done with the one before
+            const int ex_here = ex_next;
+            if (s + 1 < n) issue(s + 1, page, ex_next);
+            page = page_of(s + 2);
+            const uint32_t at = ring_u + (s & 1) * C::STAGE, at1 = at + C::HALF;
+            const bool edge = w.t + s < full0 || w.t + s >= full1;
+            const int j0 = pa_tile(u, w.t + s) * C::KT + warp * 32;
 
-                // ---- scores: keys g and g + 8, rows 2 t4 and 2 t4 + 1 ----
-                float x[NT][4];
+            // ---- scores: keys g, g + 8, g + 16, g + 24 (h = 0 .. 3), rows 2 t4 and 2 t4 + 1 ----
+            float x[2][NT][4];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[nt][e] = 0.f;
+            for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
                 for (int i = 0; i < CQ / 16; ++i) {
-                    const uint4 a0 = lds16(ks + piece_at<D>(g, t4 * (CQ / 16) + i)), a1 = lds16(ks + piece_at<D>(g + 8, t4 * (CQ / 16) + i));
+                    const uint4 a0 = lds16(at + piece_at<D>(kk * 16 + g, t4 * (CQ / 16) + i)), a1 = lds16(at + piece_at<D>(kk * 16 + g + 8, t4 * (CQ / 16) + i));
                     const uint32_t w0[4] = {a0.x, a0.y, a0.z, a0.w}, w1[4] = {a1.x, a1.y, a1.z, a1.w};
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         uint32_t f[4];
-                        codes_to_f16<FMT>(w0[j], f[0], f[2]);
-                        codes_to_f16<FMT>(w1[j], f[1], f[3]);
+                        keys_to_f16<FMT>(w0[j], f[0], f[2]);
+                        keys_to_f16<FMT>(w1[j], f[1], f[3]);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma_f16_16816(x[nt], f, qf[nt][4 * i + j][0], qf[nt][4 * i + j][1]);
+                        for (int nt = 0; nt < NT; ++nt) {
+                            if (i == 0 && j == 0) mma_f16_16816_first(x[kk][nt], f, qf[nt][0][0], qf[nt][0][1]);
+                            else mma_f16_16816(x[kk][nt], f, qf[nt][4 * i + j][0], qf[nt][4 * i + j][1]);
+                        }
                     }
                 }
-                const float fk0 = exp2_whole(exp8_clamp(ek0, FMT)), fk1 = exp2_whole(exp8_clamp(ek1, FMT));
-                bool grow = false;
+            // V's exponents.  Where those of the step lie within 2^-4 .. 2 of the output's unit, each key's goes onto its weight and
+            // the product adds to the output; else every group of 8 keys has a product of its own.  Lanes 8 h + 1 have V's of
+            // group h, lanes 8 h K's.
+            const int ex = exp8_clamp(ex_here, FMT);
+            const bool mine = (lane & 7) == 1 && ex_here != NONE;
+            if (__any_sync(0xffffffffu, mine && ex > eo + 1)) {        // a larger unit
+                const int ev_top = __reduce_max_sync(0xffffffffu, mine ? ex : NONE);
+                const float f = exp2_whole(max(eo - ev_top, -126));
+                eo = ev_top;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        x[nt][e] = x[nt][e] * rr[nt][e & 1] * (e < 2 ? fk0 : fk1);
-                        if (edge && !pa_sees(a, pos[nt][e & 1], j0 + g + (e < 2 ? 0 : 8))) x[nt][e] = -INFINITY;
-                        grow |= x[nt][e] > m[nt][e & 1] + 14.f;
-                    }
-                if (__any_sync(0xffffffffu, grow)) {
+                    for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                        for (int e = 0; e < 4; ++e) o[nt][i][e] *= f;
+            }
+            const int ev = mine ? ex - eo : 0;
+            const bool close = __all_sync(0xffffffffu, ev >= -4);
+            const float fv = exp2_whole(max(ev, -126));                // this lane's, and what its exponent adds to the weight's
+            const float scale8 = exp2_whole(ex), shift = close ? (float)ev : 0.f, unshift = close ? exp2_whole(-max(ev, -4)) : 1.f;
+            float fk[4], dv[4];
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float top = fmaxf(x[nt][e], x[nt][e + 2]);
-                            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-                            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-                            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                            if (top > m[nt][e] + 14.f) {
-                                const float f = pa_exp2(m[nt][e] - (top - 6.f));
-                                m[nt][e] = top - 6.f;
-                                l[nt][e] *= f;
+            for (int h = 0; h < 4; ++h) {
+                fk[h] = __shfl_sync(0xffffffffu, scale8, 8 * h);
+                dv[h] = __shfl_sync(0xffffffffu, shift, 8 * h + 1);
+            }
+            uint32_t pb[2][NT][2];                         // weights: row g, keys 2 t4, 2 t4 + 1 (and + 8) of each 16
+            float t[NT][2][4];                             // exponents of the weights
+            float top = -INFINITY;
+            auto exponents = [&](int nt, int e, float ref) {
 #pragma unroll
-                                for (int i = 0; i < D / 16; ++i) { o[nt][i][e] *= f; o[nt][i][e + 2] *= f; }
-                            }
-                        }
+                for (int h = 0; h < 4; ++h) {
+                    const float c = rr[nt][e] * fk[h], y = x[h >> 1][nt][(h & 1) * 2 + e];
+                    t[nt][e][h] = fmaf(FMT == CACHE_INT8 ? y - excess[nt][e] : y, c, dv[h] - ref);
+                    if (edge && !pa_sees(a, pos[nt][e], j0 + h * 8 + g)) t[nt][e][h] = -INFINITY;
                 }
-                uint32_t pb[NT][2];                        // weights: row g, keys 2 t4, 2 t4 + 1 (and + 8)
+            };
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    exponents(nt, e, m[nt][e]);
+                    top = largest3(top, largest3(t[nt][e][0], t[nt][e][1], t[nt][e][2]), t[nt][e][3]);
+                }
+            if (__any_sync(0xffffffffu, top > 15.f)) {     // the first keys of a row (m is -inf), or a maximum that grew by 9 or more
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float most = -INFINITY;
+#pragma unroll
+                        for (int h = 0; h < 4; ++h)
+                            if (t[nt][e][h] != -INFINITY) most = fmaxf(most, (x[h >> 1][nt][(h & 1) * 2 + e] - excess[nt][e]) * (rr[nt][e] * fk[h]));
+                        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 4));
+                        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 8));
+                        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 16));
+                        if (most - 6.f > m[nt][e]) {
+                            const float f = pa_exp2(m[nt][e] - (most - 6.f));
+                            m[nt][e] = most - 6.f;
+                            l[nt][e] *= f;
+#pragma unroll
+                            for (int i = 0; i < D / 16; ++i) { o[nt][i][e] *= f; o[nt][i][e + 2] *= f; }
+                        }
+                        exponents(nt, e, m[nt][e] == -INFINITY ? 0.f : m[nt][e]);       // a row that has seen nothing yet: all weights 0
+                    }
+            }
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const float f = __shfl_sync(0xffffffffu, unshift, 8 * h + 1);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    float y[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float ref = m[nt][e & 1] == -INFINITY ? 0.f : m[nt][e & 1];     // a row that has seen nothing yet: all weights 0
-                        y[e] = pa_exp2(x[nt][e] - ref);
-                        l[nt][e & 1] += y[e];
-                    }
-                    pb[nt][0] = transpose_8x8(pack_f16x2(y[0], y[1]));
-                    pb[nt][1] = transpose_8x8(pack_f16x2(y[2], y[3]));
+                    const float y0 = pa_exp2(t[nt][0][h]), y1 = pa_exp2(t[nt][1][h]);
+                    l[nt][0] = fmaf(y0, f, l[nt][0]);
+                    l[nt][1] = fmaf(y1, f, l[nt][1]);
+                    pb[h >> 1][nt][h & 1] = transpose_8x8(pack_f16x2(y0, y1));
                 }
+            }
 
-                // ---- outputs: channels g * CPT + 2 i, + 1 ----
+            // ---- outputs: channels g * CPT + 2 i, + 1 ----
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
                 uint32_t v[4][CPT / 4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int r = 2 * t4 + (k & 1) + (k >> 1) * 8;
+                    const int r = kk * 16 + 2 * t4 + (k & 1) + (k >> 1) * 8;
                     if (D == 128) {
-                        const uint4 z = lds16(vs + piece_at<D>(r, g));
+                        const uint4 z = lds16(at1 + piece_at<D>(r, g));
                         v[k][0] = z.x; v[k][1] = z.y; v[k][CPT / 4 - 2] = z.z; v[k][CPT / 4 - 1] = z.w;
                     } else {
-                        const uint2 z = lds8(vs + piece_at<D>(r, g >> 1) + (g & 1) * 8);
+                        const uint2 z = lds8(at1 + piece_at<D>(r, g >> 1) + (g & 1) * 8);
                         v[k][0] = z.x; v[k][1] = z.y;
                     }
                     // rows that no query sees may hold anything: their values become zeros, or 0 * NaN would reach the output
@@ -310,42 +387,36 @@ __global__ void __launch_bounds__(128, 3) k_paged8_attn_few(const __grid_constan
                         for (int c = 0; c < CPT / 4; ++c) v[k][c] = 0;
                     }
                 }
-                const float fv0 = exp2_whole(exp8_clamp(ev0, FMT)), fv1 = exp2_whole(exp8_clamp(ev1, FMT));
-                const bool same = ev0 == ev1;
+                const float f0 = __shfl_sync(0xffffffffu, fv, 16 * kk + 1), f1 = __shfl_sync(0xffffffffu, fv, 16 * kk + 9);
 #pragma unroll
-                for (int i = 0; i < D / 16; i += 2) {
-                    uint32_t f[2][4];
+                for (int i = 0; i < D / 16; ++i) {
+                    // channels 4 c + {0, 1} (i even) or {2, 3}: (row 2 t4, row 2 t4 + 1) of each, and the rows 8 on
+                    uint32_t f[4];
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        // channels 4 c + {0, 1} and {2, 3}: (row 2 t4, row 2 t4 + 1) of each
-                        codes_to_f16<FMT>(__byte_perm(v[2 * k][i / 2], v[2 * k + 1][i / 2], 0x5140), f[0][2 * k], f[0][2 * k + 1]);
-                        codes_to_f16<FMT>(__byte_perm(v[2 * k][i / 2], v[2 * k + 1][i / 2], 0x7362), f[1][2 * k], f[1][2 * k + 1]);
-                    }
+                    for (int y = 0; y < 2; ++y)
+                        codes_to_f16<FMT>(__byte_perm(v[2 * y][i >> 1], v[2 * y + 1][i >> 1], (i & 1) ? 0x7362 : 0x5140), f[2 * y], f[2 * y + 1]);
+                    if (close) {
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
+                        for (int nt = 0; nt < NT; ++nt) mma_f16_16816(o[nt][i], f, pb[kk][nt][0], pb[kk][nt][1]);
+                    } else {
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            float d[4] = {0.f, 0.f, 0.f, 0.f};
-                            if (same) {
-                                mma_f16_16816(d, f[k], pb[nt][0], pb[nt][1]);
-                            } else {
-                                float d1[4] = {0.f, 0.f, 0.f, 0.f};
-                                mma_f16_1688(d, f[k][0], f[k][1], pb[nt][0]);
-                                mma_f16_1688(d1, f[k][2], f[k][3], pb[nt][1]);
+                        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) o[nt][i + k][e] = fmaf(d1[e], fv1, o[nt][i + k][e]);
+                            for (int y = 0; y < 2; ++y) {
+                                float d[4] = {0.f, 0.f, 0.f, 0.f};
+                                mma_f16_1688(d, f[2 * y], f[2 * y + 1], pb[kk][nt][y]);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) o[nt][i][e] = fmaf(d[e], y ? f1 : f0, o[nt][i][e]);
                             }
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[nt][i + k][e] = fmaf(d[e], fv0, o[nt][i + k][e]);
-                        }
+                    }
                 }
             }
         }
-        cp_async_wait<0>();
         __syncwarp();
 
         // ---- the piece's result: the warps' parts meet in shared memory ----
         float *mine = reinterpret_cast<float *>(ring);     // [ROWS][D], 16-byte pieces XORed by the row
+        const float unit = exp2_whole(max(eo, EXP8_LEAST));
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -360,7 +431,7 @@ __global__ void __launch_bounds__(128, 3) k_paged8_attn_few(const __grid_constan
                 for (int i = 0; i < D / 16; i += 2) {
                     const int c = (g * CPT + 2 * i) / 4;
                     *reinterpret_cast<float4 *>(mine + r * D + ((c ^ (r & 7)) << 2)) =
-                        make_float4(o[nt][i][e], o[nt][i][e + 2], o[nt][i + 1][e], o[nt][i + 1][e + 2]);
+                        make_float4(o[nt][i][e] * unit, o[nt][i][e + 2] * unit, o[nt][i + 1][e] * unit, o[nt][i + 1][e + 2] * unit);
                 }
             }
         __syncthreads();
@@ -451,7 +522,7 @@ __global__ void __launch_bounds__(128, 3) k_paged8_attn_few(const __grid_constan
     }
 }
 
-size_t paged8_attn_few_workspace(int d) { return (size_t)2 * 3 * device_sm_count() * 16 * (d + 2) * sizeof(float); }
+size_t paged8_attn_few_workspace(int d) { return (size_t)2 * 4 * device_sm_count() * 16 * (d + 2) * sizeof(float); }
 
 template <int D, int NT, int FMT>
 static cudaError_t launch_few8(const Few8Params &P, cudaStream_t st)
@@ -460,7 +531,7 @@ static cudaError_t launch_few8(const Few8Params &P, cudaStream_t st)
     static bool attr[MAX_DEVICES] = {};
     cudaError_t e = opt_in_smem(k_paged8_attn_few<D, NT, FMT>, C::SMEM, attr);
     if (e != cudaSuccess) return e;
-    k_paged8_attn_few<D, NT, FMT><<<3 * device_sm_count(), 128, C::SMEM, st>>>(P);
+    k_paged8_attn_few<D, NT, FMT><<<C::BLOCKS * device_sm_count(), 128, C::SMEM, st>>>(P);
     e = cudaGetLastError();
     if (e == cudaSuccess) count_launch();
     return e;

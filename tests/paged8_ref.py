@@ -62,8 +62,9 @@ def attention(q, k, v, table, cu, total, scale, window=0, n_sink=0, weight=2.0 *
 
     Tolerance, element by element: the output's rounding to bf16 (2^-8 of it); every weight's rounding (`weight`, of
     sum w |v| / sum w); the score's fp32 product over d channels, in the worst order, 2 d 2^-24 of scale sum |q||k| on the
-    exponent, 2^-20 for the exponential, its argument (scores below 16 here) and the sums; and fp16's 2^-31 of the largest weight
-    for every key whose weight is below 2^-20 of that one."""
+    exponent, q held to 2^-20 of its row's largest magnitude (2^-20 of scale max|q| sum |k|), 2^-20 for the exponential, its argument
+    (scores below 16 here) and the sums; and fp16's 2^-27 of the largest weight for every key (half a subnormal step, 2^-25, under
+    2^6 for the largest weight and 2^-4 for a value's exponent)."""
     T, Hq, d = q.shape
     page, H = k.shape[1], k.shape[2]
     g = Hq // H
@@ -94,7 +95,8 @@ def attention(q, k, v, table, cu, total, scale, window=0, n_sink=0, weight=2.0 *
             safe = torch.where(l > 0, l, 1)
             out[t0:t1, h] = torch.where(l > 0, (w @ vh) / safe, 0)
             size = torch.where(l > 0, (w @ vh.abs()) / safe, 0)
-            small = (see.double() @ vh.abs()) / safe * 2.0 ** -31
+            small = (see.double() @ vh.abs()) / safe * 2.0 ** -27
             worst = float((qh.abs() @ kh.abs().T).max()) * scale if n else 0.0
-            tol[t0:t1, h] = out[t0:t1, h].abs() * 2.0 ** -8 + size * (weight + 2 * (2 * d * 2.0 ** -24 * worst + 2.0 ** -20)) + small + 1e-30
+            parts = qh.abs().amax(-1, keepdim=True) * (float(kh.abs().sum(-1).max()) * scale * 2.0 ** -20) if n else 0.0
+            tol[t0:t1, h] = out[t0:t1, h].abs() * 2.0 ** -8 + size * (weight + 2 * (2 * d * 2.0 ** -24 * worst + parts + 2.0 ** -20)) + small + 1e-30
     return out, tol
