@@ -359,7 +359,7 @@ cb_status cb_paged_attention8_workspace_bytes(int32_t head_dim, size_t *bytes)
 {
     if (!bytes) return CB_ERR_INVALID_ARG;
     if (head_dim != 64 && head_dim != 128) return CB_ERR_UNSUPPORTED;
-    *bytes = PA_COUNTER_BYTES + paged8_attn_few_workspace(head_dim);
+    *bytes = PA_COUNTER_BYTES + std::max(paged8_attn_few_workspace(head_dim), paged_attn_tc_workspace(head_dim));
     return CB_OK;
 }
 
@@ -379,7 +379,11 @@ cb_status cb_paged_attention8(const cb_page_pool8 *pool, int32_t layer, const vo
     bool nothing;
     s = attention_args(c, layer, pool->n_layers, pool->n_heads, page_log2_of(pool->page_size), pool->n_pages, need, 1, a, max_new, nothing);
     if (s != CB_OK || nothing) return s;
-    if (const cudaError_t e = launch_paged8_attn_few(a, pool8_of(pool, layer), max_new, static_cast<cudaStream_t>(stream)); e != cudaSuccess) return cuda_failed(e);
+    const bool few = (long long)max_new * a.group <= 16 || a.group > 128;
+    if (!few) a.q_min = 2;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = few ? launch_paged8_attn_few(a, pool8_of(pool, layer), max_new, st) : launch_paged8_attn_tc(a, pool8_of(pool, layer), st);
+    if (e != cudaSuccess) return cuda_failed(e);
     return CB_OK;
 }
 

@@ -47,6 +47,7 @@ cudaError_t launch_paged8_load(const Load8Args &a, bool f32, cudaStream_t st);
 
 cudaError_t launch_paged8_attn_few(const PagedArgs &a, const Pool8 &pool, int max_new, cudaStream_t st);
 size_t paged8_attn_few_workspace(int d);
+cudaError_t launch_paged8_attn_tc(const PagedArgs &a, const Pool8 &pool, cudaStream_t st);      // workspace of paged_attn_tc_workspace
 
 #ifdef __CUDACC__
 // 2^e, for e in -126 .. 127.

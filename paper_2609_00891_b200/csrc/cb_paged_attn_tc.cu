@@ -24,7 +24,15 @@
 // 0.83 PFLOP/s: the line gives every block 450 tiles, but those at its begin are of one to five tiles a piece, and the first
 // block walks 154 pieces where the others walk 14; a piece costs 7,600 cycles beside its tiles, the same number for every
 // prompt measured.  16 requests of 2 to 16 rows over 8,192 keys 109 - 144 us (4.9 - 3.7 TB/s), by rows and page size.
+//
+// The same kernel reads a cache held in 8 bits (FMT is its format; BF16_PAGES is this file's head): the copying and clearing warps give
+// way to four that convert.  Each copies the codes of 32 keys of a tile, one tile ahead of the conversion (cp.async into 32 KB beside
+// the tiles; every thread reads back its own 16 bytes, so nothing waits), and writes them as bf16 numbers code * 2^e, which are exact,
+// where the products take them from; everything after that is as above.
+#include <type_traits>
+
 #include "cb_paged.cuh"
+#include "cb_paged8.cuh"
 #include "cb_ptx.cuh"
 #include "cb_math.cuh"
 
@@ -32,20 +40,26 @@ namespace cb {
 
 using namespace ptx;
 
-template <int D>
+constexpr int BF16_PAGES = -1;
+
+template <int D, int FMT>
 struct TcAttnCfg {
+    static constexpr bool EIGHT = FMT != BF16_PAGES;
     static constexpr int ROWS = 0, KT = 128;               // rows of a unit: 2 x as many whole tokens as 128 rows hold
     static constexpr int NB = D / 64;
     static constexpr int BLK = 128 * 128;                  // bytes of 128 rows of 64 channels
     static constexpr int TILE = NB * BLK;                  // a Q, K or V tile
-    static constexpr int NS = D == 128 ? 5 : 10;           // K and V tiles in flight
-    static constexpr int THREADS = 384;
+    static constexpr int NS = (EIGHT ? 3 : 5) * (128 / D);  // K and V tiles in flight
+    static constexpr int CODES = KT * D;                   // bytes of a tile's codes; two tiles of K and V
+    static constexpr int THREADS = EIGHT ? 512 : 384;
+    // registers of the softmax warps, of those beside them, and of the converting ones: 3 x 168 or 4 x 128 launched with
+    static constexpr int REGS = EIGHT ? 184 : 208, REGS_BESIDE = EIGHT ? 64 : 88, REGS_CONVERT = 80;
     static constexpr int TMEM_COLS = 512;                  // S0, S1: 128 columns each, then O0, O1: D columns each
     // Quarters of a tile's weights that are handed on first, so that their product runs while the rest is computed.  Prefill of
     // 8,192 rows, three quarters against two: 64 channels 1,048 / 1,087 us, 128 channels 1,295 / 1,299 us alone and 1,700 /
     // 1,610 us for the chunk of 4,096 rows over 16,384 keys under the power limit.
     static constexpr int FIRST = D == 64 ? 3 : 2;
-    static constexpr size_t SMEM = 1024 + 2 * (size_t)TILE + (size_t)NS * TILE + 1280;
+    static constexpr size_t SMEM = 1024 + 2 * (size_t)TILE + (size_t)NS * TILE + (EIGHT ? 4 * CODES : 0) + 1280;
     static constexpr int REC = 256 * (D + 2);              // floats of a partial record: [D / 4][256 rows][4], maxima, sums
 };
 
@@ -54,6 +68,16 @@ struct TcAttnParams {
     PagedArgs a;
     int q_bytes;                                            // of one 64-channel block of a Q tile
 };
+struct TcAttn8Params {
+    CUtensorMap q;
+    Pool8 p;
+    PagedArgs a;
+    int q_bytes;
+};
+template <int FMT>
+struct TcParamsOf { using type = TcAttn8Params; };
+template <>
+struct TcParamsOf<BF16_PAGES> { using type = TcAttnParams; };
 
 // What the softmax warps need of a piece; t0 < 0: no more pieces.
 struct alignas(16) TcPiece {
@@ -80,15 +104,177 @@ __device__ __forceinline__ float max3(float x, float y, float z)
     return r;
 }
 
-template <int D>
-__global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant__ TcAttnParams P)
+// ================================ converting warps (a cache of 8 bits) ================================
+__device__ __forceinline__ uint32_t bf16x2_mul(uint32_t x, uint32_t y)
 {
-    using C = TcAttnCfg<D>;
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+}
+// Two of a word's codes (the lower, the upper ones) as bf16 numbers code * 2^e, exactly.
+struct ToBf16 {
+    uint32_t f;          // e4m3: 2^(120 + e) twice as bf16
+    uint32_t g;          // and the part of it that is past bf16's largest power, or 1
+    float s, m;          // int8: 2^e and -(2^23 + 128) 2^e
+    template <int FMT>
+    __device__ __forceinline__ bool set(int e)             // whether some thread of the warp needs g
+    {
+        if (FMT == CACHE_E4M3) {
+            f = (uint32_t)(min(e, 7) + 247) * 0x00800080u;             // exponent 120 + e, biased by 127, at bits 7 and 23
+            g = (uint32_t)(max(e - 7, 0) + 127) * 0x00800080u;
+        } else {
+            s = exp2_whole(e);
+            m = -8388736.f * s;
+        }
+        return FMT == CACHE_E4M3 && __any_sync(0xffffffffu, e > 7);
+    }
+    template <int FMT, bool LARGE>
+    __device__ __forceinline__ uint32_t pair(uint32_t w, int upper) const
+    {
+        if (FMT == CACHE_E4M3) {
+            // sign, exponent and mantissa of a code in the places of bf16's: the number times 2^-120, subnormal or not
+            const uint32_t x = __byte_perm(w, 0, upper ? 0x3424 : 0x1404);
+            uint32_t r = bf16x2_mul((x & 0x80008000u) | ((x >> 4) & 0x07f007f0u), f);
+            if (LARGE) r = bf16x2_mul(r, g);
+            return r;
+        }
+        // 2^23 + (code + 128) has the code in its low bits
+        const uint32_t t = w ^ 0x80808080u;
+        const float a = __uint_as_float(__byte_perm(t, 0x4b000000u, upper ? 0x7442 : 0x7440)), b = __uint_as_float(__byte_perm(t, 0x4b000000u, upper ? 0x7443 : 0x7441));
+        return pack_bf16x2(fmaf(a, s, m), fmaf(b, s, m));
+    }
+};
+
+template <int D, int FMT>
+__device__ __forceinline__ void tc_convert(const PagedArgs &a, const Pool8 &p, const PaShare &share, uint8_t *kv, uint8_t *codes, uint64_t *full,
+                                           uint64_t *empty, volatile int *abort_flag, volatile int *moves)
+{
+    using C = TcAttnCfg<D, FMT>;
+    const int lane = threadIdx.x & 31, cw = (threadIdx.x >> 5) - 12;
+    PaWalk<C::ROWS, C::KT> w;
+    if (!w.open(a, share)) return;
+    // eight lanes take the eight keys of one group, whole rows (D = 128) or two at a time (64)
+    constexpr int RI = 128 / D;
+    const int row0 = cw * 32 + (lane >> 3) * 8 + (D == 128 ? 0 : (lane >> 2) & 1), piece = D == 128 ? lane & 7 : lane & 3;
+    const int group = cw * 32 + (lane >> 3) * 8;
+    const int slot_mask = (1 << a.page_log2) - 1;
+    const uint32_t mine = smem_u32(codes) + row0 * D + piece * 16;
+    // where the two halves of a piece go: 64-channel block, then 16-byte columns 2 c and 2 c + 1 of the row, XORed by it.  Pieces of the
+    // second block go second half first, so that the eight lanes of a row meet no bank twice.
+    const bool swap = D == 128 && (piece & 4);
+    const uint32_t dst = smem_u32(kv) + (piece >> 2) * C::BLK + row0 * 128;
+    const int col = (piece & 3) * 2;
+
+    struct Tile { int j0, hi, lo, ex; bool clear; };
+    auto page_of = [&](int j0) {
+        const int key = j0 + group, c = key >> a.page_log2;
+        return pa_wanted(a, w.u, key, 8) && c < a.table_cols ? __ldg(a.table + (long long)w.u.b * a.table_stride + c) : -1;
+    };
+    auto issue = [&](int j0, int page, int slot_of_two) {
+        const unsigned slot = (unsigned)(j0 + group) & slot_mask;
+        const bool there = (unsigned)page < (unsigned)p.n_pages;
+        const uint32_t bytes = there ? 16u : 0u, to = mine + slot_of_two * 2 * C::CODES;
+        unsigned long long from = 0, step = 0;
+        if (there) {
+            from = (unsigned long long)(unsigned)page * (unsigned)p.sp + (unsigned long long)(slot + (row0 - group)) * (unsigned)p.ss;
+            step = (unsigned long long)RI * p.ss;
+        }
+        from += (unsigned long long)w.h * p.sh + piece * 16;
+        const uint8_t *ks = p.k + from, *vs = p.v + from;
+#pragma unroll
+        for (int i = 0; i < 8 / RI; ++i) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + i * RI * D), "l"(ks), "r"(bytes) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + C::CODES + i * RI * D), "l"(vs), "r"(bytes) : "memory");
+            ks += step;
+            vs += step;
+        }
+        Tile t;
+        t.j0 = j0;
+        t.hi = w.u.hi_key;
+        t.lo = w.u.lo_key;
+        t.clear = pa_clears<C::KT>(a, w.u, j0);
+        t.ex = 0;
+        if ((lane & 6) == 0 && there)                      // the first two lanes of eight: K's and V's exponent
+            t.ex = __ldg(((lane & 1) ? p.ve : p.ke) + (long long)w.h * p.eh + ((unsigned long long)(unsigned)page * (unsigned)p.ep +
+                                                                             (unsigned long long)(slot >> p.block_log2) * (unsigned)p.eb));
+        return t;
+    };
+    Ring<C::NS> st;
+    int done = 0, t = w.t;
+    Tile here = issue(pa_tile(w.u, t) * C::KT, page_of(pa_tile(w.u, t) * C::KT), 0);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    bool more = true;
+    for (int n = 0; more; ++n) {
+        // the next tile, of this piece or another
+        if (++t >= w.t1) {
+            more = w.next(a);
+            t = w.t;
+        }
+        const int j0 = more ? pa_tile(w.u, t) * C::KT : 0;
+        const int page = more ? page_of(j0) : -1;
+        Tile next = {};
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+#pragma unroll
+        for (int comp = 0; comp < 2; ++comp) {
+            if (comp == 0) {
+                if (more) next = issue(j0, page, (n + 1) & 1);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            }
+            if (!mbar_wait_to_issue_warp(&empty[st.idx], st.phase ^ 1, abort_flag)) {
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                return;
+            }
+            const int e = exp8_clamp(__shfl_sync(0xffffffffu, here.ex, (lane & 24) + comp), FMT);
+            ToBf16 to;
+            const bool large = to.template set<FMT>(e);
+            const uint32_t from = mine + ((n & 1) * 2 + comp) * C::CODES, tile = dst + st.idx * C::TILE;
+            const bool clear = comp && here.clear;
+            auto convert = [&](auto wide) {
+                constexpr bool LARGE = decltype(wide)::value;
+#pragma unroll
+                for (int i0 = 0; i0 < 8 / RI; i0 += 4) {
+                    uint4 x[4];                            // four loads in flight
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[k].x), "=r"(x[k].y), "=r"(x[k].z), "=r"(x[k].w) : "r"(from + (i0 + k) * RI * D) : "memory");
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int i = i0 + k, r = row0 + i * RI, j = here.j0 + r;
+                        // rows that no query sees may hold anything: 0 * NaN would reach the output
+                        if (clear && !(j < here.hi && (j >= here.lo || j < a.n_sink))) x[k] = make_uint4(0, 0, 0, 0);
+                        const uint32_t w0 = swap ? x[k].z : x[k].x, w1 = swap ? x[k].w : x[k].y, w2 = swap ? x[k].x : x[k].z, w3 = swap ? x[k].y : x[k].w;
+                        const uint4 y = make_uint4(to.template pair<FMT, LARGE>(w0, 0), to.template pair<FMT, LARGE>(w0, 1), to.template pair<FMT, LARGE>(w1, 0), to.template pair<FMT, LARGE>(w1, 1));
+                        const uint4 z = make_uint4(to.template pair<FMT, LARGE>(w2, 0), to.template pair<FMT, LARGE>(w2, 1), to.template pair<FMT, LARGE>(w3, 0), to.template pair<FMT, LARGE>(w3, 1));
+                        const uint32_t at = tile + i * RI * 128;
+                        const int first = (col + (swap ? 1 : 0)) ^ (r & 7);
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + (first << 4)), "r"(y.x), "r"(y.y), "r"(y.z), "r"(y.w) : "memory");
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + ((first ^ 1) << 4)), "r"(z.x), "r"(z.y), "r"(z.z), "r"(z.w) : "memory");
+                    }
+                }
+            };
+            if (large) convert(std::true_type()); else convert(std::false_type());
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&full[st.idx]);
+                if (cw == 0) *moves = ++done;
+            }
+            st.next();
+        }
+        here = next;
+    }
+}
+
+template <int D, int FMT>
+__global__ void __launch_bounds__(TcAttnCfg<D, FMT>::THREADS, 1) k_paged_attn_tc(const __grid_constant__ typename TcParamsOf<FMT>::type P)
+{
+    using C = TcAttnCfg<D, FMT>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t *qs = smem;                                     // [2][TILE]
     uint8_t *kv = smem + 2 * (size_t)C::TILE;               // [NS][TILE]
-    uint64_t *full = reinterpret_cast<uint64_t *>(kv + (size_t)C::NS * C::TILE);
+    uint8_t *codes = kv + (size_t)C::NS * C::TILE;          // [2][K, V][CODES]
+    uint64_t *full = reinterpret_cast<uint64_t *>(codes + (C::EIGHT ? 4 * C::CODES : 0));
     uint64_t *empty = full + C::NS;
     uint64_t *q_full = empty + C::NS;      // [2] Q tile written
     uint64_t *q_empty = q_full + 2;        // [2] its last scores of a piece complete
@@ -100,7 +286,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
     uint64_t *landed = o_full + 2;         // [NS] a V tile that has rows to clear: copied
     uint64_t *drain = landed + C::NS;
     PaSum *warp_sums = reinterpret_cast<PaSum *>(((uintptr_t)(drain + 1) + 15) & ~(uintptr_t)15);
-    PaShare *share = reinterpret_cast<PaShare *>(warp_sums + 12);
+    PaShare *share = reinterpret_cast<PaShare *>(warp_sums + C::THREADS / 32);
     using Walk = PaWalk<C::ROWS, C::KT>;
     TcPiece *info = reinterpret_cast<TcPiece *>(((uintptr_t)(share + 1) + 15) & ~(uintptr_t)15);   // [2]
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(info + 2);
@@ -114,7 +300,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
     const PagedArgs &a = P.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 256) {
-        for (int i = 0; i < C::NS; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&landed[i], 1); }
+        for (int i = 0; i < C::NS; ++i) { mbar_init(&full[i], C::EIGHT ? 4 : 1); mbar_init(&empty[i], 1); mbar_init(&landed[i], 1); }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&q_full[i], 1);
             mbar_init(&q_empty[i], 1);
@@ -131,8 +317,10 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
         *flight = Flight{};
         mbar_fence_init();
         tma_prefetch_desc(&P.q);
-        tma_prefetch_desc(&P.k);
-        tma_prefetch_desc(&P.v);
+        if constexpr (!C::EIGHT) {
+            tma_prefetch_desc(&P.k);
+            tma_prefetch_desc(&P.v);
+        }
     }
     if (warp == 9) tmem_alloc(tmem_slot, C::TMEM_COLS);
     tc_fence_before();
@@ -145,13 +333,18 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
     const int box_log2 = a.page_log2 < 7 ? a.page_log2 : 7;
     bool dead = false;       // a wait ran out: no more waits, the rest runs through on whatever is there
 
-    // the softmax warps hold a row of 128 scores each: 208 + 208 + 88 registers a thread of the 3 x 168 launched with
-    if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    // the softmax warps hold a row of 128 scores each
+    if (C::EIGHT && warp >= 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_CONVERT));
+        if constexpr (C::EIGHT)
+            if (any && !a.starve) tc_convert<D, FMT>(a, P.p, *share, kv, codes, full, empty, abort_flag, moves);
+    } else if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_BESIDE));
     Walk w;
     if (any) w.open(a, *share);
     if (warp == 8) {
         // ================================ producer ================================
+        if constexpr (!C::EIGHT)
         if (any && !a.starve) {
             Ring<C::NS> st;
             int issued = 0;
@@ -193,7 +386,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
         }
     } else if (warp == 10) {
         // ================================ clears rows of V tiles ================================
-        if (any) {
+        if (!C::EIGHT && any) {
             uint32_t stage = 0, uses = 0;                  // position in the ring; bit s: parity of stage s's next landing
             bool more = true;
             while (more) {
@@ -358,7 +551,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
         }
     }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::REGS));
         // ================================ softmax warps: one thread per row ================================
         const int i = warp >> 2;                           // tile
         const int r = tid & 127;                           // row in the tile
@@ -604,7 +797,7 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
         // copies in flight land before the block ends
         if (warp == 9) {
             const Flight f = *flight;
-            for (int k = 0; k < min(f.issued, C::NS); ++k) {
+            for (int k = 0; k < (C::EIGHT ? 0 : min(f.issued, C::NS)); ++k) {
                 if (f.on_landed >> k & 1) mbar_drain(&landed[k], (f.landings >> k & 1) ^ 1);
                 else mbar_drain(&full[k], ((f.issued - k - 1) / C::NS) & 1);
             }
@@ -618,17 +811,25 @@ __global__ void __launch_bounds__(384, 1) k_paged_attn_tc(const __grid_constant_
 
 size_t paged_attn_tc_workspace(int d) { return (size_t)2 * device_sm_count() * 256 * (d + 2) * sizeof(float); }
 
-template <int D>
-static cudaError_t launch_tc_attn(const TcAttnParams &P, cudaStream_t st)
+template <int D, int FMT>
+static cudaError_t launch_tc_attn(const typename TcParamsOf<FMT>::type &P, cudaStream_t st)
 {
-    using C = TcAttnCfg<D>;
+    using C = TcAttnCfg<D, FMT>;
     static bool attr[MAX_DEVICES] = {};
-    cudaError_t e = opt_in_smem(k_paged_attn_tc<D>, C::SMEM, attr);
+    cudaError_t e = opt_in_smem(k_paged_attn_tc<D, FMT>, C::SMEM, attr);
     if (e != cudaSuccess) return e;
-    k_paged_attn_tc<D><<<device_sm_count(), C::THREADS, C::SMEM, st>>>(P);
+    k_paged_attn_tc<D, FMT><<<device_sm_count(), C::THREADS, C::SMEM, st>>>(P);
     e = cudaGetLastError();
     if (e == cudaSuccess) count_launch();
     return e;
+}
+
+// The map of the query rows, and the bytes that one copy of a 64-channel block of a tile brings.
+static bool query_map(CUtensorMap *map, int *bytes, const PagedArgs &a, int d)
+{
+    const int q_tokens = a.n_rows < a.unit_tokens / 2 ? a.n_rows : a.unit_tokens / 2;
+    *bytes = q_tokens * a.group * 128;
+    return make_q_tensor_map(map, a.q, d, a.Hkv * a.group, a.n_rows, a.q_sh, a.q_st, a.group, q_tokens);
 }
 
 cudaError_t launch_paged_attn_tc(const PagedArgs &a, int d, const void *k, const void *v, int page_size, long long s_page,
@@ -637,13 +838,22 @@ cudaError_t launch_paged_attn_tc(const PagedArgs &a, int d, const void *k, const
     TcAttnParams P;
     P.a = a;
     const int box = page_size < 128 ? page_size : 128;
-    const int q_tokens = a.n_rows < a.unit_tokens / 2 ? a.n_rows : a.unit_tokens / 2;
-    P.q_bytes = q_tokens * a.group * 128;
-    if (!make_q_tensor_map(&P.q, a.q, d, a.Hkv * a.group, a.n_rows, a.q_sh, a.q_st, a.group, q_tokens) ||
+    if (!query_map(&P.q, &P.q_bytes, a, d) ||
         !make_kv_tensor_map(&P.k, k, d, a.Hkv, page_size, a.n_pages, s_head, s_slot, s_page, box, 1) ||
         !make_kv_tensor_map(&P.v, v, d, a.Hkv, page_size, a.n_pages, s_head, s_slot, s_page, box, 1))
         return cudaErrorInvalidValue;
-    return d == 128 ? launch_tc_attn<128>(P, st) : launch_tc_attn<64>(P, st);
+    return d == 128 ? launch_tc_attn<128, BF16_PAGES>(P, st) : launch_tc_attn<64, BF16_PAGES>(P, st);
+}
+
+cudaError_t launch_paged8_attn_tc(const PagedArgs &a, const Pool8 &pool, cudaStream_t st)
+{
+    TcAttn8Params P;
+    P.a = a;
+    P.p = pool;
+    if (!query_map(&P.q, &P.q_bytes, a, pool.d)) return cudaErrorInvalidValue;
+    const bool e4m3 = pool.format == CACHE_E4M3;
+    if (pool.d == 128) return e4m3 ? launch_tc_attn<128, CACHE_E4M3>(P, st) : launch_tc_attn<128, CACHE_INT8>(P, st);
+    return e4m3 ? launch_tc_attn<64, CACHE_E4M3>(P, st) : launch_tc_attn<64, CACHE_INT8>(P, st);
 }
 
 }  // namespace cb
