@@ -105,43 +105,43 @@ __device__ __forceinline__ float max3(float x, float y, float z)
 }
 
 // ================================ converting warps (a cache of 8 bits) ================================
-__device__ __forceinline__ uint32_t bf16x2_mul(uint32_t x, uint32_t y)
-{
-    uint32_t r;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
-    return r;
-}
-// Two of a word's codes (the lower, the upper ones) as bf16 numbers code * 2^e, exactly.
+// Codes as bf16 numbers code * 2^e, exactly: to fp16 (one instruction for two), times 2^e to fp32, to bf16.
 struct ToBf16 {
-    uint32_t f;          // e4m3: 2^(120 + e) twice as bf16
-    uint32_t g;          // and the part of it that is past bf16's largest power, or 1
-    float s, m;          // int8: 2^e and -(2^23 + 128) 2^e
+    float s, m;          // 2^e; int8: -(2^23 + 128) 2^e
+    uint16_t h;          // 2^e as fp16
     template <int FMT>
-    __device__ __forceinline__ bool set(int e)             // whether some thread of the warp needs g
+    __device__ __forceinline__ bool set(int e)             // whether some thread of the warp has a 2^e that fp16 does not hold
     {
-        if (FMT == CACHE_E4M3) {
-            f = (uint32_t)(min(e, 7) + 247) * 0x00800080u;             // exponent 120 + e, biased by 127, at bits 7 and 23
-            g = (uint32_t)(max(e - 7, 0) + 127) * 0x00800080u;
-        } else {
-            s = exp2_whole(e);
-            m = -8388736.f * s;
-        }
-        return FMT == CACHE_E4M3 && __any_sync(0xffffffffu, e > 7);
+        s = exp2_whole(e);
+        m = -8388736.f * s;
+        asm("cvt.rn.f16.f32 %0, %1;" : "=h"(h) : "f"(s));
+        return FMT == CACHE_E4M3 && __any_sync(0xffffffffu, e < -24 || e > 15);
     }
-    template <int FMT, bool LARGE>
+    // the lower or the upper two of a word
+    template <int FMT, bool FAR>
     __device__ __forceinline__ uint32_t pair(uint32_t w, int upper) const
     {
+        float a, b;
         if (FMT == CACHE_E4M3) {
-            // sign, exponent and mantissa of a code in the places of bf16's: the number times 2^-120, subnormal or not
-            const uint32_t x = __byte_perm(w, 0, upper ? 0x3424 : 0x1404);
-            uint32_t r = bf16x2_mul((x & 0x80008000u) | ((x >> 4) & 0x07f007f0u), f);
-            if (LARGE) r = bf16x2_mul(r, g);
-            return r;
+            uint16_t x0, x1;
+            asm("{\n\t.reg .b16 lo, hi;\n\t.reg .b32 x;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 x, %3;\n\tmov.b32 {%0, %1}, x;\n\t}"
+                : "=h"(x0), "=h"(x1) : "r"(w), "h"((uint16_t)(upper ? w >> 16 : w)));
+            if (FAR) {
+                asm("cvt.f32.f16 %0, %1;" : "=f"(a) : "h"(x0));
+                asm("cvt.f32.f16 %0, %1;" : "=f"(b) : "h"(x1));
+                a *= s;
+                b *= s;
+            } else {
+                asm("fma.rn.f32.f16 %0, %1, %2, %3;" : "=f"(a) : "h"(x0), "h"(h), "f"(0.f));
+                asm("fma.rn.f32.f16 %0, %1, %2, %3;" : "=f"(b) : "h"(x1), "h"(h), "f"(0.f));
+            }
+        } else {
+            // 2^23 + (code + 128) has the code in its low bits
+            const uint32_t t = w ^ 0x80808080u;
+            a = fmaf(__uint_as_float(__byte_perm(t, 0x4b000000u, upper ? 0x7442 : 0x7440)), s, m);
+            b = fmaf(__uint_as_float(__byte_perm(t, 0x4b000000u, upper ? 0x7443 : 0x7441)), s, m);
         }
-        // 2^23 + (code + 128) has the code in its low bits
-        const uint32_t t = w ^ 0x80808080u;
-        const float a = __uint_as_float(__byte_perm(t, 0x4b000000u, upper ? 0x7442 : 0x7440)), b = __uint_as_float(__byte_perm(t, 0x4b000000u, upper ? 0x7443 : 0x7441));
-        return pack_bf16x2(fmaf(a, s, m), fmaf(b, s, m));
+        return pack_bf16x2(a, b);
     }
 };
 
@@ -226,11 +226,11 @@ __device__ __forceinline__ void tc_convert(const PagedArgs &a, const Pool8 &p, c
             }
             const int e = exp8_clamp(__shfl_sync(0xffffffffu, here.ex, (lane & 24) + comp), FMT);
             ToBf16 to;
-            const bool large = to.template set<FMT>(e);
+            const bool far = to.template set<FMT>(e);
             const uint32_t from = mine + ((n & 1) * 2 + comp) * C::CODES, tile = dst + st.idx * C::TILE;
             const bool clear = comp && here.clear;
-            auto convert = [&](auto wide) {
-                constexpr bool LARGE = decltype(wide)::value;
+            auto convert = [&](auto any_e) {
+                constexpr bool FAR = decltype(any_e)::value;
 #pragma unroll
                 for (int i0 = 0; i0 < 8 / RI; i0 += 4) {
                     uint4 x[4];                            // four loads in flight
@@ -243,8 +243,8 @@ __device__ __forceinline__ void tc_convert(const PagedArgs &a, const Pool8 &p, c
                         // rows that no query sees may hold anything: 0 * NaN would reach the output
                         if (clear && !(j < here.hi && (j >= here.lo || j < a.n_sink))) x[k] = make_uint4(0, 0, 0, 0);
                         const uint32_t w0 = swap ? x[k].z : x[k].x, w1 = swap ? x[k].w : x[k].y, w2 = swap ? x[k].x : x[k].z, w3 = swap ? x[k].y : x[k].w;
-                        const uint4 y = make_uint4(to.template pair<FMT, LARGE>(w0, 0), to.template pair<FMT, LARGE>(w0, 1), to.template pair<FMT, LARGE>(w1, 0), to.template pair<FMT, LARGE>(w1, 1));
-                        const uint4 z = make_uint4(to.template pair<FMT, LARGE>(w2, 0), to.template pair<FMT, LARGE>(w2, 1), to.template pair<FMT, LARGE>(w3, 0), to.template pair<FMT, LARGE>(w3, 1));
+                        const uint4 y = make_uint4(to.template pair<FMT, FAR>(w0, 0), to.template pair<FMT, FAR>(w0, 1), to.template pair<FMT, FAR>(w1, 0), to.template pair<FMT, FAR>(w1, 1));
+                        const uint4 z = make_uint4(to.template pair<FMT, FAR>(w2, 0), to.template pair<FMT, FAR>(w2, 1), to.template pair<FMT, FAR>(w3, 0), to.template pair<FMT, FAR>(w3, 1));
                         const uint32_t at = tile + i * RI * 128;
                         const int first = (col + (swap ? 1 : 0)) ^ (r & 7);
                         asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + (first << 4)), "r"(y.x), "r"(y.y), "r"(y.z), "r"(y.w) : "memory");
@@ -252,7 +252,7 @@ __device__ __forceinline__ void tc_convert(const PagedArgs &a, const Pool8 &p, c
                     }
                 }
             };
-            if (large) convert(std::true_type()); else convert(std::false_type());
+            if (far) convert(std::true_type()); else convert(std::false_type());
             fence_async_smem();
             __syncwarp();
             if (lane == 0) {
