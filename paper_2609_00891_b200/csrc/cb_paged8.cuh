@@ -31,8 +31,8 @@ struct Store8Args {
     long long s_sl, s_st, s_sh;              // source strides (elements): layer, token, head
     const long long *slot_map;
     long long n_rows;
-    int tile;                                // rows of a thread block, a power of two up to 32
-    int wpr;                                 // warps that share a run of rows
+    int tile;                                // rows of a thread block, a power of two
+    int team, heads, groups;                 // warps of one run and head; heads of a block; blocks of a row's heads
 };
 cudaError_t launch_paged8_store(const Store8Args &a, bool f32, cudaStream_t st);
 

@@ -5,56 +5,73 @@
 
 namespace cb {
 
-// A run is the rows of one block that stand together in slot_map (up to 31 skipped rows between two of them); a warp does
-// one run of one head, K or V: largest magnitude, exponent, codes.  The first 16 rows stay in registers in between, so that
-// a row is read once; those of a longer run come from L2 the second time.
-// grid (row tiles, layers, groups of wpr of the 2 H heads of K and V); a block's 8 / wpr warp groups take its runs in turn.
+__device__ __forceinline__ float max3(float x, float y, float z)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    return r;
+}
+
+// A run is the rows of one block that stand together in slot_map (up to 31 skipped rows between two of them); `team` warps do
+// one run of one head, K in the lower and V in the upper half of each: largest magnitude, exponent, codes.  A warp takes CHUNK
+// rows at a time and keeps its first ones in registers in between, so that with enough warps a row is read once; the others come
+// from L1 or L2 the second time.
+// grid (row tiles x groups of heads, layers): the heads of a row are read side by side; the warps that are not needed for heads take
+// further runs of the tile.
 template <bool F32, int FMT, int D>
-__global__ void __launch_bounds__(256) k_paged8_store(const Store8Args a)
+__global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
 {
     constexpr int LPR = D / 8;                   // lanes of a row, 8 channels each
-    constexpr int RPI = 32 / LPR;                // rows of one load of the warp
-    constexpr int KEEP = 16;                     // rows of a chunk
-    constexpr int ITER = KEEP / RPI;
+    constexpr int RPI = 16 / LPR;                // rows of one load of half a warp
     constexpr int W = F32 ? 2 : 1;               // 16-byte pieces of 8 channels
+    constexpr int ITER = 16 / W, CHUNK = ITER * RPI;
+    constexpr int PART = ITER / 4;               // loads at a time of the chunks that are not kept
+    __shared__ uint32_t largest_of[8][2];
     const Pool8 &p = a.pool;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int pair = blockIdx.z * a.wpr + warp % a.wpr;
-    if (pair >= 2 * p.H) return;
-    const int h = pair >> 1, comp = pair & 1;
-    const long long r0 = (long long)blockIdx.x * a.tile;
+    const int comp = lane >> 4, half = lane & 16;
+    const int mate = warp % a.team, unit = warp / a.team;                  // of the team, and which one in the block
+    const unsigned tile = blockIdx.x / (unsigned)a.groups;
+    const int head = (int)(blockIdx.x - tile * a.groups) * a.heads + unit % a.heads, stride = 8 / a.team / a.heads;
     const int layer = blockIdx.y;
 
     auto slot_of = [&](long long row) { return row >= 0 && row < a.n_rows ? __ldg(a.slot_map + row) : -1ll; };
     auto fits = [&](long long slot) { return slot >= 0 && slot < p.n_slots; };
+    const int sub = (lane & 15) / LPR, c8 = (lane % LPR) * 8;              // row of a load, first channel
+    const int h = min(head, p.H - 1);
+    const char *src = static_cast<const char *>(comp ? a.src_v : a.src_k) + ((long long)layer * a.s_sl + (long long)h * a.s_sh + c8) * (F32 ? 4 : 2);
+    uint8_t *codes = (comp ? p.v : p.k) + (long long)layer * p.sl + (long long)h * p.sh + c8;
+    int8_t *exps = (comp ? p.ve : p.ke) + (long long)layer * p.el + (long long)h * p.eh;
+    const long long row_bytes = a.s_st * (F32 ? 4 : 2);
+    const int slot_mask = (1 << p.page_log2) - 1, block_mask = (1 << p.block_log2) - 1;
+
+    // 32 rows of the tile at a time
+    for (long long r0 = (long long)tile * a.tile, r1 = min(r0 + a.tile, a.n_rows); r0 < r1; r0 += 32) {
     // runs that begin in this tile: valid rows whose nearest valid row of the 32 before them is of another block, or missing
-    const long long mine = lane < a.tile ? slot_of(r0 + lane) : -1;
+    const long long mine = r0 + lane < r1 ? slot_of(r0 + lane) : -1, back = slot_of(r0 - 32 + lane);
     const long long my_block = mine >> p.block_log2;
     const bool ok = fits(mine);
-    const unsigned valid = __ballot_sync(0xffffffffu, ok);
-    if (!valid) return;
-    const long long back = slot_of(r0 - 32 + lane);
-    const unsigned valid_back = __ballot_sync(0xffffffffu, fits(back));
+    const unsigned valid = __ballot_sync(0xffffffffu, ok), valid_back = __ballot_sync(0xffffffffu, fits(back));
     const unsigned here = valid & ((1u << lane) - 1u);
     const int from = here ? 31 - __clz(here) : valid_back ? 31 - __clz(valid_back) : 0;
     const long long prev_here = __shfl_sync(0xffffffffu, mine, from), prev_back = __shfl_sync(0xffffffffu, back, from);
     const bool near = here || (valid_back && lane <= from);                // at most 32 rows back
-    const bool head = ok && !(near && ((here ? prev_here : prev_back) >> p.block_log2) == my_block);
-    const unsigned heads = __ballot_sync(0xffffffffu, head);
-    const int rank = __popc(heads & ((1u << lane) - 1u));
+    const bool begins = ok && !(near && ((here ? prev_here : prev_back) >> p.block_log2) == my_block);
+    const unsigned heads = __ballot_sync(0xffffffffu, begins);
+    const int rank = __popc(heads & ((1u << lane) - 1u)), n_runs = __popc(heads);
 
-    const int sub = lane / LPR, c8 = (lane % LPR) * 8;                     // row of a load, first channel
-    const char *src = static_cast<const char *>(comp ? a.src_v : a.src_k) + ((long long)layer * a.s_sl + (long long)h * a.s_sh + c8) * (F32 ? 4 : 2);
-    uint8_t *codes = (comp ? p.v : p.k) + (long long)layer * p.sl + (long long)h * p.sh;
-    int8_t *exps = (comp ? p.ve : p.ke) + (long long)layer * p.el + (long long)h * p.eh;
-    const int slot_mask = (1 << p.page_log2) - 1, n_groups = 8 / a.wpr;
-
-    for (int run = warp / a.wpr; run < __popc(heads); run += n_groups) {
-        const int at = __ffs(__ballot_sync(0xffffffffu, head && rank == run)) - 1;
-        const long long begin = r0 + at;
+    for (int run0 = 0; run0 < n_runs; run0 += stride) {                    // the same rounds in every warp: they meet below
+        const int run = run0 + unit / a.heads;
+        const bool live = run < n_runs && head < p.H;
+        const int at = live ? __ffs(__ballot_sync(0xffffffffu, begins && rank == run)) - 1 : 0;
+        const long long first = r0 + at;
         const long long block = __shfl_sync(0xffffffffu, my_block, at);
+        const long long page = block >> (p.page_log2 - p.block_log2), in_page = block & ((1 << (p.page_log2 - p.block_log2)) - 1);
+        int8_t *ep = exps + page * p.ep + in_page * p.eb;
+        uint8_t *base = codes + page * p.sp;
+        const int old = live && (lane & 15) == 0 ? (int)*ep : 0;
         // rows of the run among the 32 from `row`, as bits; `last`: the latest one found so far, -1 at the end of the run
-        long long slot;                                                    // this lane's
+        long long slot = -1;                                               // this lane's
         auto members = [&](long long row, long long &last) -> unsigned {
             slot = slot_of(row + lane);
             const bool v = fits(slot), same = v && (slot >> p.block_log2) == block;
@@ -65,19 +82,15 @@ __global__ void __launch_bounds__(256) k_paged8_store(const Store8Args a)
             last = other ? -1 : row + 31 - __clz(m);
             return m;
         };
-        uint4 keep[ITER][W];
-        float most = 0.f;
-        unsigned m0 = 0;                                                   // the first window's rows
-        long long slot0 = -1;
-        bool begun = false;
-        auto load = [&](long long row, unsigned m, int first, uint4 (&x)[ITER][W]) {
+        auto load = [&](long long row, unsigned m, int k0, auto &x) {
+            const char *at = src + (row + k0 + sub) * row_bytes;
+            m >>= k0 + sub;
 #pragma unroll
-            for (int i = 0; i < ITER; ++i) {
-                const int k = first + i * RPI + sub;
+            for (int i = 0; i < (int)(sizeof(x) / sizeof(x[0])); ++i, at += RPI * row_bytes) {
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
                     x[i][w] = make_uint4(0, 0, 0, 0);
-                    if (m >> k & 1) x[i][w] = __ldg(reinterpret_cast<const uint4 *>(src + (row + k) * a.s_st * (F32 ? 4 : 2)) + w);
+                    if (m & (1u << i * RPI)) x[i][w] = __ldg(reinterpret_cast<const uint4 *>(at) + w);
                 }
             }
         };
@@ -94,96 +107,141 @@ __global__ void __launch_bounds__(256) k_paged8_store(const Store8Args a)
                 for (int j = 0; j < 4; ++j) { f[2 * j] = __uint_as_float(u[j] << 16); f[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u); }
             }
         };
-        auto largest = [&](const uint4 (&x)[ITER][W]) {
+        float most = 0.f, finite = 0.f;                                    // finite: not 0 once a value was infinite or NaN
+        bool begun = false;                                                // the block's first row is among the run's
+        auto largest = [&](const auto &x) {
 #pragma unroll
-            for (int i = 0; i < ITER; ++i) {
+            for (int i = 0; i < (int)(sizeof(x) / sizeof(x[0])); ++i) {
                 float f[8];
                 values(x[i], f);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(f[j]));   // NaN is passed over
+                for (int j = 0; j < 8; j += 2) most = max3(most, fabsf(f[j]), fabsf(f[j + 1]));    // NaN is passed over
+                if (FMT == CACHE_INT8) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) finite = fmaf(f[j], 0.f, finite);
+                }
+            }
+        };
+        // The team's chunks go round: this warp's are the ones with number mate, mate + team, ...  `each` is called with the 32 rows'
+        // first one, their bits, and the place of a chunk of this warp among them.
+        auto chunks = [&](auto each) {
+            long long last = live ? first : -1;
+            int before = 0;                                                // chunks of the 32 rows before these
+            for (long long row = first; last >= 0; row += 32, before += 32 / CHUNK) {
+                const unsigned m = members(row, last);
+                begun |= __any_sync(0xffffffffu, (m >> lane & 1) && ((int)slot & block_mask) == 0) != 0;
+#pragma unroll 1
+                for (int k0 = ((mate - before) & (a.team - 1)) * CHUNK; k0 < 32; k0 += a.team * CHUNK)
+                    if (m >> k0) each(row, m, k0);
+                if (!m) break;
             }
         };
         // ---- largest magnitude ----
-        long long last = begin;
-        for (long long row = begin; last >= 0; row += 32) {
-            const unsigned m = members(row, last);
-            if (!m) break;
-            begun |= __any_sync(0xffffffffu, (m >> lane & 1) && (slot & ((1 << p.block_log2) - 1)) == 0);
-            if (row == begin) {
-                m0 = m;
-                slot0 = slot;
-                load(row, m, 0, keep);
+        uint4 keep[ITER][W];
+        unsigned kept = 0;                                                 // the kept chunk's rows
+        long long kept_slot = -1, kept_row = -1;
+        int kept_k0 = 0;
+        bool others = false;
+        chunks([&](long long row, unsigned m, int k0) {
+            if (kept_row < 0) {
+                kept = m;
+                kept_k0 = k0;
+                kept_row = row;
+                kept_slot = slot;
+                load(row, m, k0, keep);
                 largest(keep);
-            }
-            for (int first = row == begin ? KEEP : 0; first < 32; first += KEEP) {
-                if (!(m >> first)) break;
-                uint4 x[ITER][W];
-                load(row, m, first, x);
-                largest(x);
-            }
-        }
-        const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(most));
-        const long long page = block >> (p.page_log2 - p.block_log2), in_page = block & ((1 << (p.page_log2 - p.block_log2)) - 1);
-        int8_t *ep = exps + page * p.ep + in_page * p.eb;
-        uint8_t *base = codes + page * p.sp;
-        const int need = exp8_need<FMT>(top);
-        int e = need;
-        if (!begun) {
-            const int old = exp8_clamp(__shfl_sync(0xffffffffu, lane == 0 ? (int)*ep : 0, 0), FMT);
-            e = max(old, need);
-            if (e > old) {                                                 // the block's codes, rounded to the larger step
-                const float f = exp2_whole(max(old - e, -126));
-                for (int r = sub; r < 1 << p.block_log2; r += RPI) {
-                    uint2 *q = reinterpret_cast<uint2 *>(base + ((in_page << p.block_log2) + r) * p.ss + c8);
-                    const uint2 c = *q;
-                    *q = make_uint2(to_codes<FMT>(codes_to_f32<FMT>(c.x, f)), to_codes<FMT>(codes_to_f32<FMT>(c.y, f)));
+            } else {
+                others = true;
+#pragma unroll 1
+                for (int k = k0; k < k0 + CHUNK; k += PART * RPI) {
+                    uint4 x[PART][W];
+                    load(row, m, k, x);
+                    largest(x);
                 }
-                __syncwarp();
+            }
+        });
+        uint32_t top = __float_as_uint(most);
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (a.team > 1) {
+            if (threadIdx.x < 16) largest_of[threadIdx.x >> 1][threadIdx.x & 1] = 0;
+            __syncthreads();
+            if ((lane & 15) == 0) atomicMax(&largest_of[unit][comp], top);
+            __syncthreads();
+            top = largest_of[unit][comp];
+        }
+        const int held = exp8_clamp(__shfl_sync(0xffffffffu, old, half), FMT), need = exp8_need<FMT>(top);
+        const int e = begun ? need : max(held, need);
+        if (live && !begun && e > held) {                                  // the block's codes, rounded to the larger step
+            const float f = exp2_whole(max(held - e, -126));
+#pragma unroll 4
+            for (int r = mate * RPI + sub; r < 1 << p.block_log2; r += a.team * RPI) {
+                uint2 *q = reinterpret_cast<uint2 *>(base + ((in_page << p.block_log2) + r) * p.ss);
+                const uint2 c = *q;
+                *q = make_uint2(to_codes<FMT>(codes_to_f32<FMT>(c.x, f)), to_codes<FMT>(codes_to_f32<FMT>(c.y, f)));
             }
         }
-        if (lane == 0) *ep = (int8_t)e;
+        if (a.team > 1) __syncthreads(); else __syncwarp();
+        if (live && mate == 0 && (lane & 15) == 0) *ep = (int8_t)e;
         // ---- codes ----
         const float f = exp2_whole(-e);
-        auto write = [&](const uint4 (&x)[ITER][W], unsigned m, int first, long long slots) {
+        const bool plain = FMT == CACHE_INT8 && __all_sync(0xffffffffu, finite == 0.f && e < exp8_most(FMT));      // all are within the codes' range
+        auto write = [&](const auto &x, unsigned m, int k0, long long slots) {
 #pragma unroll
-            for (int i = 0; i < ITER; ++i) {
-                const int k = first + i * RPI + sub;
-                const long long to = __shfl_sync(0xffffffffu, slots, k);
+            for (int i = 0; i < (int)(sizeof(x) / sizeof(x[0])); ++i) {
+                const int k = k0 + i * RPI + sub;
+                const int to = __shfl_sync(0xffffffffu, (int)slots & slot_mask, k);
                 if (m >> k & 1) {
                     float v[8];
                     values(x[i], v);
-                    *reinterpret_cast<uint2 *>(base + (to & slot_mask) * p.ss + c8) =
-                        make_uint2(to_codes<FMT>(make_float4(v[0] * f, v[1] * f, v[2] * f, v[3] * f)), to_codes<FMT>(make_float4(v[4] * f, v[5] * f, v[6] * f, v[7] * f)));
+                    uint2 c;
+                    if (plain) {
+                        // 1.5 * 2^23 + x / 2^e, rounded, has the code in its low byte
+                        uint32_t u[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(fmaf(v[j], f, 12582912.f));
+                        c.x = __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
+                        c.y = __byte_perm(__byte_perm(u[4], u[5], 0x0040), __byte_perm(u[6], u[7], 0x0040), 0x5410);
+                    } else {
+                        c.x = to_codes<FMT>(make_float4(v[0] * f, v[1] * f, v[2] * f, v[3] * f));
+                        c.y = to_codes<FMT>(make_float4(v[4] * f, v[5] * f, v[6] * f, v[7] * f));
+                    }
+                    *reinterpret_cast<uint2 *>(base + (unsigned long long)(unsigned)to * (unsigned)p.ss) = c;
                 }
             }
         };
-        write(keep, m0, 0, slot0);
-        last = begin;
-        for (long long row = begin; last >= 0; row += 32) {
-            const unsigned m = members(row, last);
-            if (!m) break;
-            for (int first = row == begin ? KEEP : 0; first < 32; first += KEEP) {
-                if (!(m >> first)) break;
-                uint4 x[ITER][W];
-                load(row, m, first, x);
-                write(x, m, first, slot);
-            }
-        }
-        __syncwarp();
+        if (kept) write(keep, kept, kept_k0, kept_slot);
+        if (others)
+            chunks([&](long long row, unsigned m, int k0) {
+                if (row == kept_row && k0 == kept_k0) return;
+#pragma unroll 1
+                for (int k = k0; k < k0 + CHUNK; k += PART * RPI) {
+                    uint4 x[PART][W];
+                    load(row, m, k, x);
+                    write(x, m, k, slot);
+                }
+            });
+        if (a.team > 1) __syncthreads(); else __syncwarp();                // the block's run before this one's is no longer looked at
+    }
     }
 }
 
 cudaError_t launch_paged8_store(const Store8Args &args, bool f32, cudaStream_t st)
 {
     Store8Args a = args;
-    // Rows of a block: 32 where there are enough of them for four blocks an SM, fewer otherwise (a step's few rows).
+    // A warp for every chunk (16 rows of 128 channels in bf16, 8 in fp32), and as many heads as the block's eight warps then hold.
+    const int chunk = (f32 ? 8 : 16) * 128 / a.pool.d;
+    a.team = 1;
+    while (a.team < 8 && (chunk * a.team) >> a.pool.block_log2 == 0) a.team *= 2;
+    a.heads = 1;
+    while (a.heads < 8 / a.team && a.heads < a.pool.H) a.heads *= 2;
+    a.groups = (a.pool.H + a.heads - 1) / a.heads;
+    // Rows of a block: those of one cache block, at least 32, where that leaves four blocks an SM (a tile without the beginning of a
+    // run has nothing to do); fewer otherwise (a step's few rows).
     const long long wanted = 4ll * device_sm_count();
-    a.tile = 32;
-    a.wpr = 1;
-    while (a.wpr < 8 && a.wpr < 2 * a.pool.H) a.wpr *= 2;
-    const int groups = (2 * a.pool.H + a.wpr - 1) / a.wpr;
-    while (a.tile > 1 && (a.n_rows + a.tile - 1) / a.tile * a.pool.L * groups < wanted) a.tile /= 2;
-    dim3 grid((unsigned)((a.n_rows + a.tile - 1) / a.tile), (unsigned)a.pool.L, (unsigned)groups);
+    a.tile = a.pool.block_log2 > 5 ? 1 << a.pool.block_log2 : 32;
+    while (a.tile > 1 && (a.n_rows + a.tile - 1) / a.tile * a.pool.L * a.groups < wanted) a.tile /= 2;
+    dim3 grid((unsigned)((a.n_rows + a.tile - 1) / a.tile * a.groups), (unsigned)a.pool.L);
     auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a); };
     const bool e4m3 = a.pool.format == CACHE_E4M3;
     if (a.pool.d == 128) {
