@@ -181,7 +181,8 @@ struct alignas(16) PaSum { long long tiles; int units, most; };
 // Where there are no more pairs than blocks and the longest one is at most EVEN tiles above an equal share, every pair goes
 // to a block of its own: joining two parts costs about that much (32 requests with a window of 1,024 keys, 256 pairs of 17
 // or 18 tiles of 64 keys: 38 us split, see k_paged_attn_few; for the tensor-memory kernel the number was taken over, not
-// measured).
+// measured; for the kernel for few rows over an 8-bit cache, of 128 keys a tile, 20.9 us against 22.2 with EVEN = 1 for 32 requests of
+// 1,024 keys).
 template <int ROWS, int KT, int THREADS>
 __device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int cap, PaShare *share, PaSum *sums)
 {
@@ -353,6 +354,13 @@ __device__ __forceinline__ float pa_exp2(float x)
 {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// Largest of three (one instruction on sm_100).
+__device__ __forceinline__ float max3(float x, float y, float z)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
     return r;
 }
 #endif

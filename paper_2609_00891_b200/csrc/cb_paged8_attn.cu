@@ -81,26 +81,6 @@ __device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src, uint3
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ uint4 lds16(uint32_t a)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint2 lds8(uint32_t a)
-{
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
-    return v;
-}
-
-__device__ __forceinline__ float largest3(float x, float y, float z)
-{
-    float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
-    return r;
-}
-
 // Four codes of K as fp16: e4m3 as they are, int8 as (code + 128) 2^-24, which are the subnormal numbers with that byte: the scores
 // then have 2^-24 of 128 times the row's sum of q on them, no larger than the scores themselves can be.
 template <int FMT>
@@ -173,15 +153,13 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
             const bool there = (unsigned)page < (unsigned)p.n_pages;
             const uint32_t to = ring_u + (s & 1) * C::STAGE, bytes = there ? 16u : 0u;
             const unsigned long long from = there ? (unsigned long long)(unsigned)page * (unsigned)p.sp + (unsigned long long)slot * (unsigned)p.ss : 0ull;
-            const unsigned long long step = there ? (unsigned long long)RI * p.ss : 0ull;
+            const unsigned step = there ? (unsigned)p.ss : 0u;
             const uint8_t *ks = kb + from, *vs = vb + from;
 #pragma unroll
             for (int i = 0; i < 8 / RI; ++i) {
                 const uint32_t at = to + piece_at<D>(group8 + i * RI + crow, cpiece);
-                cp_async_16(at, ks, bytes);
-                cp_async_16(at + C::HALF, vs, bytes);
-                ks += step;
-                vs += step;
+                cp_async_16(at, ks + (unsigned long long)step * (unsigned)(i * RI), bytes);
+                cp_async_16(at + C::HALF, vs + (unsigned long long)step * (unsigned)(i * RI), bytes);
             }
             cp_async_commit();
             ex = NONE;
@@ -264,39 +242,28 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
             const int ex_here = ex_next;
             if (s + 1 < n) issue(s + 1, page, ex_next);
             page = page_of(s + 2);
-            const uint32_t at = ring_u + (s & 1) * C::STAGE, at1 = at + C::HALF;
+            const uint8_t *at = ring + (s & 1) * C::STAGE, *at1 = at + C::HALF;
             const bool edge = w.t + s < full0 || w.t + s >= full1;
             const int j0 = pa_tile(u, w.t + s) * C::KT + warp * 32;
 
-            // ---- scores: keys g, g + 8, g + 16, g + 24 (h = 0 .. 3), rows 2 t4 and 2 t4 + 1 ----
-            float x[2][NT][4];
+            // ---- exponents of the four groups of 8 keys (h = 0 .. 3), a byte each: e + 128, 0 for NONE ----
+            // Where V's lie within 2^-4 .. 2 of the output's unit, each key's goes onto its weight and the product adds to the output; else
+            // every group has a product of its own.
+            const unsigned byte = ex_here == NONE ? 0u : (unsigned)(exp8_clamp(ex_here, FMT) + 128) << (lane & 24);
+            const unsigned all_k = __reduce_or_sync(0xffffffffu, (lane & 7) == 0 ? byte : 0u);
+            const unsigned all_v = __reduce_or_sync(0xffffffffu, (lane & 7) == 1 ? byte : 0u);
+            float fk[4];                                   // 2^(K's exponent)
+            int ev[4];                                     // V's exponent less the unit's
+            int ev_top = 0;
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-                for (int i = 0; i < CQ / 16; ++i) {
-                    const uint4 a0 = lds16(at + piece_at<D>(kk * 16 + g, t4 * (CQ / 16) + i)), a1 = lds16(at + piece_at<D>(kk * 16 + g + 8, t4 * (CQ / 16) + i));
-                    const uint32_t w0[4] = {a0.x, a0.y, a0.z, a0.w}, w1[4] = {a1.x, a1.y, a1.z, a1.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t f[4];
-                        keys_to_f16<FMT>(w0[j], f[0], f[2]);
-                        keys_to_f16<FMT>(w1[j], f[1], f[3]);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            if (i == 0 && j == 0) mma_f16_16816_first(x[kk][nt], f, qf[nt][0][0], qf[nt][0][1]);
-                            else mma_f16_16816(x[kk][nt], f, qf[nt][4 * i + j][0], qf[nt][4 * i + j][1]);
-                        }
-                    }
-                }
-            // V's exponents.  Where those of the step lie within 2^-4 .. 2 of the output's unit, each key's goes onto its weight and
-            // the product adds to the output; else every group of 8 keys has a product of its own.  Lanes 8 h + 1 have V's of
-            // group h, lanes 8 h K's.
-            const int ex = exp8_clamp(ex_here, FMT);
-            const bool mine = (lane & 7) == 1 && ex_here != NONE;
-            if (__any_sync(0xffffffffu, mine && ex > eo + 1)) {        // a larger unit
-                const int ev_top = __reduce_max_sync(0xffffffffu, mine ? ex : NONE);
-                const float f = exp2_whole(max(eo - ev_top, -126));
-                eo = ev_top;
+            for (int h = 0; h < 4; ++h) {
+                fk[h] = __uint_as_float((max((all_k >> (8 * h)) & 255u, 1u) - 1u) << 23);
+                ev[h] = (int)((all_v >> (8 * h)) & 255u);
+                ev_top = max(ev_top, ev[h]);
+            }
+            if (ev_top - 128 > eo + 1 && ev_top > 0) {     // a larger unit
+                const float f = exp2_whole(max(eo - (ev_top - 128), -126));
+                eo = ev_top - 128;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -304,15 +271,43 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[nt][i][e] *= f;
             }
-            const int ev = mine ? ex - eo : 0;
-            const bool close = __all_sync(0xffffffffu, ev >= -4);
-            const float fv = exp2_whole(max(ev, -126));                // this lane's, and what its exponent adds to the weight's
-            const float scale8 = exp2_whole(ex), shift = close ? (float)ev : 0.f, unshift = close ? exp2_whole(-max(ev, -4)) : 1.f;
-            float fk[4], dv[4];
+            bool close = true;
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-                fk[h] = __shfl_sync(0xffffffffu, scale8, 8 * h);
-                dv[h] = __shfl_sync(0xffffffffu, shift, 8 * h + 1);
+                ev[h] = ev[h] == 0 ? 0 : ev[h] - 128 - eo;
+                close &= ev[h] >= -4;
+            }
+            float dv[4], undo[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                dv[h] = close ? (float)ev[h] : 0.f;
+                undo[h] = close ? exp2_whole(-ev[h]) : 1.f;
+            }
+
+            // ---- scores: keys g, g + 8, g + 16, g + 24, rows 2 t4 and 2 t4 + 1 ----
+            float x[2][NT][4];
+#pragma unroll
+            for (int i = 0; i < CQ / 16; ++i) {
+                uint4 w[2][2];
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) w[kk][y] = *reinterpret_cast<const uint4 *>(at + piece_at<D>(kk * 16 + y * 8 + g, t4 * (CQ / 16) + i));
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int kk = 0; kk < 2; ++kk) {       // two sums in turn: each waits for its last product
+                        const uint32_t w0 = j == 0 ? w[kk][0].x : j == 1 ? w[kk][0].y : j == 2 ? w[kk][0].z : w[kk][0].w;
+                        const uint32_t w1 = j == 0 ? w[kk][1].x : j == 1 ? w[kk][1].y : j == 2 ? w[kk][1].z : w[kk][1].w;
+                        uint32_t f[4];
+                        keys_to_f16<FMT>(w0, f[0], f[2]);
+                        keys_to_f16<FMT>(w1, f[1], f[3]);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            if (i == 0 && j == 0) mma_f16_16816_first(x[kk][nt], f, qf[nt][0][0], qf[nt][0][1]);
+                            else mma_f16_16816(x[kk][nt], f, qf[nt][4 * i + j][0], qf[nt][4 * i + j][1]);
+                        }
+                    }
             }
             uint32_t pb[2][NT][2];                         // weights: row g, keys 2 t4, 2 t4 + 1 (and + 8) of each 16
             float t[NT][2][4];                             // exponents of the weights
@@ -330,7 +325,7 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     exponents(nt, e, m[nt][e]);
-                    top = largest3(top, largest3(t[nt][e][0], t[nt][e][1], t[nt][e][2]), t[nt][e][3]);
+                    top = max3(top, max3(t[nt][e][0], t[nt][e][1], t[nt][e][2]), t[nt][e][3]);
                 }
             if (__any_sync(0xffffffffu, top > 15.f)) {     // the first keys of a row (m is -inf), or a maximum that grew by 9 or more
 #pragma unroll
@@ -356,12 +351,11 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
             }
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-                const float f = __shfl_sync(0xffffffffu, unshift, 8 * h + 1);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     const float y0 = pa_exp2(t[nt][0][h]), y1 = pa_exp2(t[nt][1][h]);
-                    l[nt][0] = fmaf(y0, f, l[nt][0]);
-                    l[nt][1] = fmaf(y1, f, l[nt][1]);
+                    l[nt][0] = fmaf(y0, undo[h], l[nt][0]);
+                    l[nt][1] = fmaf(y1, undo[h], l[nt][1]);
                     pb[h >> 1][nt][h & 1] = transpose_8x8(pack_f16x2(y0, y1));
                 }
             }
@@ -374,10 +368,10 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
                 for (int k = 0; k < 4; ++k) {
                     const int r = kk * 16 + 2 * t4 + (k & 1) + (k >> 1) * 8;
                     if (D == 128) {
-                        const uint4 z = lds16(at1 + piece_at<D>(r, g));
+                        const uint4 z = *reinterpret_cast<const uint4 *>(at1 + piece_at<D>(r, g));
                         v[k][0] = z.x; v[k][1] = z.y; v[k][CPT / 4 - 2] = z.z; v[k][CPT / 4 - 1] = z.w;
                     } else {
-                        const uint2 z = lds8(at1 + piece_at<D>(r, g >> 1) + (g & 1) * 8);
+                        const uint2 z = *reinterpret_cast<const uint2 *>(at1 + piece_at<D>(r, g >> 1) + (g & 1) * 8);
                         v[k][0] = z.x; v[k][1] = z.y;
                     }
                     // rows that no query sees may hold anything: their values become zeros, or 0 * NaN would reach the output
@@ -387,26 +381,34 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
                         for (int c = 0; c < CPT / 4; ++c) v[k][c] = 0;
                     }
                 }
-                const float f0 = __shfl_sync(0xffffffffu, fv, 16 * kk + 1), f1 = __shfl_sync(0xffffffffu, fv, 16 * kk + 9);
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    // channels 4 c + {0, 1} (i even) or {2, 3}: (row 2 t4, row 2 t4 + 1) of each, and the rows 8 on
-                    uint32_t f[4];
+                // channels 4 c + {0, 1} (i even) or {2, 3}: (row 2 t4, row 2 t4 + 1) of each, and the rows 8 on
+                auto fragment = [&](int i, uint32_t (&f)[4]) {
 #pragma unroll
                     for (int y = 0; y < 2; ++y)
                         codes_to_f16<FMT>(__byte_perm(v[2 * y][i >> 1], v[2 * y + 1][i >> 1], (i & 1) ? 0x7362 : 0x5140), f[2 * y], f[2 * y + 1]);
-                    if (close) {
+                };
+                if (close) {
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        uint32_t f[4];
+                        fragment(i, f);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) mma_f16_16816(o[nt][i], f, pb[kk][nt][0], pb[kk][nt][1]);
-                    } else {
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        uint32_t f[4];
+                        fragment(i, f);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int y = 0; y < 2; ++y) {
                                 float d[4] = {0.f, 0.f, 0.f, 0.f};
                                 mma_f16_1688(d, f[2 * y], f[2 * y + 1], pb[kk][nt][y]);
+                                const float fv = exp2_whole(max(ev[2 * kk + y], -126));
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) o[nt][i][e] = fmaf(d[e], y ? f1 : f0, o[nt][i][e]);
+                                for (int e = 0; e < 4; ++e) o[nt][i][e] = fmaf(d[e], fv, o[nt][i][e]);
                             }
                     }
                 }
@@ -475,21 +477,21 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
             __syncthreads();
             if (last_flag) {
                 const float *first = a.part + (size_t)w.record(b0) * C::REC;
+                auto record = [&](int c) { return c == b0 ? first : a.part + (size_t)(2 * c) * C::REC; };
                 for (int i = tid; i < u.rows * (D / 4); i += 128) {
                     const int r = i / (D / 4), c4 = (i % (D / 4)) * 4;
                     float mm = -INFINITY, ll = 0.f;
                     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-                    // eight parts at a time, so that their loads are in flight together
-                    for (int c = b0; c <= b1; c += 8) {
-                        float pm[8], pl[8];
-                        float4 pv[8];
+                    for (int c = b0; c <= b1; c += 16) {
+                        float pm[16], pl[16];
+                        float4 pv[16];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
+                        for (int k = 0; k < 16; ++k) {
                             pm[k] = -INFINITY;
                             pl[k] = 0.f;
                             pv[k] = make_float4(0.f, 0.f, 0.f, 0.f);
                             if (c + k <= b1) {
-                                const float *rc = c + k == b0 ? first : a.part + (size_t)(2 * (c + k)) * C::REC;
+                                const float *rc = record(c + k);
                                 pm[k] = __ldcg(rc + C::ROWS * D + r);
                                 pl[k] = __ldcg(rc + C::ROWS * D + C::ROWS + r);
                                 pv[k] = __ldcg(reinterpret_cast<const float4 *>(rc + r * D + c4));
@@ -497,13 +499,13 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
                         }
                         float mn = mm;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) mn = fmaxf(mn, pm[k]);
+                        for (int k = 0; k < 16; ++k) mn = fmaxf(mn, pm[k]);
                         const float ref = mn == -INFINITY ? 0.f : mn, f0 = pa_exp2(mm - ref);
                         mm = mn;
                         ll *= f0;
                         x.x *= f0; x.y *= f0; x.z *= f0; x.w *= f0;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
+                        for (int k = 0; k < 16; ++k) {
                             const float f = pa_exp2(pm[k] - ref);
                             ll = fmaf(f, pl[k], ll);
                             x.x = fmaf(f, pv[k].x, x.x); x.y = fmaf(f, pv[k].y, x.y); x.z = fmaf(f, pv[k].z, x.z); x.w = fmaf(f, pv[k].w, x.w);

@@ -5,13 +5,6 @@
 
 namespace cb {
 
-__device__ __forceinline__ float max3(float x, float y, float z)
-{
-    float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
-    return r;
-}
-
 // A run is the rows of one block that stand together in slot_map (up to 31 skipped rows between two of them); `team` warps do
 // one run of one head, K in the lower and V in the upper half of each: largest magnitude, exponent, codes.  A warp takes CHUNK
 // rows at a time and keeps its first ones in registers in between, so that with enough warps a row is read once; the others come

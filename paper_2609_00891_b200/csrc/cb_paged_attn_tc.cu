@@ -96,13 +96,6 @@ __device__ __forceinline__ int ld_acquire(const int *p)
     asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
 }
-// Largest of three (one instruction on sm_100).
-__device__ __forceinline__ float max3(float x, float y, float z)
-{
-    float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
-    return r;
-}
 
 // ================================ converting warps (a cache of 8 bits) ================================
 // Codes as bf16 numbers code * 2^e, exactly: to fp16 (one instruction for two), times 2^e to fp32, to bf16.
