@@ -534,6 +534,21 @@ static PFN_cuTensorMapEncodeTiled_v12000 encode_fn()
 }
 
 // 4-D map over (64 channels, head, token, 64-channel block): one box = 64 channels of box_heads heads of box_tokens tokens.
+bool make_code_tensor_map(CUtensorMap *map, const void *base, int d, int H, int rows, long long pages, long long sh, long long ss,
+                          long long sp, int box_rows)
+{
+    PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
+    if (!enc) return false;
+    auto stride = [&](long long bytes, long long size) -> cuuint64_t {
+        return (size == 1 || bytes == 0) ? (cuuint64_t)d : (cuuint64_t)bytes;                 // size-1 dimension: any valid stride
+    };
+    cuuint64_t gdim[4] = {(cuuint64_t)d, (cuuint64_t)rows, (cuuint64_t)H, (cuuint64_t)pages};
+    cuuint64_t gstr[3] = {stride(ss, rows), stride(sh, H), stride(sp, pages)};
+    cuuint32_t box[4] = {(cuuint32_t)d, (cuuint32_t)box_rows, 1, 1}, estr[4] = {1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(base), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool make_q_tensor_map(CUtensorMap *map, const void *base, int d, int H, long long T, long long sh, long long st, int box_heads,
                        int box_tokens)
 {

@@ -141,6 +141,11 @@ void count_launch(int n = 1);
 bool make_kv_tensor_map(CUtensorMap *map, const void *base, int d, int H, long long T, int L,
                         long long sh, long long st, long long sl, int box_tokens, int box_cblocks = 0);
 
+// 4-D tensor map over (channel, row, head, page) of the codes of a cache of 8 bits: one box = box_rows rows of one head of one page, in
+// shared memory as [row][channel].
+bool make_code_tensor_map(CUtensorMap *map, const void *base, int d, int H, int rows, long long pages, long long sh, long long ss,
+                          long long sp, int box_rows);
+
 // 4-D tensor map over (64 channels, head, token, 64-channel block) of strided bf16 query rows: one box = 64 channels of
 // box_heads heads of box_tokens tokens, in shared memory as [token][head][64 channels] with the 128-byte swizzle.
 bool make_q_tensor_map(CUtensorMap *map, const void *base, int d, int H, long long T, long long sh, long long st, int box_heads,

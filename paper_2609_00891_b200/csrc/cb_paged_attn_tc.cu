@@ -26,9 +26,9 @@
 // prompt measured.  16 requests of 2 to 16 rows over 8,192 keys 109 - 144 us (4.9 - 3.7 TB/s), by rows and page size.
 //
 // The same kernel reads a cache held in 8 bits (FMT is its format; BF16_PAGES is this file's head): the copying and clearing warps give
-// way to four that convert.  Each copies the codes of 32 keys of a tile, one tile ahead of the conversion (cp.async into 32 KB beside
-// the tiles; every thread reads back its own 16 bytes, so nothing waits), and writes them as bf16 numbers code * 2^e, which are exact,
-// where the products take them from; everything after that is as above.
+// way to four that convert.  The producer copies the codes of a tile's K and V (TMA, two tiles ahead of the products at most), and their
+// exponents beside them; the converting warps write them as bf16 numbers code * 2^e, which are exact, where the products take them
+// from; everything after that is as above.
 #include <type_traits>
 
 #include "cb_paged.cuh"
@@ -69,7 +69,7 @@ struct TcAttnParams {
     int q_bytes;                                            // of one 64-channel block of a Q tile
 };
 struct TcAttn8Params {
-    CUtensorMap q;
+    CUtensorMap q, k, v;
     Pool8 p;
     PagedArgs a;
     int q_bytes;
@@ -116,18 +116,16 @@ struct ToBf16 {
     {
         float a, b;
         if (FMT == CACHE_E4M3) {
-            uint16_t x0, x1;
-            asm("{\n\t.reg .b16 lo, hi;\n\t.reg .b32 x;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 x, %3;\n\tmov.b32 {%0, %1}, x;\n\t}"
-                : "=h"(x0), "=h"(x1) : "r"(w), "h"((uint16_t)(upper ? w >> 16 : w)));
-            if (FAR) {
-                asm("cvt.f32.f16 %0, %1;" : "=f"(a) : "h"(x0));
-                asm("cvt.f32.f16 %0, %1;" : "=f"(b) : "h"(x1));
-                a *= s;
-                b *= s;
-            } else {
-                asm("fma.rn.f32.f16 %0, %1, %2, %3;" : "=f"(a) : "h"(x0), "h"(h), "f"(0.f));
-                asm("fma.rn.f32.f16 %0, %1, %2, %3;" : "=f"(b) : "h"(x1), "h"(h), "f"(0.f));
+            if (!FAR) {
+                uint32_t r;
+                asm("{\n\t.reg .b16 x0, x1;\n\t.reg .b32 x;\n\t.reg .f32 a, b;\n\tcvt.rn.f16x2.e4m3x2 x, %1;\n\tmov.b32 {x0, x1}, x;\n\t"
+                    "fma.rn.f32.f16 a, x0, %2, 0f00000000;\n\tfma.rn.f32.f16 b, x1, %2, 0f00000000;\n\tcvt.rn.bf16x2.f32 %0, b, a;\n\t}"
+                    : "=r"(r) : "h"((uint16_t)(upper ? w >> 16 : w)), "h"(h));
+                return r;
             }
+            const float4 z = codes_to_f32<CACHE_E4M3>(upper ? w >> 16 : w, s);
+            a = z.x;
+            b = z.y;
         } else {
             // 2^23 + (code + 128) has the code in its low bits
             const uint32_t t = w ^ 0x80808080u;
@@ -139,8 +137,8 @@ struct ToBf16 {
 };
 
 template <int D, int FMT>
-__device__ __forceinline__ void tc_convert(const PagedArgs &a, const Pool8 &p, const PaShare &share, uint8_t *kv, uint8_t *codes, uint64_t *full,
-                                           uint64_t *empty, volatile int *abort_flag, volatile int *moves)
+__device__ __forceinline__ void tc_convert(const PagedArgs &a, const PaShare &share, uint8_t *kv, const uint8_t *codes, const int8_t *exps,
+                                           uint64_t *full, uint64_t *empty, uint64_t *staged, uint64_t *staged_empty, volatile int *abort_flag)
 {
     using C = TcAttnCfg<D, FMT>;
     const int lane = threadIdx.x & 31, cw = (threadIdx.x >> 5) - 12;
@@ -149,8 +147,6 @@ __device__ __forceinline__ void tc_convert(const PagedArgs &a, const Pool8 &p, c
     // eight lanes take the eight keys of one group, whole rows (D = 128) or two at a time (64)
     constexpr int RI = 128 / D;
     const int row0 = cw * 32 + (lane >> 3) * 8 + (D == 128 ? 0 : (lane >> 2) & 1), piece = D == 128 ? lane & 7 : lane & 3;
-    const int group = cw * 32 + (lane >> 3) * 8;
-    const int slot_mask = (1 << a.page_log2) - 1;
     const uint32_t mine = smem_u32(codes) + row0 * D + piece * 16;
     // where the two halves of a piece go: 64-channel block, then 16-byte columns 2 c and 2 c + 1 of the row, XORed by it.  Pieces of the
     // second block go second half first, so that the eight lanes of a row meet no bank twice.
@@ -158,70 +154,22 @@ __device__ __forceinline__ void tc_convert(const PagedArgs &a, const Pool8 &p, c
     const uint32_t dst = smem_u32(kv) + (piece >> 2) * C::BLK + row0 * 128;
     const int col = (piece & 3) * 2;
 
-    struct Tile { int j0, hi, lo, ex; bool clear; };
-    auto page_of = [&](int j0) {
-        const int key = j0 + group, c = key >> a.page_log2;
-        return pa_wanted(a, w.u, key, 8) && c < a.table_cols ? __ldg(a.table + (long long)w.u.b * a.table_stride + c) : -1;
-    };
-    auto issue = [&](int j0, int page, int slot_of_two) {
-        const unsigned slot = (unsigned)(j0 + group) & slot_mask;
-        const bool there = (unsigned)page < (unsigned)p.n_pages;
-        const uint32_t bytes = there ? 16u : 0u, to = mine + slot_of_two * 2 * C::CODES;
-        unsigned long long from = 0, step = 0;
-        if (there) {
-            from = (unsigned long long)(unsigned)page * (unsigned)p.sp + (unsigned long long)(slot + (row0 - group)) * (unsigned)p.ss;
-            step = (unsigned long long)RI * p.ss;
-        }
-        from += (unsigned long long)w.h * p.sh + piece * 16;
-        const uint8_t *ks = p.k + from, *vs = p.v + from;
-#pragma unroll
-        for (int i = 0; i < 8 / RI; ++i) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + i * RI * D), "l"(ks), "r"(bytes) : "memory");
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + C::CODES + i * RI * D), "l"(vs), "r"(bytes) : "memory");
-            ks += step;
-            vs += step;
-        }
-        Tile t;
-        t.j0 = j0;
-        t.hi = w.u.hi_key;
-        t.lo = w.u.lo_key;
-        t.clear = pa_clears<C::KT>(a, w.u, j0);
-        t.ex = 0;
-        if ((lane & 6) == 0 && there)                      // the first two lanes of eight: K's and V's exponent
-            t.ex = __ldg(((lane & 1) ? p.ve : p.ke) + (long long)w.h * p.eh + ((unsigned long long)(unsigned)page * (unsigned)p.ep +
-                                                                             (unsigned long long)(slot >> p.block_log2) * (unsigned)p.eb));
-        return t;
-    };
     Ring<C::NS> st;
-    int done = 0, t = w.t;
-    Tile here = issue(pa_tile(w.u, t) * C::KT, page_of(pa_tile(w.u, t) * C::KT), 0);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    Ring<2> in;
     bool more = true;
-    for (int n = 0; more; ++n) {
-        // the next tile, of this piece or another
-        if (++t >= w.t1) {
-            more = w.next(a);
-            t = w.t;
-        }
-        const int j0 = more ? pa_tile(w.u, t) * C::KT : 0;
-        const int page = more ? page_of(j0) : -1;
-        Tile next = {};
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
+    while (more) {
+        for (int t = w.t; t < w.t1; ++t) {
+            const int j0 = pa_tile(w.u, t) * C::KT;
+            const bool clears = pa_clears<C::KT>(a, w.u, j0);
+            if (!mbar_wait_suspended_warp(&staged[in.idx], in.phase, abort_flag)) return;
 #pragma unroll
-        for (int comp = 0; comp < 2; ++comp) {
-            if (comp == 0) {
-                if (more) next = issue(j0, page, (n + 1) & 1);
-                asm volatile("cp.async.commit_group;" ::: "memory");
-            }
-            if (!mbar_wait_to_issue_warp(&empty[st.idx], st.phase ^ 1, abort_flag)) {
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
-                return;
-            }
-            const int e = exp8_clamp(__shfl_sync(0xffffffffu, here.ex, (lane & 24) + comp), FMT);
+            for (int comp = 0; comp < 2; ++comp) {
+            if (!mbar_wait_suspended_warp(&empty[st.idx], st.phase ^ 1, abort_flag)) return;
+            const int e = exp8_clamp(exps[in.idx * 32 + comp * 16 + cw * 4 + (lane >> 3)], FMT);
             ToBf16 to;
             const bool far = to.template set<FMT>(e);
-            const uint32_t from = mine + ((n & 1) * 2 + comp) * C::CODES, tile = dst + st.idx * C::TILE;
-            const bool clear = comp && here.clear;
+            const uint32_t from = mine + (in.idx * 2 + comp) * C::CODES, tile = dst + st.idx * C::TILE;
+            const bool clear = comp && clears;
             auto convert = [&](auto any_e) {
                 constexpr bool FAR = decltype(any_e)::value;
 #pragma unroll
@@ -232,9 +180,9 @@ __device__ __forceinline__ void tc_convert(const PagedArgs &a, const Pool8 &p, c
                         asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[k].x), "=r"(x[k].y), "=r"(x[k].z), "=r"(x[k].w) : "r"(from + (i0 + k) * RI * D) : "memory");
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const int i = i0 + k, r = row0 + i * RI, j = here.j0 + r;
+                        const int i = i0 + k, r = row0 + i * RI, j = j0 + r;
                         // rows that no query sees may hold anything: 0 * NaN would reach the output
-                        if (clear && !(j < here.hi && (j >= here.lo || j < a.n_sink))) x[k] = make_uint4(0, 0, 0, 0);
+                        if (clear && !(j < w.u.hi_key && (j >= w.u.lo_key || j < a.n_sink))) x[k] = make_uint4(0, 0, 0, 0);
                         const uint32_t w0 = swap ? x[k].z : x[k].x, w1 = swap ? x[k].w : x[k].y, w2 = swap ? x[k].x : x[k].z, w3 = swap ? x[k].y : x[k].w;
                         const uint4 y = make_uint4(to.template pair<FMT, FAR>(w0, 0), to.template pair<FMT, FAR>(w0, 1), to.template pair<FMT, FAR>(w1, 0), to.template pair<FMT, FAR>(w1, 1));
                         const uint4 z = make_uint4(to.template pair<FMT, FAR>(w2, 0), to.template pair<FMT, FAR>(w2, 1), to.template pair<FMT, FAR>(w3, 0), to.template pair<FMT, FAR>(w3, 1));
@@ -250,11 +198,13 @@ __device__ __forceinline__ void tc_convert(const PagedArgs &a, const Pool8 &p, c
             __syncwarp();
             if (lane == 0) {
                 mbar_arrive(&full[st.idx]);
-                if (cw == 0) *moves = ++done;
+                if (comp) mbar_arrive(&staged_empty[in.idx]);
             }
             st.next();
+            }
+            in.next();
         }
-        here = next;
+        more = w.next(a);
     }
 }
 
@@ -277,7 +227,8 @@ __global__ void __launch_bounds__(TcAttnCfg<D, FMT>::THREADS, 1) k_paged_attn_tc
     uint64_t *p_ready = s_full + 2;        // [2][2] weights of the first keys and of the rest written (4 warps)
     uint64_t *o_full = p_ready + 4;        // [2] last product with V of a piece complete
     uint64_t *landed = o_full + 2;         // [NS] a V tile that has rows to clear: copied
-    uint64_t *drain = landed + C::NS;
+    [[maybe_unused]] uint64_t *staged_empty = landed + C::NS;      // [2] 8 bits: codes of a tile converted (4 warps); landed[2]: copied
+    uint64_t *drain = staged_empty + 2;
     PaSum *warp_sums = reinterpret_cast<PaSum *>(((uintptr_t)(drain + 1) + 15) & ~(uintptr_t)15);
     PaShare *share = reinterpret_cast<PaShare *>(warp_sums + C::THREADS / 32);
     using Walk = PaWalk<C::ROWS, C::KT>;
@@ -288,14 +239,16 @@ __global__ void __launch_bounds__(TcAttnCfg<D, FMT>::THREADS, 1) k_paged_attn_tc
     // last copy went to `landed`, and the parity of its next phase there; copies of each query tile.
     struct Flight { int issued; uint32_t on_landed, landings, n_query[2]; };
     Flight *flight = reinterpret_cast<Flight *>(tmem_slot + 3);
+    [[maybe_unused]] int8_t *exps = reinterpret_cast<int8_t *>(flight + 1);      // [2][K, V][16 groups of 8 keys]
     volatile int *moves = &flight->issued;                  // counted up per stage, for the waits that outlast many tiles
 
     const PagedArgs &a = P.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 256) {
-        for (int i = 0; i < C::NS; ++i) { mbar_init(&full[i], C::EIGHT ? 4 : 1); mbar_init(&empty[i], 1); mbar_init(&landed[i], 1); }
+        for (int i = 0; i < C::NS; ++i) { mbar_init(&full[i], C::EIGHT ? 4 : 1); mbar_init(&empty[i], 1); mbar_init(&landed[i], C::EIGHT ? 2 : 1); }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&q_full[i], 1);
+            mbar_init(&staged_empty[i], 4);
             mbar_init(&q_empty[i], 1);
             mbar_init(&info_full[i], 1);
             mbar_init(&info_empty[i], 8);
@@ -310,10 +263,8 @@ __global__ void __launch_bounds__(TcAttnCfg<D, FMT>::THREADS, 1) k_paged_attn_tc
         *flight = Flight{};
         mbar_fence_init();
         tma_prefetch_desc(&P.q);
-        if constexpr (!C::EIGHT) {
-            tma_prefetch_desc(&P.k);
-            tma_prefetch_desc(&P.v);
-        }
+        tma_prefetch_desc(&P.k);
+        tma_prefetch_desc(&P.v);
     }
     if (warp == 9) tmem_alloc(tmem_slot, C::TMEM_COLS);
     tc_fence_before();
@@ -330,15 +281,62 @@ __global__ void __launch_bounds__(TcAttnCfg<D, FMT>::THREADS, 1) k_paged_attn_tc
     if (C::EIGHT && warp >= 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_CONVERT));
         if constexpr (C::EIGHT)
-            if (any && !a.starve) tc_convert<D, FMT>(a, P.p, *share, kv, codes, full, empty, abort_flag, moves);
+            if (any) tc_convert<D, FMT>(a, *share, kv, codes, exps, full, empty, landed, staged_empty, abort_flag);
     } else if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_BESIDE));
     Walk w;
     if (any) w.open(a, *share);
     if (warp == 8) {
         // ================================ producer ================================
-        if constexpr (!C::EIGHT)
-        if (any && !a.starve) {
+        if constexpr (C::EIGHT) {
+            if (any && !a.starve) {
+                Ring<2> st;
+                int issued = 0;
+                const int n_page = 1 << (7 - box_log2);                      // boxes of a tile's K, and of its V
+                const bool has_box = lane < 2 * n_page;
+                const int comp = lane >= n_page, i = lane - comp * n_page;
+                // the lane that looks up the page of keys 8 (lane & 15) on of the tile, whose exponent this lane has
+                const int looks = (lane >> 4) * n_page + ((lane & 15) >> (box_log2 - 3));
+                const Pool8 &p = P.p;
+                bool more = true;
+                int t = w.t;
+                auto page_of = [&]() {                                       // of this lane's box
+                    const int key = pa_tile(w.u, t) * C::KT + (i << box_log2);
+                    const int c = key >> a.page_log2;
+                    int page = a.n_pages;                                    // outside the pool: the copy writes zeros
+                    if (more && has_box && pa_wanted(a, w.u, key, 1 << box_log2) && c < a.table_cols) page = __ldg(a.table + (long long)w.u.b * a.table_stride + c);
+                    return page;
+                };
+                int page = page_of();
+                while (more) {
+                    const int h = w.h, key = pa_tile(w.u, t) * C::KT;
+                    if (!mbar_wait_to_issue_warp(&staged_empty[st.idx], st.phase ^ 1, abort_flag)) { dead = true; break; }
+                    if (lane == 0) mbar_arrive_expect_tx(&landed[st.idx], 2 * C::CODES);
+                    __syncwarp();
+                    if (has_box)
+                        tma_load_4d(codes + (st.idx * 2 + comp) * C::CODES + ((size_t)i << box_log2) * D, comp ? &P.v : &P.k, &landed[st.idx], 0,
+                                    (key + (i << box_log2)) & ((1 << a.page_log2) - 1), h, page);
+                    const int page_e = __shfl_sync(0xffffffffu, page, looks);
+                    const unsigned slot = (unsigned)(key + (lane & 15) * 8) & ((1u << a.page_log2) - 1u);
+                    int e = 0;                                               // of a block that nobody sees it may be anything
+                    if ((unsigned)page_e < (unsigned)p.n_pages && pa_wanted(a, w.u, key + (lane & 15) * 8, 8))
+                        e = __ldg((lane < 16 ? p.ke : p.ve) + (long long)h * p.eh + ((unsigned long long)(unsigned)page_e * (unsigned)p.ep +
+                                                                                    (unsigned long long)(slot >> p.block_log2) * (unsigned)p.eb));
+                    if (++t >= w.t1) {
+                        more = w.next(a);
+                        t = w.t;
+                    }
+                    page = page_of();
+                    exps[st.idx * 32 + lane] = (int8_t)e;
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(&landed[st.idx]);
+                        *moves = ++issued;
+                    }
+                    st.next();
+                }
+            }
+        } else if (any && !a.starve) {
             Ring<C::NS> st;
             int issued = 0;
             uint32_t on_landed = 0, landings = 0;
@@ -790,6 +788,7 @@ __global__ void __launch_bounds__(TcAttnCfg<D, FMT>::THREADS, 1) k_paged_attn_tc
         // copies in flight land before the block ends
         if (warp == 9) {
             const Flight f = *flight;
+            for (int k = 0; C::EIGHT && k < min(f.issued, 2); ++k) mbar_drain(&landed[k], ((f.issued - k - 1) / 2) & 1);
             for (int k = 0; k < (C::EIGHT ? 0 : min(f.issued, C::NS)); ++k) {
                 if (f.on_landed >> k & 1) mbar_drain(&landed[k], (f.landings >> k & 1) ^ 1);
                 else mbar_drain(&full[k], ((f.issued - k - 1) / C::NS) & 1);
@@ -843,7 +842,11 @@ cudaError_t launch_paged8_attn_tc(const PagedArgs &a, const Pool8 &pool, cudaStr
     TcAttn8Params P;
     P.a = a;
     P.p = pool;
-    if (!query_map(&P.q, &P.q_bytes, a, pool.d)) return cudaErrorInvalidValue;
+    const int page_size = 1 << pool.page_log2, box = page_size < 128 ? page_size : 128;
+    if (!query_map(&P.q, &P.q_bytes, a, pool.d) ||
+        !make_code_tensor_map(&P.k, pool.k, pool.d, pool.H, page_size, pool.n_pages, pool.sh, pool.ss, pool.sp, box) ||
+        !make_code_tensor_map(&P.v, pool.v, pool.d, pool.H, page_size, pool.n_pages, pool.sh, pool.ss, pool.sp, box))
+        return cudaErrorInvalidValue;
     const bool e4m3 = pool.format == CACHE_E4M3;
     if (pool.d == 128) return e4m3 ? launch_tc_attn<128, CACHE_E4M3>(P, st) : launch_tc_attn<128, CACHE_INT8>(P, st);
     return e4m3 ? launch_tc_attn<64, CACHE_E4M3>(P, st) : launch_tc_attn<64, CACHE_INT8>(P, st);
