@@ -595,8 +595,9 @@ cb_status cb_paged_load8(const cb_page_pool8 *pool, void *dst_k, void *dst_v, in
                          int64_t stride_layer, int64_t stride_token, int64_t stride_head, const int64_t *slot_map, void *stream);
 
 /*
- * cb_paged_attention over a pool of 8 bits: the same arguments, rows, masks, splits, and promises (and the same test hooks
- * and device status), with its own workspace size.  Codes become 16-bit numbers exactly.  Weights are rounded to fp16
+ * cb_paged_attention over a pool of 8 bits: the same arguments, rows, masks, splits and promises, with its own workspace
+ * size.  (Device-side time-outs and the test hooks concern the kernel for many rows; the one for few rows has no wait that
+ * could run out.)  Codes become 16-bit numbers exactly.  Weights are rounded to fp16
  * (2^-11 of each that is above 2^-16 of the largest) or bf16 (2^-8), as max_new chooses between kernels.  Rows of a page
  * that no row of the request sees may hold anything, and so may the exponents of blocks without a seen row; values that
  * some row sees must be finite and below 2^90.

@@ -458,6 +458,97 @@ def test_attention_repeats_its_bits_on_streams_and_in_graphs(kind, new):
         assert torch.equal(out, _attend(q, pool, table, cu, [t - shrink for t in total]))
 
 
+# ---------------------------------------------------------------------------------------------------- sizes, batches, waits
+@KINDS
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page,block", [(8, 8), (16, 8), (32, 32), (64, 16), (128, 8), (128, 128), (256, 64), (256, 256)])
+def test_attention_over_every_page_size(kind, d, page, block):
+    """Decode and chunks, with and without a window, one slot of the last page used and all of them."""
+    for new, total in (([1, 1, 2], [page, page + 1, 5 * page - 1]), ([70, 33], [3 * page + 70, 300])):
+        b = _batch(kind, new, total, 2, 4, d, page, block, hnd=page >= 64, pad_rows=1, seed=page + block)
+        _compare(*b)
+        _compare(*b, window=page + 3, n_sink=5)
+
+
+@KINDS
+@pytest.mark.parametrize("new", [[1] * 6, [40, 1, 7, 100, 2, 33]])
+def test_attention_of_the_later_requests_of_a_batch_by_themselves(kind, new):
+    """Slices of a batch's tables: rows are counted from the batch's first, so q and out are the whole batch's."""
+    total = [n + 50 * i for i, n in enumerate(new)]
+    q, pool, table, cu, total = _batch(kind, new, total, 2, 4, 128, 16, 16)
+    want = _attend(q, pool, table, cu, total)
+    k, v = _plain(pool, 0)
+    ref_out, tol = ref.attention(q, k, v, table, cu, total, 128 ** -0.5, weight=2.0 ** -8)
+    for first in (2, 5):
+        out = torch.full_like(want, 5.0)
+        cb.cb_paged_attention8(q, out, pool, 0, table[first:], _i32(cu)[first:].contiguous(), _i32(total)[first:], 128 ** -0.5, _workspace(128),
+                               max_new=max(new[first:]))
+        assert (out[:cu[first]] == 5).all()
+        assert ((out[cu[first]:].double() - ref_out[cu[first]:]).abs() <= tol[cu[first]:]).all()
+
+
+@KINDS
+@pytest.mark.parametrize("seed", range(12))
+def test_attention_of_random_shapes(kind, seed):
+    rng = np.random.default_rng(seed)
+    page = int(rng.choice([8, 16, 32, 64, 128, 256]))
+    block = int(rng.choice([b for b in (8, 16, 32, 64, 128, 256) if b <= page]))
+    n = int(rng.integers(1, 9))
+    new = rng.integers(0, rng.choice([2, 5, 40, 300]), n).tolist()
+    total = [x + int(rng.integers(0, 700)) for x in new]
+    window, n_sink = (0, 0) if rng.random() < 0.5 else (int(rng.integers(1, 400)), int(rng.integers(0, 140)))
+    b = _batch(kind, new, total, int(rng.integers(1, 5)), int(rng.choice([1, 2, 3, 5, 8, 12])), int(rng.choice([64, 128])), page, block,
+               hnd=bool(rng.random() < 0.5), pad_rows=int(rng.integers(0, 4)), seed=seed, grow=2.0)
+    if b[0].shape[0]:
+        _compare(*b, window=window, n_sink=n_sink, max_new=int(rng.choice([0, max(new + [1])])))
+
+
+@KINDS
+@pytest.mark.parametrize("seed", range(12))
+def test_store_of_random_shapes(kind, seed):
+    """Several calls of a ragged batch: some requests go on inside a block, some begin, some write their last rows again."""
+    rng = np.random.default_rng(seed)
+    page = int(rng.choice([8, 16, 32, 64, 128, 256]))
+    block = int(rng.choice([b for b in (8, 16, 32, 64, 128, 256) if b <= page]))
+    n, L, H, d = int(rng.integers(1, 6)), int(rng.integers(1, 4)), int(rng.integers(1, 11)), int(rng.choice([64, 128]))
+    dtype = [torch.bfloat16, torch.float32][seed % 2]
+    length = rng.integers(1, 300, n)
+    pages = [-(-int(x) // page) for x in length]
+    order = rng.permutation(sum(pages) + 2)
+    own = np.split(order[:sum(pages)], np.cumsum(pages)[:-1])
+    pool = _pool(kind, L, sum(pages) + 2, page, block, H, d, hnd=bool(rng.random() < 0.5), seed=seed)
+    state = _state(pool)
+    at = [0] * n
+    for call in range(4):
+        slot = []
+        for b in range(n):
+            first = max(0, at[b] - int(rng.integers(0, 3))) if call else 0
+            last = int(length[b]) if call == 3 else min(int(length[b]), at[b] + int(rng.integers(0, 120)))
+            slot += [int(own[b][t // page]) * page + t % page for t in range(first, last)] + [-1] * int(rng.integers(0, 3))
+            at[b] = max(at[b], last)
+        if slot:
+            _store(pool, state, _rows(L, len(slot), H, d, dtype, 100 * seed + call, spread=2.0), slot)
+
+
+@KINDS
+@pytest.mark.parametrize("new,total,d,page,window", [([70, 9], [3000, 700], 128, 16, 0), ([300], [9000], 128, 128, 0), ([300, 40], [5000, 40], 64, 8, 1000)])
+def test_attention_waits_that_run_out(kind, new, total, d, page, window):
+    """Nothing copied, or consumers that give up while copies are in flight: the status says so, and the next call is right."""
+    b = _batch(kind, new, total, 2, 8, d, page, 8)
+    want = _compare(*b, window=window, n_sink=2)
+    try:
+        for hook in (dict(starve_producer=True), dict(consumers_give_up=True)):
+            cb.cb_test_hooks(poll_limit=2000, **hook)
+            _attend(*b, window=window, n_sink=2)
+            with pytest.raises(cb.CbError) as e:
+                cb.cb_last_device_status()
+            assert e.value.status == cb.CB_ERR_TIMEOUT
+            cb.cb_test_hooks()
+            assert torch.equal(_compare(*b, window=window, n_sink=2), want)
+    finally:
+        cb.cb_test_hooks()
+
+
 # ---------------------------------------------------------------------------------------------------- together
 @KINDS
 def test_a_served_target_cache(kind):
