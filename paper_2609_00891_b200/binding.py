@@ -749,17 +749,21 @@ def cb_paged_attention_workspace_bytes(head_dim: int) -> int:
     return n.value
 
 
-def _attention_call(q, out, pool, layer, block_table, cu_new, total_len, scale, workspace, max_new, window, n_sink, stream) -> tuple:
-    T, Hq, d = q.shape
-    qs, os_ = q.stride(), out.stride()
-    assert q.dtype == torch.bfloat16 and out.dtype == torch.bfloat16 and q.shape == out.shape and qs[2] == 1 and os_[2] == 1
+def _attention_call(call, name, q, out, pool, layer, block_table, cu_new, total_len, scale, workspace, max_new, window, n_sink, stream) -> None:
+    shape, qs, os_ = q.shape, q.stride(), out.stride()
+    T, Hq, d = shape
     B, cols = block_table.shape
-    assert d == pool.head_dim and block_table.dtype == cu_new.dtype == total_len.dtype == torch.int32
-    assert (cols <= 1 or block_table.stride(1) == 1) and cu_new.is_contiguous() and total_len.is_contiguous()
-    assert cu_new.numel() == B + 1 and total_len.numel() == B and workspace.dtype == torch.uint8 and workspace.is_contiguous()
+    bf16, i32, u8 = torch.bfloat16, torch.int32, torch.uint8
+    row, column = block_table.stride()
+    assert q.dtype is bf16 and out.dtype is bf16 and shape == out.shape and qs[2] == 1 and os_[2] == 1 and d == pool.head_dim
+    assert block_table.dtype is i32 and cu_new.dtype is i32 and total_len.dtype is i32 and workspace.dtype is u8
+    assert (cols <= 1 or column == 1) and cu_new.is_contiguous() and total_len.is_contiguous() and workspace.is_contiguous()
+    assert cu_new.numel() == B + 1 and total_len.numel() == B
     st = _on_one_device(stream, q, out, pool.k, block_table, cu_new, total_len, workspace)
-    return (pool.c, layer, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1], T, Hq, block_table.data_ptr(), block_table.stride(0), cols,
-            cu_new.data_ptr(), total_len.data_ptr(), B, max_new, scale, window, n_sink, workspace.data_ptr(), workspace.numel(), st)
+    status = call(pool.c, layer, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1], T, Hq, block_table.data_ptr(), row, cols,
+                  cu_new.data_ptr(), total_len.data_ptr(), B, max_new, scale, window, n_sink, workspace.data_ptr(), workspace.numel(), st)
+    if status:
+        _check(status, name)
 
 
 def cb_paged_attention(q: torch.Tensor, out: torch.Tensor, pool: PagePool, layer: int, block_table: torch.Tensor,
@@ -767,8 +771,8 @@ def cb_paged_attention(q: torch.Tensor, out: torch.Tensor, pool: PagePool, layer
                        max_new: int = 0, window: int = 0, n_sink: int = 0, stream=None) -> None:
     """Attention of new rows q [T][Hq][d] (bf16) over layer `layer` of the pool; block_table [B][max_pages], cu_new [B + 1],
     total_len [B] as cb_page_tables leaves them; workspace: uint8, zero-filled once (torch.zeros)."""
-    _check(lib().cb_paged_attention(*_attention_call(q, out, pool, layer, block_table, cu_new, total_len, scale, workspace, max_new, window,
-                                                     n_sink, stream)), "cb_paged_attention")
+    _attention_call((_lib or lib()).cb_paged_attention, "cb_paged_attention", q, out, pool, layer, block_table, cu_new, total_len, scale,
+                    workspace, max_new, window, n_sink, stream)
 
 
 class _PagePool8(ctypes.Structure):
@@ -782,6 +786,7 @@ class _PagePool8(ctypes.Structure):
 
 
 _PAGE_POOL8 = struct.Struct("PPPPiiiiiiqqqqqqqqq")
+_CODES = {torch.float8_e4m3fn: CB_CACHE_E4M3, torch.int8: CB_CACHE_INT8}
 
 
 class PagePool8:
@@ -791,40 +796,42 @@ class PagePool8:
     __slots__ = ("k", "v", "k_exp", "v_exp", "n_layers", "n_heads", "head_dim", "page_size", "n_pages", "block", "c")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor):
-        strides, shape, exps, code = k.stride(), k.shape, k_exp.stride(), k.dtype
-        sl, sp, ss, sh, sc = strides
+        shape, strides, code, blocks, exps = k.shape, k.stride(), k.dtype, k_exp.shape, k_exp.stride()
         L, N, S, H, d = shape
-        n = k_exp.shape[2]
-        assert (code is torch.float8_e4m3fn or code is torch.int8) and v.dtype is code and v.shape == shape and v.stride() == strides and sc == 1
-        assert k_exp.dtype is torch.int8 and v_exp.dtype is torch.int8 and k_exp.shape == (L, N, n, H) == v_exp.shape and exps == v_exp.stride()
-        assert n > 0 and S % n == 0
+        sl, sp, ss, sh, sc = strides
+        n = blocks[2]
+        assert v.dtype is code and v.shape == shape and v.stride() == strides and sc == 1 and code in _CODES
+        assert k_exp.dtype is torch.int8 and v_exp.dtype is torch.int8 and blocks == v_exp.shape and exps == v_exp.stride()
+        assert blocks == (L, N, n, H) and n > 0 and S % n == 0
         dev = k.get_device()
-        assert dev == v.get_device() == k_exp.get_device() == v_exp.get_device()
+        assert dev == v.get_device() and dev == k_exp.get_device() and dev == v_exp.get_device()
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.n_layers, self.n_pages, self.page_size, self.n_heads, self.head_dim, self.block = L, N, S, H, d, S // n
-        self.c = _PAGE_POOL8.pack(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), L, H, d, S,
-                                  CB_CACHE_INT8 if code is torch.int8 else CB_CACHE_E4M3, S // n, N, sl, sp, ss, sh, *exps)
+        self.c = _PAGE_POOL8.pack(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), L, H, d, S, _CODES[code], S // n, N,
+                                  sl, sp, ss, sh, *exps)
 
 
-def _rows8(pool: PagePool8, k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, stream) -> tuple:
-    L, T, H, d = k.shape
-    ss = k.stride()
-    assert k.dtype == v.dtype and k.shape == v.shape and ss == v.stride() and ss[3] == 1
+def _rows8(call, name, pool: PagePool8, k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, stream) -> None:
+    shape, ss, kind = k.shape, k.stride(), k.dtype
+    L, T, H, d = shape
+    assert v.dtype is kind and shape == v.shape and ss == v.stride() and ss[3] == 1
     assert L == pool.n_layers and H == pool.n_heads and d == pool.head_dim
-    assert slot_map.dtype == torch.int64 and slot_map.is_contiguous() and slot_map.numel() == T
-    dt = CB_DTYPE_BF16 if k.dtype == torch.bfloat16 else {torch.float32: CB_DTYPE_F32}[k.dtype]
+    assert slot_map.dtype is torch.int64 and slot_map.is_contiguous() and slot_map.numel() == T
+    dt = CB_DTYPE_BF16 if kind is torch.bfloat16 else {torch.float32: CB_DTYPE_F32}[kind]
     st = _on_one_device(stream, pool.k, k, v, slot_map)
-    return pool.c, k.data_ptr(), v.data_ptr(), dt, T, ss[0], ss[1], ss[2], slot_map.data_ptr(), st
+    status = call(pool.c, k.data_ptr(), v.data_ptr(), dt, T, ss[0], ss[1], ss[2], slot_map.data_ptr(), st)
+    if status:
+        _check(status, name)
 
 
 def cb_paged_store8(pool: PagePool8, src_k: torch.Tensor, src_v: torch.Tensor, slot_map: torch.Tensor, stream=None) -> None:
     """Rows [L][T][H][d] (bf16 or fp32) of all layers, quantised into the slots slot_map [T] (int64, -1: skipped)."""
-    _check(lib().cb_paged_store8(*_rows8(pool, src_k, src_v, slot_map, stream)), "cb_paged_store8")
+    _rows8((_lib or lib()).cb_paged_store8, "cb_paged_store8", pool, src_k, src_v, slot_map, stream)
 
 
 def cb_paged_load8(pool: PagePool8, dst_k: torch.Tensor, dst_v: torch.Tensor, slot_map: torch.Tensor, stream=None) -> None:
     """The rows at slots slot_map [T] (int64, -1: the row is left as it is) of all layers into dst [L][T][H][d] (bf16 or fp32)."""
-    _check(lib().cb_paged_load8(*_rows8(pool, dst_k, dst_v, slot_map, stream)), "cb_paged_load8")
+    _rows8((_lib or lib()).cb_paged_load8, "cb_paged_load8", pool, dst_k, dst_v, slot_map, stream)
 
 
 def cb_paged_attention8_workspace_bytes(head_dim: int) -> int:
@@ -837,8 +844,8 @@ def cb_paged_attention8(q: torch.Tensor, out: torch.Tensor, pool: PagePool8, lay
                         cu_new: torch.Tensor, total_len: torch.Tensor, scale: float, workspace: torch.Tensor,
                         max_new: int = 0, window: int = 0, n_sink: int = 0, stream=None) -> None:
     """As cb_paged_attention, over layer `layer` of a pool of 8 bits."""
-    _check(lib().cb_paged_attention8(*_attention_call(q, out, pool, layer, block_table, cu_new, total_len, scale, workspace, max_new, window,
-                                                      n_sink, stream)), "cb_paged_attention8")
+    _attention_call((_lib or lib()).cb_paged_attention8, "cb_paged_attention8", q, out, pool, layer, block_table, cu_new, total_len, scale,
+                    workspace, max_new, window, n_sink, stream)
 
 
 def cb_device_status(ctx: Context, stream=None) -> None:

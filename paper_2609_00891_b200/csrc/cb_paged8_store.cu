@@ -1,5 +1,7 @@
 // Rows into the pages of a cache held in 8 bits, and back.  Both are bound by HBM: every row is read once and written once,
 // in 3 bytes a value (bf16) or 5 (fp32).
+#include <type_traits>
+
 #include "cb_paged8.cuh"
 #include "cb_math.cuh"
 
@@ -75,11 +77,11 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
             last = other ? -1 : row + 31 - __clz(m);
             return m;
         };
-        auto load = [&](long long row, unsigned m, int k0, auto &x) {
+        auto load = [&](long long row, unsigned m, int k0, auto &x, auto count) {
             const char *at = src + (row + k0 + sub) * row_bytes;
             m >>= k0 + sub;
 #pragma unroll
-            for (int i = 0; i < (int)(sizeof(x) / sizeof(x[0])); ++i, at += RPI * row_bytes) {
+            for (int i = 0; i < decltype(count)::value; ++i, at += RPI * row_bytes) {
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
                     x[i][w] = make_uint4(0, 0, 0, 0);
@@ -102,9 +104,9 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
         };
         float most = 0.f, finite = 0.f;                                    // finite: not 0 once a value was infinite or NaN
         bool begun = false;                                                // the block's first row is among the run's
-        auto largest = [&](const auto &x) {
+        auto largest = [&](const auto &x, auto count) {
 #pragma unroll
-            for (int i = 0; i < (int)(sizeof(x) / sizeof(x[0])); ++i) {
+            for (int i = 0; i < decltype(count)::value; ++i) {
                 float f[8];
                 values(x[i], f);
 #pragma unroll
@@ -134,22 +136,30 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
         unsigned kept = 0;                                                 // the kept chunk's rows
         long long kept_slot = -1, kept_row = -1;
         int kept_k0 = 0;
-        bool others = false;
+        bool others = false, few = false;
+        const std::integral_constant<int, ITER> all;
+        const std::integral_constant<int, PART> part;
         chunks([&](long long row, unsigned m, int k0) {
             if (kept_row < 0) {
                 kept = m;
                 kept_k0 = k0;
                 kept_row = row;
                 kept_slot = slot;
-                load(row, m, k0, keep);
-                largest(keep);
+                few = (m >> k0) >> (PART * RPI - 1) <= 1u;                 // a step's single row, for one
+                if (few) {
+                    load(row, m, k0, keep, part);
+                    largest(keep, part);
+                } else {
+                    load(row, m, k0, keep, all);
+                    largest(keep, all);
+                }
             } else {
                 others = true;
 #pragma unroll 1
                 for (int k = k0; k < k0 + CHUNK; k += PART * RPI) {
                     uint4 x[PART][W];
-                    load(row, m, k, x);
-                    largest(x);
+                    load(row, m, k, x, part);
+                    largest(x, part);
                 }
             }
         });
@@ -179,9 +189,9 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
         // ---- codes ----
         const float f = exp2_whole(-e);
         const bool plain = FMT == CACHE_INT8 && __all_sync(0xffffffffu, finite == 0.f && e < exp8_most(FMT));      // all are within the codes' range
-        auto write = [&](const auto &x, unsigned m, int k0, long long slots) {
+        auto write = [&](const auto &x, unsigned m, int k0, long long slots, auto count) {
 #pragma unroll
-            for (int i = 0; i < (int)(sizeof(x) / sizeof(x[0])); ++i) {
+            for (int i = 0; i < decltype(count)::value; ++i) {
                 const int k = k0 + i * RPI + sub;
                 const int to = __shfl_sync(0xffffffffu, (int)slots & slot_mask, k);
                 if (m >> k & 1) {
@@ -203,15 +213,16 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
                 }
             }
         };
-        if (kept) write(keep, kept, kept_k0, kept_slot);
+        if (kept && few) write(keep, kept, kept_k0, kept_slot, part);
+        else if (kept) write(keep, kept, kept_k0, kept_slot, all);
         if (others)
             chunks([&](long long row, unsigned m, int k0) {
                 if (row == kept_row && k0 == kept_k0) return;
 #pragma unroll 1
                 for (int k = k0; k < k0 + CHUNK; k += PART * RPI) {
                     uint4 x[PART][W];
-                    load(row, m, k, x);
-                    write(x, m, k, slot);
+                    load(row, m, k, x, part);
+                    write(x, m, k, slot, part);
                 }
             });
         if (a.team > 1) __syncthreads(); else __syncwarp();                // the block's run before this one's is no longer looked at
