@@ -33,10 +33,10 @@ struct Few8Cfg {
     static constexpr int KT = 128;                     // keys of a tile, 32 for each warp
     static constexpr int HALF = 32 * D;                // bytes of a step's K (or V)
     static constexpr int STAGE = 2 * HALF;
-    static constexpr int RING = 2 * STAGE;             // of a warp; holds its output at the end of a piece
+    static constexpr int RING = 2 * STAGE;             // of a warp; a stage holds its output at the end of a piece
     static constexpr int REC = ROWS * (D + 2);         // floats of a partial record: output rows, maxima, sums
-    static constexpr int BLOCKS = D == 128 ? 4 - NT : 5 - NT;      // of an SM, by registers
-    static_assert(RING >= ROWS * D * 4, "the warp's output must fit its stages");
+    static constexpr int BLOCKS = D == 128 ? 4 - NT : 3;           // of an SM, by registers
+    static_assert(STAGE >= ROWS * D * 4, "the warp's output must fit a stage");
     static constexpr size_t SMEM = 4 * RING;
 };
 
@@ -130,47 +130,54 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
     constexpr int RI = 128 / D;                        // rows of a group that one copy of the warp brings
     const int group8 = (lane >> 3) * 8, crow = D == 128 ? 0 : (lane >> 2) & 1, cpiece = D == 128 ? lane & 7 : lane & 3;
     const int slot_mask = (1 << a.page_log2) - 1;
-    bool more = true;
-    while (more) {
-        const PaUnit &u = w.u;
-        const int n = w.t1 - w.t;
-        const int *row = a.table + (long long)u.b * a.table_stride;
-        const uint8_t *kb = p.k + (long long)w.h * p.sh + crow * p.ss + cpiece * 16, *vb = p.v + (long long)w.h * p.sh + crow * p.ss + cpiece * 16;
-        const int8_t *eb = ((lane & 1) ? p.ve : p.ke) + (long long)w.h * p.eh;    // the first two lanes of eight: K's and V's exponent
+    const PaUnit &u = w.u;                             // of the piece whose codes are copied
+    int n = 0, odd = 0;                                // its steps, and the stage of the first
+    const int *row = nullptr;
+    const uint8_t *kb = nullptr, *vb = nullptr;
+    const int8_t *eb = nullptr;
 
-        // first key of this lane's group in step s, and its page; outside the pool where no key is wanted
-        auto key_of = [&](int s) { return pa_tile(u, w.t + s) * C::KT + warp * 32 + group8; };
-        auto page_of = [&](int s) {
-            int page = -1;
-            if (s < n) {
-                const int key = key_of(s), col = key >> a.page_log2;
-                if (pa_wanted(a, u, key, 8) && col < a.table_cols) page = __ldg(row + col);
-            }
-            return page;
-        };
-        auto issue = [&](int s, int page, int &ex) {
-            const unsigned slot = (unsigned)key_of(s) & slot_mask;
-            const bool there = (unsigned)page < (unsigned)p.n_pages;
-            const uint32_t to = ring_u + (s & 1) * C::STAGE, bytes = there ? 16u : 0u;
-            const unsigned long long from = there ? (unsigned long long)(unsigned)page * (unsigned)p.sp + (unsigned long long)slot * (unsigned)p.ss : 0ull;
-            const unsigned step = there ? (unsigned)p.ss : 0u;
-            const uint8_t *ks = kb + from, *vs = vb + from;
+    // first key of this lane's group in step s, and its page; outside the pool where no key is wanted
+    auto key_of = [&](int s) { return pa_tile(u, w.t + s) * C::KT + warp * 32 + group8; };
+    auto page_of = [&](int s) {
+        int page = -1;
+        if (s < n) {
+            const int key = key_of(s), col = key >> a.page_log2;
+            if (pa_wanted(a, u, key, 8) && col < a.table_cols) page = __ldg(row + col);
+        }
+        return page;
+    };
+    auto issue = [&](int s, int page, int &ex) {
+        const unsigned slot = (unsigned)key_of(s) & slot_mask;
+        const bool there = (unsigned)page < (unsigned)p.n_pages;
+        const uint32_t to = ring_u + ((s + odd) & 1) * C::STAGE, bytes = there ? 16u : 0u;
+        const unsigned long long from = there ? (unsigned long long)(unsigned)page * (unsigned)p.sp + (unsigned long long)slot * (unsigned)p.ss : 0ull;
+        const unsigned step = there ? (unsigned)p.ss : 0u;
+        const uint8_t *ks = kb + from, *vs = vb + from;
 #pragma unroll
-            for (int i = 0; i < 8 / RI; ++i) {
-                const uint32_t at = to + piece_at<D>(group8 + i * RI + crow, cpiece);
-                cp_async_16(at, ks + (unsigned long long)step * (unsigned)(i * RI), bytes);
-                cp_async_16(at + C::HALF, vs + (unsigned long long)step * (unsigned)(i * RI), bytes);
-            }
-            cp_async_commit();
-            ex = NONE;
-            if ((lane & 6) == 0 && there)
-                ex = __ldg(eb + ((unsigned long long)(unsigned)page * (unsigned)p.ep + (unsigned long long)(slot >> p.block_log2) * (unsigned)p.eb));
-        };
-
-        int ex_next, page = page_of(0);
+        for (int i = 0; i < 8 / RI; ++i) {
+            const uint32_t at = to + piece_at<D>(group8 + i * RI + crow, cpiece);
+            cp_async_16(at, ks + (unsigned long long)step * (unsigned)(i * RI), bytes);
+            cp_async_16(at + C::HALF, vs + (unsigned long long)step * (unsigned)(i * RI), bytes);
+        }
+        cp_async_commit();
+        ex = NONE;
+        if ((lane & 6) == 0 && there)
+            ex = __ldg(eb + ((unsigned long long)(unsigned)page * (unsigned)p.ep + (unsigned long long)(slot >> p.block_log2) * (unsigned)p.eb));
+    };
+    int ex_next = NONE, page = -1;
+    auto begin = [&]() {                               // the first step's copies of the piece at hand
+        n = w.t1 - w.t;
+        row = a.table + (long long)u.b * a.table_stride;
+        kb = p.k + (long long)w.h * p.sh + crow * p.ss + cpiece * 16;
+        vb = p.v + (long long)w.h * p.sh + crow * p.ss + cpiece * 16;
+        eb = ((lane & 1) ? p.ve : p.ke) + (long long)w.h * p.eh;       // the first two lanes of eight: K's and V's exponent
+        page = page_of(0);
         issue(0, page, ex_next);
         page = page_of(1);
-
+    };
+    begin();
+    bool more = true;
+    while (more) {
         // q: row g (and g + 8), channels t4 * CQ onwards, as fp16
         uint32_t qf[NT][D / 16][2];
         float rr[NT][2];                                   // what the scores of rows 2 t4, 2 t4 + 1 are multiplied by
@@ -242,7 +249,7 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
             const int ex_here = ex_next;
             if (s + 1 < n) issue(s + 1, page, ex_next);
             page = page_of(s + 2);
-            const uint8_t *at = ring + (s & 1) * C::STAGE, *at1 = at + C::HALF;
+            const uint8_t *at = ring + ((s + odd) & 1) * C::STAGE, *at1 = at + C::HALF;
             const bool edge = w.t + s < full0 || w.t + s >= full1;
             const int j0 = pa_tile(u, w.t + s) * C::KT + warp * 32;
 
@@ -416,8 +423,10 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
         }
         __syncwarp();
 
-        // ---- the piece's result: the warps' parts meet in shared memory ----
-        float *mine = reinterpret_cast<float *>(ring);     // [ROWS][D], 16-byte pieces XORed by the row
+        // ---- the piece's result: the warps' parts meet in shared memory, in the stage of the last step; the next piece's first codes
+        // come into the other one meanwhile ----
+        uint8_t *const meet = smem_raw + ((n - 1 + odd) & 1) * C::STAGE;
+        float *mine = reinterpret_cast<float *>(meet + warp * C::RING);     // [ROWS][D], 16-byte pieces XORed by the row
         const float unit = exp2_whole(max(eo, EXP8_LEAST));
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -436,10 +445,23 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
                         make_float4(o[nt][i][e] * unit, o[nt][i][e + 2] * unit, o[nt][i + 1][e] * unit, o[nt][i + 1][e + 2] * unit);
                 }
             }
-        __syncthreads();
         const bool whole = w.whole();
+        const int rows = u.rows, row0 = u.row0, tok0 = u.tok0, h = w.h;
+        const int b0 = w.first_block(), b1 = w.last_block();
         float *rec = a.part + (size_t)w.record(blockIdx.x) * C::REC;
-        for (int i = tid; i < u.rows * (D / 4); i += 128) {
+        const float *first = a.part + (size_t)w.record(b0) * C::REC;
+        auto store = [&](int r, int c4, float sum, float4 y) {
+            const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);         // NaN stays NaN
+            const int fr = row0 + r, rt = pa_token(a, fr), tok = tok0 + rt;
+            if ((unsigned)tok < (unsigned)a.n_rows)
+                *reinterpret_cast<uint2 *>(a.out + (long long)tok * a.o_st + (long long)(h * a.group + fr - rt * a.group) * a.o_sh + c4 * 4) =
+                    make_uint2(pack_bf16x2(y.x * inv, y.y * inv), pack_bf16x2(y.z * inv, y.w * inv));
+        };
+        odd = (n + odd) & 1;
+        more = w.next(a);
+        if (more) begin();
+        __syncthreads();
+        for (int i = tid; i < rows * (D / 4); i += 128) {
             const int r = i / (D / 4), c4 = i % (D / 4);
             float top = stat_m[0][r];
 #pragma unroll
@@ -451,15 +473,11 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
             for (int k = 0; k < 4; ++k) {
                 const float f = pa_exp2(stat_m[k][r] - ref);
                 sum = fmaf(f, stat_l[k][r], sum);
-                const float4 z = *reinterpret_cast<const float4 *>(smem_raw + k * C::RING + (r * D + ((c4 ^ (r & 7)) << 2)) * 4);
+                const float4 z = *reinterpret_cast<const float4 *>(meet + k * C::RING + (r * D + ((c4 ^ (r & 7)) << 2)) * 4);
                 y.x = fmaf(f, z.x, y.x); y.y = fmaf(f, z.y, y.y); y.z = fmaf(f, z.z, y.z); y.w = fmaf(f, z.w, y.w);
             }
             if (whole) {
-                const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);     // NaN stays NaN
-                const int fr = u.row0 + r, rt = pa_token(a, fr), tok = u.tok0 + rt;
-                if ((unsigned)tok < (unsigned)a.n_rows)
-                    *reinterpret_cast<uint2 *>(a.out + (long long)tok * a.o_st + (long long)(w.h * a.group + fr - rt * a.group) * a.o_sh + c4 * 4) =
-                        make_uint2(pack_bf16x2(y.x * inv, y.y * inv), pack_bf16x2(y.z * inv, y.w * inv));
+                store(r, c4, sum, y);
             } else {
                 *reinterpret_cast<float4 *>(rec + r * D + c4 * 4) = y;
                 if (c4 == 0) { rec[C::ROWS * D + r] = top; rec[C::ROWS * D + C::ROWS + r] = sum; }
@@ -467,7 +485,6 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
         }
         if (!whole) {
             // the block that writes the last part of the pair joins all of them, in block order
-            const int b0 = w.first_block(), b1 = w.last_block();
             __syncthreads();
             if (tid == 0) {
                 const int last = pa_arrive(&a.counters[b0]) == b1 - b0;
@@ -476,51 +493,60 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
             }
             __syncthreads();
             if (last_flag) {
-                const float *first = a.part + (size_t)w.record(b0) * C::REC;
-                auto record = [&](int c) { return c == b0 ? first : a.part + (size_t)(2 * c) * C::REC; };
-                for (int i = tid; i < u.rows * (D / 4); i += 128) {
-                    const int r = i / (D / 4), c4 = (i % (D / 4)) * 4;
-                    float mm = -INFINITY, ll = 0.f;
-                    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (int c = b0; c <= b1; c += 16) {
-                        float pm[16], pl[16];
-                        float4 pv[16];
+                // this thread's pieces of four channels side by side, as many parts at a time as make 16 loads
+                constexpr int NI = C::ROWS * (D / 4) / 128, PB = 16 / NI;
+                float mm[NI], ll[NI];
+                float4 x[NI];
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            pm[k] = -INFINITY;
-                            pl[k] = 0.f;
-                            pv[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                            if (c + k <= b1) {
-                                const float *rc = record(c + k);
-                                pm[k] = __ldcg(rc + C::ROWS * D + r);
-                                pl[k] = __ldcg(rc + C::ROWS * D + C::ROWS + r);
-                                pv[k] = __ldcg(reinterpret_cast<const float4 *>(rc + r * D + c4));
+                for (int j = 0; j < NI; ++j) {
+                    mm[j] = -INFINITY;
+                    ll[j] = 0.f;
+                    x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+                for (int c = b0; c <= b1; c += PB) {
+                    float pm[NI][PB], pl[NI][PB];
+                    float4 pv[NI][PB];
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+#pragma unroll
+                        for (int k = 0; k < PB; ++k) {
+                            const int i = tid + j * 128, r = i / (D / 4), c4 = i % (D / 4);
+                            pm[j][k] = -INFINITY;
+                            pl[j][k] = 0.f;
+                            pv[j][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (c + k <= b1 && r < rows) {
+                                const float *rc = c + k == b0 ? first : a.part + (size_t)(2 * (c + k)) * C::REC;
+                                pm[j][k] = __ldcg(rc + C::ROWS * D + r);
+                                pl[j][k] = __ldcg(rc + C::ROWS * D + C::ROWS + r);
+                                pv[j][k] = __ldcg(reinterpret_cast<const float4 *>(rc + r * D + c4 * 4));
                             }
                         }
-                        float mn = mm;
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) mn = fmaxf(mn, pm[k]);
-                        const float ref = mn == -INFINITY ? 0.f : mn, f0 = pa_exp2(mm - ref);
-                        mm = mn;
-                        ll *= f0;
-                        x.x *= f0; x.y *= f0; x.z *= f0; x.w *= f0;
+                    for (int j = 0; j < NI; ++j) {
+                        float mn = mm[j];
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            const float f = pa_exp2(pm[k] - ref);
-                            ll = fmaf(f, pl[k], ll);
-                            x.x = fmaf(f, pv[k].x, x.x); x.y = fmaf(f, pv[k].y, x.y); x.z = fmaf(f, pv[k].z, x.z); x.w = fmaf(f, pv[k].w, x.w);
+                        for (int k = 0; k < PB; ++k) mn = fmaxf(mn, pm[j][k]);
+                        const float ref = mn == -INFINITY ? 0.f : mn, f0 = pa_exp2(mm[j] - ref);
+                        mm[j] = mn;
+                        ll[j] *= f0;
+                        x[j].x *= f0; x[j].y *= f0; x[j].z *= f0; x[j].w *= f0;
+#pragma unroll
+                        for (int k = 0; k < PB; ++k) {
+                            const float f = pa_exp2(pm[j][k] - ref);
+                            ll[j] = fmaf(f, pl[j][k], ll[j]);
+                            x[j].x = fmaf(f, pv[j][k].x, x[j].x); x[j].y = fmaf(f, pv[j][k].y, x[j].y);
+                            x[j].z = fmaf(f, pv[j][k].z, x[j].z); x[j].w = fmaf(f, pv[j][k].w, x[j].w);
                         }
                     }
-                    const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
-                    const int fr = u.row0 + r, rt = pa_token(a, fr), tok = u.tok0 + rt;
-                    if ((unsigned)tok < (unsigned)a.n_rows)
-                        *reinterpret_cast<uint2 *>(a.out + (long long)tok * a.o_st + (long long)(w.h * a.group + fr - rt * a.group) * a.o_sh + c4) =
-                            make_uint2(pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv));
+                }
+#pragma unroll
+                for (int j = 0; j < NI; ++j) {
+                    const int i = tid + j * 128;
+                    if (i / (D / 4) < rows) store(i / (D / 4), i % (D / 4), ll[j], x[j]);
                 }
             }
         }
-        more = w.next(a);
-        if (more) __syncthreads();                         // the parts are read before the next piece's copies land there
+        if (more) __syncthreads();                         // the parts are read before the next piece's second copies land there
     }
 }
 
