@@ -32,7 +32,7 @@ struct Store8Args {
     const long long *slot_map;
     long long n_rows;
     int tile;                                // rows of a thread block, a power of two
-    int team, heads, groups;                 // warps of one run and head; heads of a block; blocks of a row's heads
+    int team, heads, repeat, groups;         // warps of one run and head; heads of a block at a time, in turn; blocks of a row's heads
 };
 cudaError_t launch_paged8_store(const Store8Args &a, bool f32, cudaStream_t st);
 

@@ -27,22 +27,22 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
     const int comp = lane >> 4, half = lane & 16;
     const int mate = warp % a.team, unit = warp / a.team;                  // of the team, and which one in the block
     const unsigned tile = blockIdx.x / (unsigned)a.groups;
-    const int head = (int)(blockIdx.x - tile * a.groups) * a.heads + unit % a.heads, stride = 8 / a.team / a.heads;
+    const int head0 = ((int)(blockIdx.x - tile * a.groups) * a.heads + unit % a.heads) * a.repeat, stride = 8 / a.team / a.heads;
     const int layer = blockIdx.y;
+    const int sub = (lane & 15) / LPR, c8 = (lane % LPR) * 8;              // row of a load, first channel
+    const long long row_bytes = a.s_st * (F32 ? 4 : 2);
+    const char *src = static_cast<const char *>(comp ? a.src_v : a.src_k) + ((long long)layer * a.s_sl + c8) * (F32 ? 4 : 2);
+    uint8_t *codes = (comp ? p.v : p.k) + (long long)layer * p.sl + c8;
+    int8_t *exps = (comp ? p.ve : p.ke) + (long long)layer * p.el;
+    const int slot_mask = (1 << p.page_log2) - 1, block_mask = (1 << p.block_log2) - 1;
+    const std::integral_constant<int, ITER> all;
+    const std::integral_constant<int, PART> part;
 
     auto slot_of = [&](long long row) { return row >= 0 && row < a.n_rows ? __ldg(a.slot_map + row) : -1ll; };
     auto fits = [&](long long slot) { return slot >= 0 && slot < p.n_slots; };
-    const int sub = (lane & 15) / LPR, c8 = (lane % LPR) * 8;              // row of a load, first channel
-    const int h = min(head, p.H - 1);
-    const char *src = static_cast<const char *>(comp ? a.src_v : a.src_k) + ((long long)layer * a.s_sl + (long long)h * a.s_sh + c8) * (F32 ? 4 : 2);
-    uint8_t *codes = (comp ? p.v : p.k) + (long long)layer * p.sl + (long long)h * p.sh + c8;
-    int8_t *exps = (comp ? p.ve : p.ke) + (long long)layer * p.el + (long long)h * p.eh;
-    const long long row_bytes = a.s_st * (F32 ? 4 : 2);
-    const int slot_mask = (1 << p.page_log2) - 1, block_mask = (1 << p.block_log2) - 1;
-
     // 32 rows of the tile at a time
     for (long long r0 = (long long)tile * a.tile, r1 = min(r0 + a.tile, a.n_rows); r0 < r1; r0 += 32) {
-    // runs that begin in this tile: valid rows whose nearest valid row of the 32 before them is of another block, or missing
+    // runs that begin among them: valid rows whose nearest valid row of the 32 before them is of another block, or missing
     const long long mine = r0 + lane < r1 ? slot_of(r0 + lane) : -1, back = slot_of(r0 - 32 + lane);
     const long long my_block = mine >> p.block_log2;
     const bool ok = fits(mine);
@@ -57,14 +57,11 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
 
     for (int run0 = 0; run0 < n_runs; run0 += stride) {                    // the same rounds in every warp: they meet below
         const int run = run0 + unit / a.heads;
-        const bool live = run < n_runs && head < p.H;
-        const int at = live ? __ffs(__ballot_sync(0xffffffffu, begins && rank == run)) - 1 : 0;
+        const bool there = run < n_runs;
+        const int at = there ? __ffs(__ballot_sync(0xffffffffu, begins && rank == run)) - 1 : 0;
         const long long first = r0 + at;
         const long long block = __shfl_sync(0xffffffffu, my_block, at);
         const long long page = block >> (p.page_log2 - p.block_log2), in_page = block & ((1 << (p.page_log2 - p.block_log2)) - 1);
-        int8_t *ep = exps + page * p.ep + in_page * p.eb;
-        uint8_t *base = codes + page * p.sp;
-        const int old = live && (lane & 15) == 0 ? (int)*ep : 0;
         // rows of the run among the 32 from `row`, as bits; `last`: the latest one found so far, -1 at the end of the run
         long long slot = -1;                                               // this lane's
         auto members = [&](long long row, long long &last) -> unsigned {
@@ -77,15 +74,54 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
             last = other ? -1 : row + 31 - __clz(m);
             return m;
         };
+        // The team's chunks go round: this warp's are the ones with number mate, mate + team, ...  `each` is called with the 32 rows'
+        // first one, their bits, and the place of a chunk of this warp among them.
+        bool begun = false;                                                // the block's first row is among the run's
+        auto chunks = [&](auto each) {
+            long long last = there ? first : -1;
+            int before = 0;                                                // chunks of the 32 rows before these
+            for (long long row = first; last >= 0; row += 32, before += 32 / CHUNK) {
+                const unsigned m = members(row, last);
+                begun |= __any_sync(0xffffffffu, (m >> lane & 1) && ((int)slot & block_mask) == 0) != 0;
+#pragma unroll 1
+                for (int k0 = ((mate - before) & (a.team - 1)) * CHUNK; k0 < 32; k0 += a.team * CHUNK)
+                    if (m >> k0) each(row, m, k0);
+                if (!m) break;
+            }
+        };
+        // this warp's first chunk, which it keeps, and whether it has more
+        unsigned kept = 0;
+        long long kept_row = -1;
+        int kept_slot = -1, kept_k0 = 0;
+        bool others = false;
+        chunks([&](long long row, unsigned m, int k0) {
+            if (kept_row < 0) {
+                kept = m;
+                kept_k0 = k0;
+                kept_row = row;
+                kept_slot = (int)slot & slot_mask;
+            } else {
+                others = true;
+            }
+        });
+        const bool few = (kept >> kept_k0) >> (PART * RPI - 1) <= 1u;      // a step's single row, for one
+
+        for (int head = head0; head < head0 + a.repeat; ++head) {
+        const bool live = there && head < p.H;
+        const int h = min(head, p.H - 1);
+        const char *src_h = src + (long long)h * a.s_sh * (F32 ? 4 : 2);
+        int8_t *ep = exps + (long long)h * p.eh + page * p.ep + in_page * p.eb;
+        uint8_t *base = codes + (long long)h * p.sh + page * p.sp;
+        const int old = live && (lane & 15) == 0 ? (int)*ep : 0;
         auto load = [&](long long row, unsigned m, int k0, auto &x, auto count) {
-            const char *at = src + (row + k0 + sub) * row_bytes;
+            const char *from_row = src_h + (row + k0 + sub) * row_bytes;
             m >>= k0 + sub;
 #pragma unroll
-            for (int i = 0; i < decltype(count)::value; ++i, at += RPI * row_bytes) {
+            for (int i = 0; i < decltype(count)::value; ++i, from_row += RPI * row_bytes) {
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
                     x[i][w] = make_uint4(0, 0, 0, 0);
-                    if (m & (1u << i * RPI)) x[i][w] = __ldg(reinterpret_cast<const uint4 *>(at) + w);
+                    if (m & (1u << i * RPI)) x[i][w] = __ldg(reinterpret_cast<const uint4 *>(from_row) + w);
                 }
             }
         };
@@ -103,7 +139,6 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
             }
         };
         float most = 0.f, finite = 0.f;                                    // finite: not 0 once a value was infinite or NaN
-        bool begun = false;                                                // the block's first row is among the run's
         auto largest = [&](const auto &x, auto count) {
 #pragma unroll
             for (int i = 0; i < decltype(count)::value; ++i) {
@@ -117,52 +152,26 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
                 }
             }
         };
-        // The team's chunks go round: this warp's are the ones with number mate, mate + team, ...  `each` is called with the 32 rows'
-        // first one, their bits, and the place of a chunk of this warp among them.
-        auto chunks = [&](auto each) {
-            long long last = live ? first : -1;
-            int before = 0;                                                // chunks of the 32 rows before these
-            for (long long row = first; last >= 0; row += 32, before += 32 / CHUNK) {
-                const unsigned m = members(row, last);
-                begun |= __any_sync(0xffffffffu, (m >> lane & 1) && ((int)slot & block_mask) == 0) != 0;
-#pragma unroll 1
-                for (int k0 = ((mate - before) & (a.team - 1)) * CHUNK; k0 < 32; k0 += a.team * CHUNK)
-                    if (m >> k0) each(row, m, k0);
-                if (!m) break;
-            }
-        };
         // ---- largest magnitude ----
         uint4 keep[ITER][W];
-        unsigned kept = 0;                                                 // the kept chunk's rows
-        long long kept_slot = -1, kept_row = -1;
-        int kept_k0 = 0;
-        bool others = false, few = false;
-        const std::integral_constant<int, ITER> all;
-        const std::integral_constant<int, PART> part;
-        chunks([&](long long row, unsigned m, int k0) {
-            if (kept_row < 0) {
-                kept = m;
-                kept_k0 = k0;
-                kept_row = row;
-                kept_slot = slot;
-                few = (m >> k0) >> (PART * RPI - 1) <= 1u;                 // a step's single row, for one
-                if (few) {
-                    load(row, m, k0, keep, part);
-                    largest(keep, part);
-                } else {
-                    load(row, m, k0, keep, all);
-                    largest(keep, all);
-                }
-            } else {
-                others = true;
+        const unsigned mine_kept = live ? kept : 0u;
+        if (few) {
+            load(kept_row, mine_kept, kept_k0, keep, part);
+            largest(keep, part);
+        } else {
+            load(kept_row, mine_kept, kept_k0, keep, all);
+            largest(keep, all);
+        }
+        if (others && live)
+            chunks([&](long long row, unsigned m, int k0) {
+                if (row == kept_row && k0 == kept_k0) return;
 #pragma unroll 1
                 for (int k = k0; k < k0 + CHUNK; k += PART * RPI) {
                     uint4 x[PART][W];
                     load(row, m, k, x, part);
                     largest(x, part);
                 }
-            }
-        });
+            });
         uint32_t top = __float_as_uint(most);
 #pragma unroll
         for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -189,11 +198,11 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
         // ---- codes ----
         const float f = exp2_whole(-e);
         const bool plain = FMT == CACHE_INT8 && __all_sync(0xffffffffu, finite == 0.f && e < exp8_most(FMT));      // all are within the codes' range
-        auto write = [&](const auto &x, unsigned m, int k0, long long slots, auto count) {
+        auto write = [&](const auto &x, unsigned m, int k0, int slots, auto count) {
 #pragma unroll
             for (int i = 0; i < decltype(count)::value; ++i) {
                 const int k = k0 + i * RPI + sub;
-                const int to = __shfl_sync(0xffffffffu, (int)slots & slot_mask, k);
+                const int to = __shfl_sync(0xffffffffu, slots, k);
                 if (m >> k & 1) {
                     float v[8];
                     values(x[i], v);
@@ -213,18 +222,20 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
                 }
             }
         };
-        if (kept && few) write(keep, kept, kept_k0, kept_slot, part);
-        else if (kept) write(keep, kept, kept_k0, kept_slot, all);
-        if (others)
+        if (few) write(keep, mine_kept, kept_k0, kept_slot, part);
+        else write(keep, mine_kept, kept_k0, kept_slot, all);
+        if (others && live)
             chunks([&](long long row, unsigned m, int k0) {
                 if (row == kept_row && k0 == kept_k0) return;
+                const int in_block_page = (int)slot & slot_mask;
 #pragma unroll 1
                 for (int k = k0; k < k0 + CHUNK; k += PART * RPI) {
                     uint4 x[PART][W];
                     load(row, m, k, x, part);
-                    write(x, m, k, slot, part);
+                    write(x, m, k, in_block_page, part);
                 }
             });
+        }
         if (a.team > 1) __syncthreads(); else __syncwarp();                // the block's run before this one's is no longer looked at
     }
     }
@@ -245,6 +256,12 @@ cudaError_t launch_paged8_store(const Store8Args &args, bool f32, cudaStream_t s
     const long long wanted = 4ll * device_sm_count();
     a.tile = a.pool.block_log2 > 5 ? 1 << a.pool.block_log2 : 32;
     while (a.tile > 1 && (a.n_rows + a.tile - 1) / a.tile * a.pool.L * a.groups < wanted) a.tile /= 2;
+    // Heads that a team does one after the other, with one look at the run: where that leaves 16 blocks an SM.
+    a.repeat = 1;
+    while (a.groups > 1 && (a.n_rows + a.tile - 1) / a.tile * a.pool.L * (a.groups / 2) >= 4 * wanted) {
+        a.repeat *= 2;
+        a.groups = (a.pool.H + a.heads * a.repeat - 1) / (a.heads * a.repeat);
+    }
     dim3 grid((unsigned)((a.n_rows + a.tile - 1) / a.tile * a.groups), (unsigned)a.pool.L);
     auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a); };
     const bool e4m3 = a.pool.format == CACHE_E4M3;
