@@ -25,10 +25,13 @@
 // block walks 154 pieces where the others walk 14; a piece costs 7,600 cycles beside its tiles, the same number for every
 // prompt measured.  16 requests of 2 to 16 rows over 8,192 keys 109 - 144 us (4.9 - 3.7 TB/s), by rows and page size.
 //
-// The same kernel reads a cache held in 8 bits (FMT is its format; BF16_PAGES is this file's head): the copying and clearing warps give
-// way to four that convert.  The producer copies the codes of a tile's K and V (TMA, two tiles ahead of the products at most), and their
-// exponents beside them; the converting warps write them as bf16 numbers code * 2^e, which are exact, where the products take them
-// from; everything after that is as above.
+// The same kernel reads a cache held in 8 bits (FMT is its format; BF16_PAGES is this file's head): the producer copies the codes of a
+// tile's K and V (TMA, two tiles ahead of the products at most), and their exponents beside them; four converting warps write them as
+// bf16 numbers code * 2^e, which are exact, where the products take them from; everything after that is as above.  Bound by the
+// conversions: 640 instructions a warp for 128 keys, beside the softmax warps' own, and by the power limit.  Measured: the chunk of 4,096
+// rows 1.83 - 1.89 ms (1.61 without converting anything; copies made by the converting warps themselves 1.93), the prompt of 8,192
+// rows 1.48 ms, 16 requests of 6 rows over 8,192 keys 133 us.  K and q as fp16 with a scale for 32 keys need fewer conversions, but
+// more in the softmax warps and at each piece: 1.91 ms, and 102 us instead of 84 for the window chunk of 64 channels.
 #include <type_traits>
 
 #include "cb_paged.cuh"
