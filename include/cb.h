@@ -549,8 +549,9 @@ cb_status cb_paged_attention(const cb_page_pool *pool, int32_t layer, const void
  *     code at (uint8*)k + layer*stride_layer + page*stride_page + slot*stride_slot + head*stride_head + c
  *     exp  at k_exp + layer*exp_stride_layer + page*exp_stride_page + (slot / block)*exp_stride_block + head*exp_stride_head
  * Channels are contiguous, k and v 16-byte aligned, code strides (bytes) multiples of 16, exponents anywhere; strides of
- * pages, slots and blocks below 2^32, of layers and heads below 2^40, 0 only on a dimension of size 1 (CB_ERR_UNSUPPORTED otherwise).  head_dim 64 or 128; page_size 8, 16, 32, 64, 128 or
- * 256; block one of these too, at most page_size; n_pages < 2^31.  Exponents lie in -100 .. 119 (e4m3) or .. 121 (int8), and
+ * pages, slots and blocks below 2^32, of layers and heads below 2^40, 0 only on a dimension of size 1 (CB_ERR_UNSUPPORTED
+ * otherwise).  head_dim 64 or 128; page_size 8, 16, 32, 64, 128 or 256; block one of these too, at most page_size; n_pages < 2^31;
+ * in store and load at most 65,535 layers and heads, and fewer than 2^34 rows x heads.  Exponents lie in -100 .. 119 (e4m3) or .. 121 (int8), and
  * one outside counts as the nearest of these.  A cache needs no initialisation.
  */
 enum { CB_CACHE_E4M3 = 0, CB_CACHE_INT8 = 1 };
@@ -580,7 +581,8 @@ typedef struct cb_page_pool8 {
  * leaves them (where they do not, the block's contents are unspecified); of two rows with one slot either may end there,
  * piece by piece.  Rows must be finite: an infinity becomes the largest code of a block whose other rows vanish beside it,
  * NaN becomes e4m3's NaN or int8's 0.  (Of int8 codes, magnitudes of 2^127 and more become 127 * 2^121.)
- * src_k / src_v: as for cb_paged_store (bf16 or fp32, 16-byte aligned, strides in elements, multiples of 8), not in the pool.
+ * src_k / src_v: as for cb_paged_store (bf16 or fp32, 16-byte aligned, strides in elements, multiples of 8), not in the pool.  The
+ * pool's four arrays do not overlap.
  */
 cb_status cb_paged_store8(const cb_page_pool8 *pool, const void *src_k, const void *src_v, int32_t src_dtype, int64_t n_rows,
                           int64_t stride_layer, int64_t stride_token, int64_t stride_head, const int64_t *slot_map, void *stream);
@@ -597,10 +599,11 @@ cb_status cb_paged_load8(const cb_page_pool8 *pool, void *dst_k, void *dst_v, in
 /*
  * cb_paged_attention over a pool of 8 bits: the same arguments, rows, masks, splits and promises, with its own workspace
  * size.  (Device-side time-outs and the test hooks concern the kernel for many rows; the one for few rows has no wait that
- * could run out.)  Codes become 16-bit numbers exactly.  Weights are rounded to fp16
- * (2^-11 of each that is above 2^-16 of the largest) or bf16 (2^-8), as max_new chooses between kernels.  Rows of a page
- * that no row of the request sees may hold anything, and so may the exponents of blocks without a seen row; values that
- * some row sees must be finite and below 2^90.
+ * could run out.)  Codes become 16-bit numbers exactly; weights are rounded to fp16 (by 2^-11 of each that is above 2^-16 of the
+ * largest, by 2^-27 of the largest below that) or bf16 (2^-8), as max_new chooses between kernels; int8 scores are off by less
+ * than 2^-11 of a code's step in every channel.  Rows of a page that no row of the request sees may hold anything, and so may the
+ * exponents of blocks without a seen row.  Rows that are seen hold finite values, under exponents of at most 80, and scale times
+ * |q| times 2^exp of a seen block of K stays below 2^100.
  */
 cb_status cb_paged_attention8_workspace_bytes(int32_t head_dim, size_t *bytes);
 cb_status cb_paged_attention8(const cb_page_pool8 *pool, int32_t layer, const void *q, int64_t q_stride_token, int64_t q_stride_head,

@@ -533,7 +533,7 @@ static PFN_cuTensorMapEncodeTiled_v12000 encode_fn()
     return fn;
 }
 
-// 4-D map over (64 channels, head, token, 64-channel block): one box = 64 channels of box_heads heads of box_tokens tokens.
+// 4-D map over (channel, row of a page, head, page) of one-byte codes: one box = all channels of box_rows rows of one head.
 bool make_code_tensor_map(CUtensorMap *map, const void *base, int d, int H, int rows, long long pages, long long sh, long long ss,
                           long long sp, int box_rows)
 {
@@ -549,6 +549,7 @@ bool make_code_tensor_map(CUtensorMap *map, const void *base, int d, int H, int 
                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// 4-D map over (64 channels, head, token, 64-channel block): one box = 64 channels of box_heads heads of box_tokens tokens.
 bool make_q_tensor_map(CUtensorMap *map, const void *base, int d, int H, long long T, long long sh, long long st, int box_heads,
                        int box_tokens)
 {

@@ -175,7 +175,7 @@ cb_status check_rows8(const cb_page_pool8 *pool, const void *k, const void *v, i
     if (n_rows < 0 || stride_layer < 0 || stride_token < 0 || stride_head < 0) return CB_ERR_INVALID_ARG;
     if ((stride_layer | stride_token | stride_head) & 7) return CB_ERR_INVALID_ARG;
     if (n_rows >= (1ll << 31) || pool->n_layers > 65535 || pool->n_heads > 65535) return CB_ERR_UNSUPPORTED;
-    if (n_rows * pool->n_heads >= (1ll << 35)) return CB_ERR_UNSUPPORTED;      // blocks of one launch
+    if (n_rows * pool->n_heads >= (1ll << 34)) return CB_ERR_UNSUPPORTED;      // blocks of one launch
     if (n_rows == 0) return CB_OK;
     if (!k || !v || !slot_map || (((uintptr_t)k | (uintptr_t)v) & 15) || ((uintptr_t)slot_map & 7)) return CB_ERR_INVALID_ARG;
     return CB_OK;

@@ -16,7 +16,9 @@
 //             batch below where conversions took 136.)
 //   weights   2^6 exp2(s - m), with m at most 13 behind the row's maximum; rounded to fp16 (2^-11 of each weight above 2^-16 of the
 //             largest) for the product with V, whose codes fp16 holds exactly, and summed unrounded.
-// A block's exponent multiplies its scores and its part of the output, in fp32.
+// A block's exponent multiplies its scores and its part of the output, in fp32.  The output is held in units of 2^-60 to 2^20, about the
+// largest exponent of V so far: blocks near it go by way of their weights, others by a product of their own, and neither leaves
+// fp32's range (exponents up to 80).
 //
 // Measured, 64 requests of 512 to 8,192 keys, 8 KV heads of 128, pages and blocks of 16: e4m3 and 8 query heads a KV head 108 - 114 us
 // (box to box) for 0.56 GB = 4.9 - 5.2 TB/s, of which the copies alone take 104 us (rows of 128 bytes, 1 KB apart, arrive at 6.1 TB/s;
@@ -127,6 +129,7 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
     const int g = lane >> 2, t4 = lane & 3;
     constexpr int CQ = D / 4, CPT = D / 8;
     constexpr int NONE = -1000;                        // exponent of a group of keys that nobody sees, or without a page
+    constexpr int UNIT_LEAST = -60, UNIT_MOST = 20;    // of the output
 
     pa_schedule<C::ROWS, C::KT, 128>(a, reinterpret_cast<int *>(smem_raw), (int)(C::SMEM / 4), &share, warp_sums);
     PaWalk<C::ROWS, C::KT> w;
@@ -276,9 +279,10 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
                 ev[h] = (int)((all_v >> (8 * h)) & 255u);
                 ev_top = max(ev_top, ev[h]);
             }
-            if (ev_top - 128 > eo + 1 && ev_top > 0) {     // a larger unit
-                const float f = exp2_whole(max(eo - (ev_top - 128), -126));
-                eo = ev_top - 128;
+            if (min(ev_top - 128, UNIT_MOST) > eo + 1 && ev_top > 0) {     // a larger unit
+                const int larger = max(min(ev_top - 128, UNIT_MOST), UNIT_LEAST);
+                const float f = exp2_whole(max(eo - larger, -126));        // the first one: of zeros
+                eo = larger;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -290,7 +294,7 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
                 ev[h] = ev[h] == 0 ? 0 : ev[h] - 128 - eo;
-                close &= ev[h] >= -4;
+                close &= ev[h] >= -4 && ev[h] <= 1;
             }
             float dv[4], undo[4];
 #pragma unroll
@@ -421,7 +425,7 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
                             for (int y = 0; y < 2; ++y) {
                                 float d[4] = {0.f, 0.f, 0.f, 0.f};
                                 mma_f16_1688(d, f[2 * y], f[2 * y + 1], pb[kk][nt][y]);
-                                const float fv = exp2_whole(max(ev[2 * kk + y], -126));
+                                const float fv = exp2_whole(ev[2 * kk + y]);
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) o[nt][i][e] = fmaf(d[e], fv, o[nt][i][e]);
                             }
@@ -435,7 +439,7 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
         // come into the other one meanwhile ----
         uint8_t *const meet = smem_raw + ((n - 1 + odd) & 1) * C::STAGE;
         float *mine = reinterpret_cast<float *>(meet + warp * C::RING);     // [ROWS][D], 16-byte pieces XORed by the row
-        const float unit = exp2_whole(max(eo, EXP8_LEAST));
+        const float unit = exp2_whole(max(eo, UNIT_LEAST));
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

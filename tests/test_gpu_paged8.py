@@ -403,6 +403,26 @@ def test_attention_with_exponents_far_apart(kind, new):
 
 
 @KINDS
+@pytest.mark.parametrize("new", [1, 6, 40])
+@pytest.mark.parametrize("low,high", [(-100, 60), (-100, -70), (-61, 80), (19, 80), (-100, 80)])
+def test_attention_with_exponents_at_the_ends_of_what_is_allowed(kind, new, low, high):
+    """Blocks of V at both ends, the large ones in turn of zeros only and seen: what the small ones give is not lost, whichever come first."""
+    H, group, d, page, block, n = 2, 4, 128, 16, 8, 300
+    for large_first in (False, True):
+        for zeros in (False, True):
+            q, pool, table, cu, total = _batch(kind, [new], [n], H, group, d, page, block)
+            e = torch.full_like(pool.v_exp, low)
+            late = torch.zeros(pool.v.shape[1], dtype=torch.bool, device=DEV)
+            late[table[0, 4:11].long()] = True
+            large = ~late if large_first else late
+            e[:, large] = high
+            pool.v_exp.copy_(e)
+            if zeros:
+                pool.v.view(torch.uint8)[:, large] = 0
+            _compare(q, pool, table, cu, total)
+
+
+@KINDS
 @pytest.mark.parametrize("new", [1, 30])
 def test_attention_of_queries_of_any_size(kind, new):
     """Rows of q from 2^-60 to 2^10, one of zeros, with channels 2^-20 of its largest: the same weights as in 64 bits."""

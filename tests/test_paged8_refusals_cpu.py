@@ -35,6 +35,8 @@ POOLS = [(dict(k=0), BAD), (dict(v=0x2008), BAD), (dict(ke=0), BAD), (dict(ve=0)
          (dict(d=96, sh=96), UNS), (dict(ps=24), UNS), (dict(ps=4, block=4), UNS), (dict(ps=512), UNS), (dict(block=4), UNS), (dict(block=12), UNS),
          (dict(block=32), UNS), (dict(n=1 << 31, sl=0, L=1), UNS), (dict(sl=0), UNS), (dict(sp=0), UNS), (dict(ss=0), UNS), (dict(sh=0), UNS),
          (dict(el=0), UNS), (dict(ep=0), UNS), (dict(eb=0), UNS), (dict(eh=0), UNS), (dict(sp=1 << 40), UNS), (dict(ep=1 << 40), UNS),
+         (dict(sp=1 << 32), UNS), (dict(ss=1 << 32), UNS), (dict(ep=1 << 32), UNS), (dict(eb=1 << 32), UNS), (dict(sl=1 << 40), UNS), (dict(sh=1 << 40), UNS),
+         (dict(el=1 << 40), UNS), (dict(eh=1 << 40), UNS), (dict(sp=(1 << 32) - 16, ss=(1 << 32) - 16, ep=(1 << 32) - 1, eb=(1 << 32) - 1), CUDA),
          (dict(block=16, eb=0), CUDA), (dict(L=1, sl=0, el=0), CUDA), (dict(H=1, sh=0, eh=0, ss=128), CUDA), (dict(fmt=cb.CB_CACHE_INT8), CUDA)]
 
 
@@ -46,7 +48,7 @@ def _rows(call, pool=None, k=0x10000, v=0x20000, dt=cb.CB_DTYPE_BF16, rows=5, sl
 @pytest.mark.parametrize("change,want", [
     ({}, CUDA), (dict(rows=0), OK), (dict(rows=0, k=0, v=0, slot=0), OK), (dict(dt=cb.CB_DTYPE_F32), CUDA), (dict(dt=2), BAD), (dict(k=0), BAD),
     (dict(v=0x20008), BAD), (dict(rows=-1), BAD), (dict(slot=0), BAD), (dict(slot=0x104), BAD), (dict(st=516), BAD), (dict(sh=-8), BAD),
-    (dict(rows=1 << 31), UNS), (dict(pool=_pool(H=1 << 17)), UNS), (dict(pool=_pool(L=1 << 16)), UNS)])
+    (dict(rows=1 << 31), UNS), (dict(pool=_pool(H=1 << 17)), UNS), (dict(rows=1 << 30, pool=_pool(H=16)), UNS), (dict(rows=(1 << 30) - 1, pool=_pool(H=16)), CUDA), (dict(pool=_pool(L=1 << 16)), UNS)])
 def test_rows(change, want):
     assert _rows(cb.lib().cb_paged_store8, **change) == want
     assert _rows(cb.lib().cb_paged_load8, **change) == want
