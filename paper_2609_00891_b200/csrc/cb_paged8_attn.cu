@@ -131,7 +131,10 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
     constexpr int NONE = -1000;                        // exponent of a group of keys that nobody sees, or without a page
     constexpr int UNIT_LEAST = -60, UNIT_MOST = 20;    // of the output
 
-    pa_schedule<C::ROWS, C::KT, 128>(a, reinterpret_cast<int *>(smem_raw), (int)(C::SMEM / 4), &share, warp_sums);
+    // Windows of 1,024 keys and 4 sinks, 10 tiles a pair, 256 pairs: 26 us split, 29 in blocks of their own; 8 tiles a pair 21.5 either way.
+    // One tile a block against two where there are blocks enough: one request of 1,024 keys 9.0 / 9.5 us, 2,048 10.8 / 9.9, 4,096 15.1 / 12.1
+    // (each round of the join takes eight parts).
+    pa_schedule<C::ROWS, C::KT, 128, 1, 12>(a, reinterpret_cast<int *>(smem_raw), (int)(C::SMEM / 4), &share, warp_sums);
     PaWalk<C::ROWS, C::KT> w;
     if (!w.open(a, share)) return;
 
