@@ -14,7 +14,7 @@
 //             magnitude to 2^14 .. 2^15, so that a bf16 number above 2^-29 of that one stays exact, and the rest is off by 2^-40 of it.
 //             (8-bit operands of the warp-level instruction, q in parts of 8 bits, took more instructions: 144 us for the decode
 //             batch below where conversions took 136.)
-//   weights   2^6 exp2(s - m), with m at most 13 behind the row's maximum; rounded to fp16 (2^-11 of each weight above 2^-16 of the
+//   weights   2^6 exp2(s - m), with m at most 8 behind the row's maximum; rounded to fp16 (2^-11 of each weight above 2^-16 of the
 //             largest) for the product with V, whose codes fp16 holds exactly, and summed unrounded.
 // A block's exponent multiplies its scores and its part of the output, in fp32.  The output is held in units of 2^-60 to 2^20, about the
 // largest exponent of V so far: blocks near it go by way of their weights, others by a product of their own, and neither leaves
@@ -60,11 +60,17 @@ __device__ __forceinline__ void mma_f16_16816(float (&c)[4], const uint32_t (&a)
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// The same onto zeros.
-__device__ __forceinline__ void mma_f16_16816_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+// The same onto one number a column.
+__device__ __forceinline__ void mma_f16_16816_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1)
 {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
-        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ float2 f2_of(uint64_t v)
+{
+    float2 r;
+    f2_unpack(v, r.x, r.y);
+    return r;
 }
 __device__ __forceinline__ void mma_f16_1688(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b)
 {
@@ -194,8 +200,8 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
     while (more) {
         // q: row g (and g + 8), channels t4 * CQ onwards, as fp16
         uint32_t qf[NT][D / 16][2];
-        float rr[NT][2];                                   // what the scores of rows 2 t4, 2 t4 + 1 are multiplied by
-        float excess[NT][2];                               // and what they are too large by (int8)
+        float2 rr[NT];                                     // what the scores of rows 2 t4, 2 t4 + 1 are multiplied by
+        float2 start[NT];                                  // and begin with: less what they are too large by (int8)
         int pos[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -233,16 +239,17 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
             }
             // a row of q that is not finite has no weights that are: NaN, as in 32 bits
             const float whole = top < 0x7f800000u ? back : __int_as_float(0x7fc00000);
+            rr[nt] = make_float2(__shfl_sync(0xffffffffu, whole, 8 * t4), __shfl_sync(0xffffffffu, whole, 8 * t4 + 4));
+            start[nt] = make_float2(0.f, 0.f);
+            if (FMT == CACHE_INT8) start[nt] = make_float2(-__shfl_sync(0xffffffffu, sum, 8 * t4), -__shfl_sync(0xffffffffu, sum, 8 * t4 + 4));
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                rr[nt][e] = __shfl_sync(0xffffffffu, whole, (2 * t4 + e) * 4);
-                excess[nt][e] = FMT == CACHE_INT8 ? __shfl_sync(0xffffffffu, sum, (2 * t4 + e) * 4) : 0.f;
                 const int r2 = nt * 8 + 2 * t4 + e, tok2 = pa_token(a, u.row0 + r2);
                 pos[nt][e] = r2 < u.rows && (unsigned)(u.tok0 + tok2) < (unsigned)a.n_rows ? u.base + tok2 : -1;
             }
         }
         float o[NT][D / 16][4];
-        float m[NT][2], l[NT][2];                          // 2^6 below the maximum that counts, sum of this thread's weights
+        float2 minus[NT], l[NT];                           // less (6 below the maximum that counts); sum of this thread's weights
         int eo = NONE;                                     // o is in units of 2^eo
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -250,8 +257,8 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) { m[nt][e] = -INFINITY; l[nt][e] = 0.f; }
+            minus[nt] = make_float2(INFINITY, INFINITY);
+            l[nt] = make_float2(0.f, 0.f);
         }
         int full0, full1;                                  // tiles [full0, full1) need no mask
         pa_full_tiles<C::KT>(a, u, full0, full1);
@@ -267,23 +274,16 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
             const bool edge = w.t + s < full0 || w.t + s >= full1;
             const int j0 = pa_tile(u, w.t + s) * C::KT + warp * 32;
 
-            // ---- exponents of the four groups of 8 keys (h = 0 .. 3), a byte each: e + 128, 0 for NONE ----
+            if (!pa_wanted(a, u, j0, 32)) continue;        // none of the warp's keys is seen
+
+            // ---- exponents of the four groups of 8 keys, in the lanes that loaded them ----
             // Where V's lie within 2^-4 .. 2 of the output's unit, each key's goes onto its weight and the product adds to the output; else
             // every group has a product of its own.
-            const unsigned byte = ex_here == NONE ? 0u : (unsigned)(exp8_clamp(ex_here, FMT) + 128) << (lane & 24);
-            const unsigned all_k = __reduce_or_sync(0xffffffffu, (lane & 7) == 0 ? byte : 0u);
-            const unsigned all_v = __reduce_or_sync(0xffffffffu, (lane & 7) == 1 ? byte : 0u);
-            float fk[4];                                   // 2^(K's exponent)
-            int ev[4];                                     // V's exponent less the unit's
-            int ev_top = 0;
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                fk[h] = __uint_as_float((max((all_k >> (8 * h)) & 255u, 1u) - 1u) << 23);
-                ev[h] = (int)((all_v >> (8 * h)) & 255u);
-                ev_top = max(ev_top, ev[h]);
-            }
-            if (min(ev_top - 128, UNIT_MOST) > eo + 1 && ev_top > 0) {     // a larger unit
-                const int larger = max(min(ev_top - 128, UNIT_MOST), UNIT_LEAST);
+            const bool of_v = (lane & 7) == 1 && ex_here != NONE;
+            const int e_here = exp8_clamp(ex_here, FMT);
+            const int ev_top = __reduce_max_sync(0xffffffffu, of_v ? e_here : NONE);
+            if (min(ev_top, UNIT_MOST) > eo + 1) {         // a larger unit
+                const int larger = max(min(ev_top, UNIT_MOST), UNIT_LEAST);
                 const float f = exp2_whole(max(eo - larger, -126));        // the first one: of zeros
                 eo = larger;
 #pragma unroll
@@ -293,17 +293,14 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[nt][i][e] *= f;
             }
-            bool close = true;
+            const int ev_here = of_v ? e_here - eo : 0;
+            const bool close = __all_sync(0xffffffffu, ev_here >= -4 && ev_here <= 1);
+            const float mine = ex_here == NONE ? 0.f : exp2_whole((lane & 1) ? (close ? ev_here : 0) : e_here);
+            float fk[4], fv[4];                            // 2^(K's exponent), what V's makes of a weight
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-                ev[h] = ev[h] == 0 ? 0 : ev[h] - 128 - eo;
-                close &= ev[h] >= -4 && ev[h] <= 1;
-            }
-            float dv[4], undo[4];
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                dv[h] = close ? (float)ev[h] : 0.f;
-                undo[h] = close ? exp2_whole(-ev[h]) : 1.f;
+                fk[h] = __shfl_sync(0xffffffffu, mine, h * 8);
+                fv[h] = __shfl_sync(0xffffffffu, mine, h * 8 + 1);
             }
 
             // ---- scores: keys g, g + 8, g + 16, g + 24, rows 2 t4 and 2 t4 + 1 ----
@@ -326,59 +323,68 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
                         keys_to_f16<FMT>(w1, f[1], f[3]);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            if (i == 0 && j == 0) mma_f16_16816_first(x[kk][nt], f, qf[nt][0][0], qf[nt][0][1]);
+                            if (i == 0 && j == 0) mma_f16_16816_first(x[kk][nt], f, qf[nt][0][0], qf[nt][0][1], start[nt].x, start[nt].y);
                             else mma_f16_16816(x[kk][nt], f, qf[nt][4 * i + j][0], qf[nt][4 * i + j][1]);
                         }
                     }
             }
             uint32_t pb[2][NT][2];                         // weights: row g, keys 2 t4, 2 t4 + 1 (and + 8) of each 16
-            float t[NT][2][4];                             // exponents of the weights
+            float2 t[NT][4];                               // exponents of the weights
             float top = -INFINITY;
-            auto exponents = [&](int nt, int e, float ref) {
+            auto exponents = [&](int nt, float2 ref) {
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
-                    const float c = rr[nt][e] * fk[h], y = x[h >> 1][nt][(h & 1) * 2 + e];
-                    t[nt][e][h] = fmaf(FMT == CACHE_INT8 ? y - excess[nt][e] : y, c, dv[h] - ref);
-                    if (edge && !pa_sees(a, pos[nt][e], j0 + h * 8 + g)) t[nt][e][h] = -INFINITY;
+                    const float(&y)[4] = x[h >> 1][nt];
+                    t[nt][h] = f2_of(f2_fma(f2_pack(y[(h & 1) * 2], y[(h & 1) * 2 + 1]), f2_mul(f2_pack(rr[nt].x, rr[nt].y), f2_pack(fk[h], fk[h])), f2_pack(ref.x, ref.y)));
+                    if (edge) {
+                        if (!pa_sees(a, pos[nt][0], j0 + h * 8 + g)) t[nt][h].x = -INFINITY;
+                        if (!pa_sees(a, pos[nt][1], j0 + h * 8 + g)) t[nt][h].y = -INFINITY;
+                    }
                 }
             };
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) {
+                exponents(nt, minus[nt]);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    exponents(nt, e, m[nt][e]);
-                    top = max3(top, max3(t[nt][e][0], t[nt][e][1], t[nt][e][2]), t[nt][e][3]);
-                }
-            if (__any_sync(0xffffffffu, top > 15.f)) {     // the first keys of a row (m is -inf), or a maximum that grew by 9 or more
+                for (int h = 0; h < 4; ++h) top = max3(top, t[nt][h].x, t[nt][h].y);
+            }
+            if (__any_sync(0xffffffffu, top > 14.f)) {     // the first keys of a row (minus is inf), or a maximum that grew by 8 or more
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int nt = 0; nt < NT; ++nt) {
+                    float most[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        const float(&y)[4] = x[h >> 1][nt];
+                        if (t[nt][h].x != -INFINITY) most[0] = fmaxf(most[0], y[(h & 1) * 2] * (rr[nt].x * fk[h]));
+                        if (t[nt][h].y != -INFINITY) most[1] = fmaxf(most[1], y[(h & 1) * 2 + 1] * (rr[nt].y * fk[h]));
+                    }
+                    float ref[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float most = -INFINITY;
-#pragma unroll
-                        for (int h = 0; h < 4; ++h)
-                            if (t[nt][e][h] != -INFINITY) most = fmaxf(most, (x[h >> 1][nt][(h & 1) * 2 + e] - excess[nt][e]) * (rr[nt][e] * fk[h]));
-                        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 4));
-                        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 8));
-                        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 16));
-                        if (most - 6.f > m[nt][e]) {
-                            const float f = pa_exp2(m[nt][e] - (most - 6.f));
-                            m[nt][e] = most - 6.f;
-                            l[nt][e] *= f;
+                        float &now = e ? minus[nt].y : minus[nt].x, &sum = e ? l[nt].y : l[nt].x;
+                        most[e] = fmaxf(most[e], __shfl_xor_sync(0xffffffffu, most[e], 4));
+                        most[e] = fmaxf(most[e], __shfl_xor_sync(0xffffffffu, most[e], 8));
+                        most[e] = fmaxf(most[e], __shfl_xor_sync(0xffffffffu, most[e], 16));
+                        if (6.f - most[e] < now) {
+                            const float f = pa_exp2(6.f - most[e] - now);
+                            now = 6.f - most[e];
+                            sum *= f;
 #pragma unroll
                             for (int i = 0; i < D / 16; ++i) { o[nt][i][e] *= f; o[nt][i][e + 2] *= f; }
                         }
-                        exponents(nt, e, m[nt][e] == -INFINITY ? 0.f : m[nt][e]);       // a row that has seen nothing yet: all weights 0
+                        ref[e] = now == INFINITY ? 0.f : now;      // a row that has seen nothing yet: all weights 0
                     }
+                    exponents(nt, make_float2(ref[0], ref[1]));
+                }
             }
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const float y0 = pa_exp2(t[nt][0][h]), y1 = pa_exp2(t[nt][1][h]);
-                    l[nt][0] = fmaf(y0, undo[h], l[nt][0]);
-                    l[nt][1] = fmaf(y1, undo[h], l[nt][1]);
-                    pb[h >> 1][nt][h & 1] = transpose_8x8(pack_f16x2(y0, y1));
+                    const uint64_t y = f2_pack(pa_exp2(t[nt][h].x), pa_exp2(t[nt][h].y));
+                    const float2 z = f2_of(f2_mul(y, f2_pack(fv[h], fv[h])));
+                    l[nt] = f2_of(f2_add(f2_pack(l[nt].x, l[nt].y), y));
+                    pb[h >> 1][nt][h & 1] = transpose_8x8(pack_f16x2(z.x, z.y));
                 }
             }
 
@@ -428,9 +434,9 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
                             for (int y = 0; y < 2; ++y) {
                                 float d[4] = {0.f, 0.f, 0.f, 0.f};
                                 mma_f16_1688(d, f[2 * y], f[2 * y + 1], pb[kk][nt][y]);
-                                const float fv = exp2_whole(ev[2 * kk + y]);
+                                const float f8 = exp2_whole(__shfl_sync(0xffffffffu, ev_here, (2 * kk + y) * 8 + 1));
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) o[nt][i][e] = fmaf(d[e], fv, o[nt][i][e]);
+                                for (int e = 0; e < 4; ++e) o[nt][i][e] = fmaf(d[e], f8, o[nt][i][e]);
                             }
                     }
                 }
@@ -447,12 +453,12 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float sum = l[nt][e];
+                float sum = e ? l[nt].y : l[nt].x;
                 sum += __shfl_xor_sync(0xffffffffu, sum, 4);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 8);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 16);
                 const int r = nt * 8 + 2 * t4 + e;
-                if (g == 0) { stat_m[warp][r] = m[nt][e]; stat_l[warp][r] = sum; }
+                if (g == 0) { stat_m[warp][r] = -(e ? minus[nt].y : minus[nt].x); stat_l[warp][r] = sum; }
 #pragma unroll
                 for (int i = 0; i < D / 16; i += 2) {
                     const int c = (g * CPT + 2 * i) / 4;
