@@ -29,8 +29,8 @@
 // tile's K and V (TMA, two tiles ahead of the products at most), and their exponents beside them; four converting warps write them as
 // bf16 numbers code * 2^e, which are exact, where the products take them from; everything after that is as above.  Bound by the
 // conversions: 640 instructions a warp for 128 keys, beside the softmax warps' own, and by the power limit.  Measured: the chunk of 4,096
-// rows 1.83 - 1.89 ms (1.61 without converting anything; copies made by the converting warps themselves 1.93), the prompt of 8,192
-// rows 1.48 ms, 16 requests of 6 rows over 8,192 keys 133 us.  K and q as fp16 with a scale for 32 keys need fewer conversions, but
+// rows 1.57 - 1.71 ms (with the loop over K and V unrolled the code misses the instruction cache: 1.75 - 1.89; with copies made by the
+// converting warps themselves 1.93), 16 requests of 6 rows over 8,192 keys 122 us.  K and q as fp16 with a scale for 32 keys need fewer conversions, but
 // more in the softmax warps and at each piece: 1.91 ms, and 102 us instead of 84 for the window chunk of 64 channels.
 #include <type_traits>
 
@@ -165,7 +165,7 @@ __device__ __forceinline__ void tc_convert(const PagedArgs &a, const PaShare &sh
             const int j0 = pa_tile(w.u, t) * C::KT;
             const bool clears = pa_clears<C::KT>(a, w.u, j0);
             if (!mbar_wait_suspended_warp(&staged[in.idx], in.phase, abort_flag)) return;
-#pragma unroll
+#pragma unroll 1                                           // K and V by the same code: it has to stay in the instruction cache
             for (int comp = 0; comp < 2; ++comp) {
             if (!mbar_wait_suspended_warp(&empty[st.idx], st.phase ^ 1, abort_flag)) return;
             const int e = exp8_clamp(exps[in.idx * 32 + comp * 16 + cw * 4 + (lane >> 3)], FMT);
