@@ -381,7 +381,8 @@ cb_status cb_paged_attention8(const cb_page_pool8 *pool, int32_t layer, const vo
     if (s != CB_OK || nothing) return s;
     // Up to 32 flattened rows per request and KV head: the warp-level kernel, in units of 16 rows that share the codes through L2.
     // Measured on 16 requests of 8,192 keys, 8 KV heads x 128 (268 MB), warp-level against tensor-memory kernel, e4m3 / int8: 8 rows 61 / 62
-    // against 164 / 175 us, 16 rows 73 / 79, 24 and 32 rows 120 / 132; of 64 channels 32 rows 89 / 98 against 123 / 128 us.
+    // against 126 / 130 us, 16 rows 67 / 71, 32 rows 111 / 121; of 64 channels 32 rows 84 / 91 against 110 / 113; 64 requests of 1,024
+    // keys, 32 rows 77 / 84 against 82 / 83.
     const bool few = (long long)max_new * a.group <= 32 || a.group > 128;
     if (!few) a.q_min = 2;
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -181,8 +181,9 @@ struct alignas(16) PaSum { long long tiles; int units, most; };
 // Where there are no more pairs than blocks and the longest one is at most EVEN tiles above an equal share, every pair goes
 // to a block of its own: joining two parts costs about that much (32 requests with a window of 1,024 keys, 256 pairs of 17
 // or 18 tiles of 64 keys: 38 us split, see k_paged_attn_few; for the tensor-memory kernel the number was taken over, not
-// measured).  A block takes at least q_min tiles, one more where the longest pair has more than LONG (0: never).
-template <int ROWS, int KT, int THREADS, int EVEN = 4, int LONG = 0>
+// measured).  A block takes at least q_min tiles, and the root of (tiles of the longest pair / JOINS), where its tiles and the
+// join of its pair's parts take equally long (0: q_min alone).
+template <int ROWS, int KT, int THREADS, int EVEN = 4, int JOINS = 0>
 __device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int cap, PaShare *share, PaSum *sums)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -247,7 +248,7 @@ __device__ __forceinline__ void pa_schedule(const PagedArgs &a, int *staged, int
     }
     long long line = all * a.Hkv;
     long long q = pa_div(line + gridDim.x - 1, gridDim.x);
-    q = max(q, (long long)a.q_min + (LONG && most > LONG ? 1 : 0));
+    q = max(q, (long long)max(a.q_min, JOINS ? 1 + (int)sqrtf((float)max(most - 1, 0) / (JOINS ? JOINS : 1)) : 0));
     long long pre = (before + incl - mine) * a.Hkv;
     int even = 0;
     if ((long long)all_units * a.Hkv <= gridDim.x && most <= q + EVEN && most > 0) {

@@ -137,8 +137,8 @@ __global__ void __launch_bounds__(128, Few8Cfg<D, NT>::BLOCKS) k_paged8_attn_few
     constexpr int UNIT_LEAST = -60, UNIT_MOST = 20;    // of the output
 
     // Windows of 1,024 keys and 4 sinks, 10 tiles a pair, 256 pairs: 26 us split, 29 in blocks of their own; 8 tiles a pair 21.5 either way.
-    // One tile a block against two where there are blocks enough: one request of 1,024 keys 9.0 / 9.5 us, 2,048 10.8 / 9.9, 4,096 15.1 / 12.1
-    // (each round of the join takes eight parts).
+    // A tile a block against two and more where there are blocks enough: one request of 1,024 keys 9.0 / 9.5 us, 4,096 15.1 / 12.1; 100,000 keys
+    // and a single KV head 62 us with two tiles, 27 with nine (each round of the join takes eight parts).
     pa_schedule<C::ROWS, C::KT, 128, 1, 12>(a, reinterpret_cast<int *>(smem_raw), (int)(C::SMEM / 4), &share, warp_sums);
     PaWalk<C::ROWS, C::KT> w;
     if (!w.open(a, share)) return;
