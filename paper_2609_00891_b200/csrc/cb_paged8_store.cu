@@ -16,7 +16,8 @@ namespace cb {
 // further runs of the tile.  Finding a run costs a warp some 500 instructions, so a team does several heads after one look
 // at it where there is work enough (440 us against 656).
 // Measured: 4,099 fp32 rows x 64 layers x 8 heads x 128 into int8 blocks of 64 rows 440 us = 6.1 TB/s; one row of each of 32
-// requests, 64 layers, e4m3 blocks of 16, 21 us; 3,400 rows of one layer 11 us.
+// requests, 64 layers, e4m3 blocks of 16, 19 us; 3,400 rows of one layer 11 us.  Short runs are bound by the instructions that find
+// them: 36 layers of 2 heads x 64, five rows of each of 500 requests, 75 us = 0.8 TB/s.
 template <bool F32, int FMT, int D>
 __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
 {
@@ -31,7 +32,8 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
     const int comp = lane >> 4, half = lane & 16;
     const int mate = warp % a.team, unit = warp / a.team;                  // of the team, and which one in the block
     const unsigned tile = blockIdx.x / (unsigned)a.groups;
-    const int head0 = ((int)(blockIdx.x - tile * a.groups) * a.heads + unit % a.heads) * a.repeat, stride = 8 / a.team / a.heads;
+    const int group = (int)(blockIdx.x - tile * a.groups);
+    int head0 = (group * a.heads + unit % a.heads) * a.repeat, repeat = a.repeat, stride = 8 / a.team / a.heads, my_run = unit / a.heads;
     const int layer = blockIdx.y;
     const int sub = (lane & 15) / LPR, c8 = (lane % LPR) * 8;              // row of a load, first channel
     const long long row_bytes = a.s_st * (F32 ? 4 : 2);
@@ -58,9 +60,17 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
     const bool begins = ok && !(near && ((here ? prev_here : prev_back) >> p.block_log2) == my_block);
     const unsigned heads = __ballot_sync(0xffffffffu, begins);
     const int rank = __popc(heads & ((1u << lane) - 1u)), n_runs = __popc(heads);
+    // Many short runs: all heads of a run in turn by the team that found it (64 layers, a row of each of 500 requests: 180 us against
+    // 254; from five runs on, rows of 17 in fp32 173 us against 156).  Tiles of 32 rows at most, which come by here once.
+    if (n_runs >= 8 && a.tile <= 32) {
+        head0 = group * a.heads * a.repeat;
+        repeat = a.heads * a.repeat;
+        stride = 8 / a.team;
+        my_run = unit;
+    }
 
     for (int run0 = 0; run0 < n_runs; run0 += stride) {                    // the same rounds in every warp: they meet below
-        const int run = run0 + unit / a.heads;
+        const int run = run0 + my_run;
         const bool there = run < n_runs;
         const int at = there ? __ffs(__ballot_sync(0xffffffffu, begins && rank == run)) - 1 : 0;
         const long long first = r0 + at;
@@ -110,7 +120,7 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
         });
         const bool few = (kept >> kept_k0) >> (PART * RPI - 1) <= 1u;      // a step's single row, for one
 
-        for (int head = head0; head < head0 + a.repeat; ++head) {
+        for (int head = head0; head < head0 + repeat; ++head) {
         const bool live = there && head < p.H;
         const int h = min(head, p.H - 1);
         const char *src_h = src + (long long)h * a.s_sh * (F32 ? 4 : 2);
