@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(256, 2) k_paged8_store(const Store8Args a)
     // 254; from five runs on, rows of 17 in fp32 173 us against 156).  Tiles of 32 rows at most, which come by here once.
     if (n_runs >= 8 && a.tile <= 32) {
         head0 = group * a.heads * a.repeat;
-        repeat = a.heads * a.repeat;
+        repeat = min(a.heads * a.repeat, p.H - head0);
         stride = 8 / a.team;
         my_run = unit;
     }

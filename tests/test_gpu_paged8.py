@@ -162,6 +162,25 @@ def test_store_of_many_requests(kind, n, L, H):
 
 
 @KINDS
+@pytest.mark.parametrize("block,dtype,d,H,L", [(16, torch.bfloat16, 128, 5, 20), (32, torch.bfloat16, 128, 3, 20), (16, torch.float32, 128, 8, 20),
+                                               (8, torch.float32, 64, 2, 24), (32, torch.float32, 64, 9, 8), (64, torch.bfloat16, 64, 1, 24)])
+def test_store_of_short_runs_in_many_layers(kind, block, dtype, d, H, L):
+    """One to four rows of each of 400 requests, some of them twice: enough work that a thread block has 32 rows of the slot map."""
+    page, n = 64, 400
+    rng = np.random.default_rng(block + d)
+    pool = _pool(kind, L, n, page, block, H, d)
+    slot, row = [], []
+    for p in rng.permutation(n):
+        first = int(rng.integers(0, page - 4))
+        for o in range(first, first + int(rng.integers(1, 5))):
+            again = 1 + int(rng.integers(0, 8) == 0)
+            row += [len(set(row))] * again
+            slot += [int(p) * page + o] * again
+    x = [y[:, row] for y in _rows(L, len(set(row)), H, d, dtype, 9, spread=3.0)]
+    _store(pool, _state(pool), x, slot)
+
+
+@KINDS
 def test_store_and_load_nothing(kind):
     pool = _pool(kind, 2, 3, 8, 8, 2, 64)
     state = _state(pool)
